@@ -377,6 +377,97 @@ int lvr_stream_read(const void *src_dev, int64_t bytes, uint32_t *sink_dev, int3
 /* n = keys held per (sequence, KV head); n_indexed = keys inside groups. */
 int lvr_length(const lvr_index *ix, int64_t *n_host, int64_t *n_indexed_host);
 
+/* ---- A paged cache: from the prompt to the index -------------------------------------------------
+ * lvr_build takes the keys and values of a prompt as rows.  The calls below bring them there: new
+ * tokens' K and V go into the pages of a paged cache, rotated by their positions on the way
+ * (lvr_paged_append); the new tokens attend everything their sequence holds (lvr_paged_attention,
+ * a chunk of a prompt or a single token); the pages' rows are laid out for lvr_build
+ * (lvr_paged_gather).  The pools of pages are the caller's memory, K and V apart; one lvr_paged
+ * serves all layers of the same shape.  The conventions at the top of this file hold.
+ *
+ * A batch is n_seqs sequences (0 .. 4096, LVR_E_CAPACITY beyond):
+ *   seq_start_dev [n_seqs + 1] int32, ascending: sequence b brings the tokens seq_start[b] ..
+ *                 seq_start[b+1]-1 of the packed token arrays, perhaps none.  Tokens before
+ *                 seq_start[0] and behind seq_start[n_seqs] belong to no sequence: nothing is stored
+ *                 for them and their rows of the outputs stay as they were.
+ *   seq_len_dev   [n_seqs] int32: keys the sequence holds, its new ones among them.  New token i of m
+ *                 therefore sits at position seq_len - m + i.  A token at a negative position is
+ *                 not stored and attends nothing.
+ *   table_dev     [n_seqs][table_width] int32: the page of positions p * page_size ..
+ *                 (p + 1) * page_size - 1.  An entry outside 0 .. n_pages-1 stands for no page:
+ *                 nothing is stored there, and its keys take no part in an attention.  The same for
+ *                 positions past table_width * page_size (at most 2^30, LVR_E_CAPACITY beyond).
+ *                 Entries past the pages of seq_len keys are not looked at.
+ * These arrays are read on the device when the call's work runs: a captured call replays with what they
+ * hold then.  n_tokens is the number of rows of the packed arrays (n_tokens times n_q_heads, or 16 if
+ * that is more, at most 2^27, LVR_E_CAPACITY beyond); rows are [n_tokens][heads][head_dim] with the stride between tokens (elements)
+ * given, heads of a token contiguous, so that q, k and v may be slices of one projection's output.
+ * Token strides and page strides are multiples of 16 bytes. */
+typedef struct lvr_paged lvr_paged; /* opaque, owned by the library */
+
+/* Which coordinates are rotated together: HALVES c and c + rot_dim / 2; NEIGHBOURS 2 c and 2 c + 1. */
+enum lvr_rot_pairs { LVR_ROT_HALVES = 0, LVR_ROT_NEIGHBOURS = 1 };
+
+typedef struct lvr_paged_config {
+    int32_t n_q_heads;    /* H_q, at most 1024                                                       */
+    int32_t n_kv_heads;   /* H_kv, divides H_q (any ratio), at most 256                              */
+    int32_t head_dim;     /* this build supports 128                                                 */
+    int32_t kv_dtype;     /* lvr_dtype of the pages, of new K, V, q, and of the outputs               */
+    int32_t page_size;    /* tokens per page: a power of two, 16 .. 65536                            */
+    int32_t rot_dim;      /* leading coordinates that are rotated, a multiple of 16 up to head_dim; 0: none */
+    int32_t rot_axes;     /* axes a position has, 1 .. 4 (a text's has one; time, row, column: three)  */
+    int32_t rot_pairs;    /* lvr_rot_pairs                                                           */
+    int64_t n_pages;      /* pages in each pool, 1 .. 2^30                                           */
+    int64_t page_strides[3]; /* element strides of the pools: page, kv head, token; head_dim is contiguous */
+    float scale;          /* sigma; 0 means 1/sqrt(head_dim)                                         */
+} lvr_paged_config;
+
+/* inv_freq_host [rot_dim / 2]: radians per position of every pair (any finite values: scaled and
+ * extended variants of the rotation differ here and nowhere else); axis_host [rot_dim / 2]: which axis
+ * of the position turns the pair, 0 .. rot_axes-1, NULL = axis 0.  Both are copied; with rot_dim = 0
+ * they are not looked at.  Allocates the work space of the attention on the current device, which has
+ * to be current in every later call (LVR_E_STATE otherwise). */
+int lvr_paged_create(const lvr_paged_config *cfg_host, const double *inv_freq_host, const int32_t *axis_host,
+                     lvr_paged **out);
+int lvr_paged_destroy(lvr_paged *pc);
+/* Device bytes lvr_paged_create would allocate for this configuration (0 if it is invalid). */
+size_t lvr_paged_bytes(const lvr_paged_config *cfg_host);
+
+/* Stores the new tokens' K and V in their pages.  K is rotated on the way, and q, if there is one (q_dev
+ * and q_out_dev NULL: none), into q_out_dev [n_tokens][n_q_heads][head_dim], contiguous: pair (x, y) of a
+ * head becomes (x cos a - y sin a, x sin a + y cos a), a = position[axis] * inv_freq, in fp32 with the
+ * angle exact to 2^-32 of a turn, rounded once to the cache's type.  positions_dev [n_tokens][rot_axes] int32, any values; NULL:
+ * the token's position in its sequence, on every axis.  token_strides_host = {k, v, q}.  q_out_dev may be
+ * q_dev itself where q is contiguous; other overlaps of inputs and outputs are not allowed.  Two tokens of one
+ * call must not share a row of a page. */
+int lvr_paged_append(lvr_paged *pc, void *k_pages_dev, void *v_pages_dev, const void *k_new_dev, const void *v_new_dev,
+                     const void *q_dev, void *q_out_dev, const int64_t token_strides_host[3],
+                     const int32_t *positions_dev, const int32_t *seq_start_dev, const int32_t *seq_len_dev,
+                     const int32_t *table_dev, int64_t table_width, int64_t n_seqs, int64_t n_tokens, void *stream);
+
+/* Attention of the new tokens over the pages (Sec. 2 "Attention", causal): the token at position p attends the
+ * keys at positions 0 .. p of its sequence, or with window > 0 the last `window` of them (window = 0: all;
+ * negative: LVR_E_INVALID).  Softmax over those keys of sigma <q, k>; a token with no key to attend gives
+ * zeros.  K and V of keys that no token sees may hold anything, infinities and NaN included; a value that is
+ * infinite or NaN reaches the tokens that see it and no others.
+ *   q_dev    [n_tokens][n_q_heads][head_dim] of kv_dtype, q_token_stride elements between tokens
+ *   out_dev  [n_tokens][n_q_heads][head_dim] of kv_dtype, contiguous, apart from q
+ * Sums, maxima and the output are held in fp32; bf16 caches round the probabilities to bf16 before they meet V.
+ * Launches kernels only (no allocation, no host synchronisation, no memset): the call may be recorded under HIP graph
+ * capture.  Calls on one lvr_paged share its work space and must be ordered by the caller, those of replayed graphs
+ * among them. */
+int lvr_paged_attention(lvr_paged *pc, const void *k_pages_dev, const void *v_pages_dev, const void *q_dev,
+                        int64_t q_token_stride, const int32_t *seq_start_dev, const int32_t *seq_len_dev,
+                        const int32_t *table_dev, int64_t table_width, int64_t n_seqs, int64_t n_tokens, int32_t window,
+                        void *out_dev, void *stream);
+
+/* The pages' rows as lvr_build reads them: row j of KV head h of sequence b goes to K_out_dev / V_out_dev
+ * [n_seqs][n_kv_heads][n][head_dim] (contiguous) for j < min(seq_len[b], n); other rows, and those whose table
+ * entry stands for no page, stay as they were.  n at most 2^30. */
+int lvr_paged_gather(lvr_paged *pc, const void *k_pages_dev, const void *v_pages_dev, const int32_t *seq_len_dev,
+                     const int32_t *table_dev, int64_t table_width, int64_t n_seqs, int64_t n, void *K_out_dev,
+                     void *V_out_dev, void *stream);
+
 const char *lvr_strerror(int code);
 /* hipError_t value of the most recent failing HIP call made by this library on this thread. */
 int lvr_last_hip_error(void);

@@ -34,6 +34,7 @@ LVR_SEPARATE_KERNELS = 2
 LVR_CONCURRENT_UPDATE = 4
 LVR_KV_IN_HOST_MEMORY = 8
 LVR_INDEX_AUTO, LVR_INDEX_SAME, LVR_INDEX_FP8, LVR_INDEX_FP6 = 0, 1, 2, 3
+LVR_ROT_HALVES, LVR_ROT_NEIGHBOURS = 0, 1
 LVR_OK, LVR_E_INVALID, LVR_E_UNSUPPORTED, LVR_E_CAPACITY = 0, -1, -2, -3
 LVR_E_OVERFLOW, LVR_E_HIP, LVR_E_NOMEM, LVR_E_STATE = -4, -5, -6, -7
 
@@ -60,6 +61,14 @@ class lvr_stats(C.Structure):
         return {k: int(getattr(self, k)) for k, _ in self._fields_}
 
 
+class lvr_paged_config(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("kv_dtype", C.c_int32),
+        ("page_size", C.c_int32), ("rot_dim", C.c_int32), ("rot_axes", C.c_int32), ("rot_pairs", C.c_int32),
+        ("n_pages", C.c_int64), ("page_strides", C.c_int64 * 3), ("scale", C.c_float),
+    ]
+
+
 class lvr_profile(C.Structure):
     _fields_ = [("ms", C.c_double * 9), ("launches", C.c_int64 * 9)]
 
@@ -74,6 +83,7 @@ EXPORTS = [
     "lvr_profile_enable", "lvr_profile_read", "lvr_threshold", "lvr_export_reservoir", "lvr_publish", "lvr_query1", "lvr_append_decode_step", "lvr_host_bytes",
     "lvr_subspace_thresholds", "lvr_sparse_attention_static",
     "lvr_set_bound_test", "lvr_stream_read", "lvr_export_labels", "lvr_export_channel_scales",
+    "lvr_paged_create", "lvr_paged_destroy", "lvr_paged_bytes", "lvr_paged_append", "lvr_paged_attention", "lvr_paged_gather",
 ]
 
 _lib = None
@@ -127,6 +137,13 @@ def lib():
     L.lvr_stream_read.argtypes = [vp, i64, vp, C.c_int32, vp]
     L.lvr_threshold.argtypes = [vp, vp, C.c_int, C.c_float, vp, vp]
     L.lvr_export_reservoir.argtypes = [vp, vp]
+    L.lvr_paged_create.argtypes = [C.POINTER(lvr_paged_config), C.POINTER(C.c_double), C.POINTER(C.c_int32), C.POINTER(vp)]
+    L.lvr_paged_destroy.argtypes = [vp]
+    L.lvr_paged_bytes.argtypes = [C.POINTER(lvr_paged_config)]
+    L.lvr_paged_bytes.restype = C.c_size_t
+    L.lvr_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, C.POINTER(i64), vp, vp, vp, vp, i64, i64, i64, vp]
+    L.lvr_paged_attention.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, C.c_int32, vp, vp]
+    L.lvr_paged_gather.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp]
     L.lvr_strerror.argtypes = [C.c_int]
     L.lvr_strerror.restype = C.c_char_p
     L.lvr_last_hip_error.restype = C.c_int
@@ -430,3 +447,143 @@ def lvr_export_index(h, cfg: lvr_config):
                                   slot_pos.ctypes.data_as(C.c_void_p), keys.ctypes.data_as(C.c_void_p)),
            "lvr_export_index")
     return centres, radii, slot_pos, keys
+
+
+# ---- the paged cache: from the prompt to the index
+class PagedHandle(C.c_void_p):
+    """What lvr_paged_create returns: the C handle, with what the calls check tensors against."""
+    cfg: lvr_paged_config
+    dtype: torch.dtype
+
+
+def make_paged_config(*, n_q_heads, n_kv_heads, head_dim=128, kv_dtype=LVR_BF16, page_size, n_pages, layout="head", page_strides=None,
+                      scale=0.0, rot_dim=0, rot_axes=1, rot_pairs=LVR_ROT_HALVES) -> lvr_paged_config:
+    """layout: "head" for pools [page][head][token][head_dim], "token" for [page][token][head][head_dim], both contiguous; or
+    page_strides, the element strides {page, head, token} of pools laid out otherwise."""
+    if page_strides is None:
+        if layout not in ("head", "token"):
+            raise ValueError('layout must be "head" or "token"')
+        page = n_kv_heads * page_size * head_dim
+        page_strides = (page, page_size * head_dim, head_dim) if layout == "head" else (page, head_dim, n_kv_heads * head_dim)
+    return lvr_paged_config(n_q_heads, n_kv_heads, head_dim, kv_dtype, page_size, rot_dim, rot_axes, rot_pairs, n_pages,
+                            (C.c_int64 * 3)(*page_strides), scale)
+
+
+def lvr_paged_bytes(cfg: lvr_paged_config) -> int:
+    return int(lib().lvr_paged_bytes(C.byref(cfg)))
+
+
+def lvr_paged_create(cfg: lvr_paged_config, inv_freq=None, axis=None) -> PagedHandle:
+    """inv_freq: radians per position of each of the rot_dim / 2 pairs; axis: the axis of each, None for the first."""
+    half = cfg.rot_dim // 2
+    freq = ax = None
+    if half > 0:
+        if inv_freq is None or len(inv_freq) != half or (axis is not None and len(axis) != half):
+            raise ValueError(f"inv_freq (and axis) must have rot_dim / 2 = {half} entries")
+        freq = (C.c_double * half)(*[float(x) for x in inv_freq])
+        ax = None if axis is None else (C.c_int32 * half)(*[int(x) for x in axis])
+    h = PagedHandle()
+    _check(lib().lvr_paged_create(C.byref(cfg), freq, ax, C.byref(h)), "lvr_paged_create")
+    h.cfg = lvr_paged_config.from_buffer_copy(cfg)
+    h.dtype = torch.bfloat16 if cfg.kv_dtype == LVR_BF16 else torch.float32
+    return h
+
+
+def lvr_paged_destroy(h) -> None:
+    _check(lib().lvr_paged_destroy(h), "lvr_paged_destroy")
+
+
+def _pool(h, t: torch.Tensor, name: str):
+    """A pool of pages: [page][head][token][head_dim] or [page][token][head][head_dim] with the strides of the configuration."""
+    c = h.cfg
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != h.dtype:
+        raise ValueError(f"{name} must be {h.dtype}, got {t.dtype}")
+    want, shape = tuple(c.page_strides), tuple(t.shape)
+    if t.dim() == 4 and t.stride(3) == 1:
+        s = t.stride()
+        if shape == (c.n_pages, c.n_kv_heads, c.page_size, c.head_dim) and s[:3] == want:
+            return t.data_ptr()
+        if shape == (c.n_pages, c.page_size, c.n_kv_heads, c.head_dim) and (s[0], s[2], s[1]) == want:
+            return t.data_ptr()
+    raise ValueError(f"{name} must be {c.n_pages} pages of {c.page_size} tokens and {c.n_kv_heads} heads of {c.head_dim} with strides "
+                     f"{want} (page, head, token), got {shape} with strides {tuple(t.stride())}")
+
+
+def _tokens(h, t: torch.Tensor, heads: int, n, name: str):
+    """Rows of new tokens [n_tokens][heads][head_dim], the heads of a token contiguous.  Returns pointer and token stride."""
+    c = h.cfg
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != h.dtype:
+        raise ValueError(f"{name} must be {h.dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != c.head_dim or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must be [{'n_tokens' if n is None else n}][{heads}][{c.head_dim}], got {tuple(t.shape)}")
+    if t.shape[0] == 0:
+        return t.data_ptr(), heads * c.head_dim
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != c.head_dim):
+        raise ValueError(f"the heads of a token in {name} must be contiguous")
+    # (the stride of one token's array says nothing)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * c.head_dim
+
+
+def _whole(t: torch.Tensor, dtype, shape, name: str):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {list(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _batch(seq_start, seq_len, table):
+    if table.dim() != 2:
+        raise ValueError("table must be [n_seqs][table_width]")
+    n, width = table.shape
+    start = None if seq_start is None else _whole(seq_start, torch.int32, (n + 1,), "seq_start")
+    return start, _whole(seq_len, torch.int32, (n,), "seq_len"), _whole(table, torch.int32, (n, width), "table"), width, n
+
+
+def lvr_paged_append(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q=None, q_out=None, positions=None, stream=None) -> None:
+    """k_new, v_new [n_tokens][n_kv_heads][128], q and q_out [n_tokens][n_q_heads][128] (q_out contiguous, or q itself);
+    positions [n_tokens][rot_axes] int32, None: the token's position in its sequence; seq_start, seq_len, table: int32."""
+    kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
+    k, ks = _tokens(h, k_new, h.cfg.n_kv_heads, None, "k_new")
+    n = k_new.shape[0]
+    v, vs = _tokens(h, v_new, h.cfg.n_kv_heads, n, "v_new")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    qp = qo = None
+    qs = 0
+    if q is not None:
+        qp, qs = _tokens(h, q, h.cfg.n_q_heads, n, "q")
+        qo = _whole(q_out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "q_out")
+    pos = None if positions is None else _whole(positions, torch.int32, (n, max(h.cfg.rot_axes, 1)), "positions")
+    start, length, tab, width, seqs = _batch(seq_start, seq_len, table)
+    _check(lib().lvr_paged_append(h, kp, vp, k, v, qp, qo, (C.c_int64 * 3)(ks, vs, qs), pos, start, length, tab, width, seqs, n,
+                                  _stream(stream)), "lvr_paged_append")
+
+
+def lvr_paged_attention(h, k_pages, v_pages, q, seq_start, seq_len, table, out, window=0, stream=None) -> None:
+    """q [n_tokens][n_q_heads][128], out the same and contiguous; seq_start, seq_len, table: int32."""
+    kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
+    qp, qs = _tokens(h, q, h.cfg.n_q_heads, None, "q")
+    n = q.shape[0]
+    o = _whole(out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "out")
+    start, length, tab, width, seqs = _batch(seq_start, seq_len, table)
+    _check(lib().lvr_paged_attention(h, kp, vp, qp, qs, start, length, tab, width, seqs, n, int(window), o, _stream(stream)),
+           "lvr_paged_attention")
+
+
+def lvr_paged_gather(h, k_pages, v_pages, seq_len, table, K_out, V_out, stream=None) -> None:
+    """K_out, V_out: contiguous device tensors [n_seqs][n_kv_heads][n][128]; rows past a sequence's end stay as they are."""
+    kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
+    _, length, tab, width, seqs = _batch(None, seq_len, table)
+    if K_out.dim() != 4:
+        raise ValueError("K_out must be [n_seqs][n_kv_heads][n][head_dim]")
+    n = K_out.shape[2]
+    shape = (seqs, h.cfg.n_kv_heads, n, h.cfg.head_dim)
+    ko, vo = _whole(K_out, h.dtype, shape, "K_out"), _whole(V_out, h.dtype, shape, "V_out")
+    _check(lib().lvr_paged_gather(h, kp, vp, length, tab, width, seqs, n, ko, vo, _stream(stream)), "lvr_paged_gather")

@@ -278,6 +278,8 @@ inline bool on_home_device(const lvr_index *ix) {
 
 }  // namespace
 
+int lvr_note_hip_error(hipError_t e) { return hip_fail(e); }
+
 extern "C" {
 
 size_t lvr_arena_bytes(const lvr_config *cfg) {

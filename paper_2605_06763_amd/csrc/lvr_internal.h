@@ -136,6 +136,9 @@ static inline int8_t *lvr_chan_exp(const lvr_index *ix) {
     return reinterpret_cast<int8_t *>((p + 127) & ~(uintptr_t)127);
 }
 
+// keeps a failing HIP call's error for lvr_last_hip_error; returns LVR_E_HIP
+int lvr_note_hip_error(hipError_t e);
+
 // ---- launchers (each returns a hipError_t from hipGetLastError after the launch) ----
 // channel exponents from the keys about to be indexed (element strides ks for (sequence, head, token)); one launch; with V it also
 // copies the value rows and the key rows from k_first on into the arena (lvr_launch_copy_kv at row 0)

@@ -1,0 +1,50 @@
+// The paged cache's handle and what its kernels share: where a token, a page and a row lie.
+#pragma once
+#include "lvr_internal.h"
+
+#define LVR_PAGED_MAX_SEQS 4096
+
+struct lvr_paged {
+    lvr_paged_config cfg;
+    int device;
+    float sigma;
+    uint64_t *turns;      // [64] turns per position of every pair, in units of 2^-64 turn (whole turns dropped)
+    int32_t *axis;        // [64] axis of every pair
+};
+
+// What every kernel over a batch gets.
+struct lvr_paged_batch {
+    const int32_t *seq_start, *seq_len, *table;
+    int32_t n_seqs, n_tokens, table_width;
+    int32_t page_shift;        // log2 of the page size
+    int32_t n_pages;
+    int64_t page_stride, head_stride, row_stride;   // bytes
+};
+
+hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
+                                      int64_t q_stride_bytes, int32_t window, void *out, hipStream_t st);
+
+#ifdef __HIPCC__
+// The page that holds a position of a sequence, or -1: a position outside the table, or an entry outside the pool.
+__host__ __device__ __forceinline__ int32_t lvr_page_of(const lvr_paged_batch &b, int seq, int64_t position) {
+    if (position < 0 || position >= (int64_t)b.table_width << b.page_shift) return -1;
+    const int32_t page = b.table[(int64_t)seq * b.table_width + (position >> b.page_shift)];
+    return page >= 0 && page < b.n_pages ? page : -1;
+}
+// Bytes from the start of a pool to the row of a position in that page.
+__host__ __device__ __forceinline__ int64_t lvr_row_at(const lvr_paged_batch &b, int32_t page, int head, int64_t position) {
+    return page * b.page_stride + head * b.head_stride + (position & (((int64_t)1 << b.page_shift) - 1)) * b.row_stride;
+}
+
+// The sequence a row of the packed arrays belongs to: the last one that starts at or before it (an empty one starts where its
+// successor does).  -1 or n_seqs: none.  One load per 64 sequences and no dependent search; all lanes of a wave call it with the same t.
+__device__ __forceinline__ int lvr_seq_of(const lvr_paged_batch &b, int t) {
+    int before = 0;
+    for (int i0 = 0; i0 <= b.n_seqs; i0 += 64) {
+        const int i = i0 + lvr_lane();
+        const bool starts = i <= b.n_seqs && b.seq_start[i] <= t;
+        before += __popcll(__ballot(starts));
+    }
+    return before - 1;
+}
+#endif

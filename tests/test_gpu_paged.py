@@ -1,0 +1,458 @@
+"""The paged cache on the GPU: append with rotation, attention of new tokens, pages to rows, against plain implementations in
+64 bits on the host.
+
+Tolerances are bounds: HALF_STEP is what one rounding to the type is off by relative to the value; what else enters is counted
+where it is used."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_06763_amd as L
+
+pytestmark = pytest.mark.gpu
+
+D = 128
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+class Cache:
+    """Pools with scattered pages and the tables of a batch.  lens: (new tokens, keys held) of every sequence."""
+
+    def __init__(self, lens, *, dtype="bf16", hq=8, hkv=2, page=16, layout="head", scale=0.0, rot_dim=0, rot_axes=1, pairs=L.LVR_ROT_HALVES,
+                 inv_freq=None, axis=None, seed=0, spare=2, extra_width=1, behind=0, gap=0):
+        self.g = torch.Generator().manual_seed(seed + 1)
+        self.lens, self.dtype, self.hq, self.hkv, self.page, self.layout = lens, dtype, hq, hkv, page, layout
+        self.dt, self.scale = DTYPES[dtype], scale if scale > 0 else 1 / math.sqrt(D)
+        used = [max(0, -(-n // page)) for _, n in lens]
+        self.width = max(used + [0]) + extra_width
+        self.n_pages = sum(used) + spare
+        order = torch.randperm(self.n_pages, generator=self.g).tolist()
+        self.table = torch.full((len(lens), self.width), -1, dtype=torch.int32)
+        for b, u in enumerate(used):
+            for p in range(u):
+                self.table[b, p] = order.pop()
+        starts = [gap]
+        for t, _ in lens:
+            starts.append(starts[-1] + t)
+        self.T = starts[-1] + behind
+        self.start = torch.tensor(starts, dtype=torch.int32)
+        self.len = torch.tensor([n for _, n in lens], dtype=torch.int32)
+        self.K, self.V = (self.randn(self.n_pages, hkv, page, D) for _ in range(2))     # [page][head][token][D], rounded to the type
+        self.cfg = L.make_paged_config(n_q_heads=hq, n_kv_heads=hkv, kv_dtype=L.LVR_BF16 if dtype == "bf16" else L.LVR_F32, page_size=page,
+                                       n_pages=self.n_pages, layout=layout, scale=scale, rot_dim=rot_dim, rot_axes=rot_axes, rot_pairs=pairs)
+        self.h = L.lvr_paged_create(self.cfg, inv_freq=inv_freq, axis=axis)
+
+    def randn(self, *shape):
+        return torch.randn(shape, generator=self.g).to(self.dt)
+
+    def pools(self):
+        to = (lambda p: p.cuda()) if self.layout == "head" else (lambda p: p.transpose(1, 2).contiguous().cuda())
+        return to(self.K), to(self.V)
+
+    def from_pool(self, p):
+        return p.cpu() if self.layout == "head" else p.cpu().transpose(1, 2).contiguous()
+
+    def batch(self):
+        return self.start.cuda(), self.len.cuda(), self.table.cuda()
+
+    def close(self):
+        L.lvr_paged_destroy(self.h)
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    def rows(self, b, n):
+        """K, V [hkv][n][D] and which of the n positions have a page."""
+        K, V = torch.zeros(self.hkv, n, D, dtype=torch.float64), torch.zeros(self.hkv, n, D, dtype=torch.float64)
+        held = torch.zeros(n, dtype=torch.bool)
+        for p in range(-(-n // self.page)):
+            id = int(self.table[b, p]) if p < self.width else -1
+            if 0 <= id < self.n_pages:
+                e = min(n, (p + 1) * self.page)
+                K[:, p * self.page:e], V[:, p * self.page:e] = self.K[id, :, :e - p * self.page].double(), self.V[id, :, :e - p * self.page].double()
+                held[p * self.page:e] = True
+        return K, V, held
+
+    def attention(self, q, window):
+        """The definition in 64 bits: outputs [T][hq][D] and how far off the kernel's may be; NaN rows belong to no sequence."""
+        out = torch.full((self.T, self.hq, D), math.nan, dtype=torch.float64)
+        tol = torch.zeros_like(out)
+        G, step = self.hq // self.hkv, HALF_STEP[self.dtype]
+        for b, (t, n) in enumerate(self.lens):
+            if t == 0:
+                continue
+            s0 = int(self.start[b])
+            K, V, held = self.rows(b, max(n, 0))
+            pos = torch.arange(n - t, n)[:, None]
+            j = torch.arange(max(n, 0))[None]
+            sees = (j <= pos) & held[None]
+            if window:
+                sees &= j > pos - window
+            for h in range(self.hq):
+                Kh, Vh = K[h // G], V[h // G]
+                qh = q[s0:s0 + t, h].double()
+                x = torch.where(sees, qh @ Kh.T * self.scale, torch.tensor(-math.inf, dtype=torch.float64))
+                some = sees.any(dim=1)
+                m = torch.where(some, x.amax(dim=1) if n > 0 else torch.zeros(t, dtype=torch.float64), torch.zeros(t, dtype=torch.float64))
+                w = torch.exp(x - m[:, None])
+                w = w / torch.where(some, w.sum(dim=1), torch.ones(t, dtype=torch.float64))[:, None]
+                for i in range(t):      # row by row, so that a value that is no number reaches the rows that see it alone
+                    v = sees[i]
+                    out[s0 + i, h] = w[i, v] @ Vh[v]
+                    size = w[i, v] @ Vh[v].abs() + out[s0 + i, h].abs()
+                    # A weight is off by the error of its score (128 products and sums of 2^-24 each, as many in the scaling), by
+                    # two roundings of the exponential, and for bf16 by its own rounding; the outputs by the weights' errors against the
+                    # size of what is summed, by the sums of up to n terms, and by the last rounding.
+                    S = (qh[i].abs() @ Kh[v].abs().T * self.scale).amax() if v.any() else torch.tensor(0.0)
+                    weight = 2 * (136 * 2.0 ** -24 * S + 2.0 ** -21) + (1.02 * step if self.dtype == "bf16" else 0)
+                    tol[s0 + i, h] = (weight + (int(v.sum()) + 64) * 2.0 ** -24) * size + step * out[s0 + i, h].abs()
+        return out, tol
+
+
+def check_attention(c, window=0, q=None, note=""):
+    q = c.randn(c.T, c.hq, D) if q is None else q
+    say(f"attention {note} lens={c.lens} {c.dtype} heads={c.hq}/{c.hkv} page={c.page} {c.layout} window={window}")
+    out = torch.full((c.T, c.hq, D), 7.0, dtype=c.dt, device="cuda")
+    L.lvr_paged_attention(c.h, *c.pools(), q.cuda(), *c.batch(), out, window=window)
+    torch.cuda.synchronize()
+    out = out.cpu().double()
+    ref, tol = c.attention(q, window)
+    inside = torch.zeros(c.T, dtype=torch.bool)
+    inside[int(c.start[0]):int(c.start[-1])] = True
+    assert (out[~inside] == 7).all(), "rows of no sequence were written"
+    out, ref, tol = out[inside], ref[inside], tol[inside]
+    finite = torch.isfinite(ref)
+    assert torch.equal(torch.isnan(out), torch.isnan(ref))
+    assert torch.equal(out[~finite & ~torch.isnan(ref)], ref[~finite & ~torch.isnan(ref)])
+    err = (out - ref).abs()[finite]
+    assert (err <= tol[finite]).all(), float((err - tol[finite]).max())
+    return out
+
+
+LENS = {
+    "one_key": [(1, 1)],
+    "single_tokens": [(1, 17), (1, 16), (1, 15), (0, 5), (1, 300), (1, 31), (1, 33)],
+    "long_single": [(1, 2500)],
+    "whole_prompts": [(5, 5), (17, 17), (0, 0), (64, 64)],
+    "chunks": [(33, 100), (1, 257), (7, 129), (16, 64)],
+    "one_chunk": [(130, 130)],
+    "late_chunk": [(70, 700), (3, 3)],
+    "beside_decodes": [(200, 333), (1, 90), (1, 1), (1, 513)],
+    "tokens_before_the_cache": [(5, 3), (1, 0), (4, 0), (2, 40)],
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", LENS)
+def test_attention_over_lengths(lens, dtype):
+    with Cache(LENS[lens], dtype=dtype, seed=3) as c:
+        check_attention(c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq, hkv", [(1, 1), (3, 1), (4, 4), (8, 1), (12, 2), (20, 1), (40, 8), (71, 1)])
+def test_attention_over_heads(hq, hkv, dtype):
+    with Cache([(1, 70), (9, 41), (1, 200)], dtype=dtype, hq=hq, hkv=hkv, seed=4) as c:
+        check_attention(c)
+
+
+@pytest.mark.parametrize("layout", ["head", "token"])
+@pytest.mark.parametrize("page", [16, 32, 128, 1024])
+def test_attention_over_pages(page, layout):
+    with Cache([(1, 70), (40, 300), (1, 1040)], page=page, layout=layout, seed=5) as c:
+        check_attention(c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [1, 7, 33, 64, 300, 100000])
+def test_attention_with_a_window(window, dtype):
+    with Cache([(1, 400), (90, 333), (5, 5), (1, 30)], dtype=dtype, seed=6) as c:
+        check_attention(c, window=window)
+
+
+def test_attention_with_a_scale_of_its_own():
+    with Cache([(3, 50)], scale=0.7, seed=7) as c:
+        check_attention(c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [0, 50])
+def test_what_no_token_sees_may_be_anything(window, dtype):
+    """NaN and infinities behind the end of a sequence, in spare pages, before every window, and in keys and values of later tokens."""
+    with Cache([(20, 90), (1, 200), (1, 17)], dtype=dtype, seed=8) as c:
+        seen = torch.zeros(c.n_pages, c.page, dtype=torch.bool)
+        for b, (t, n) in enumerate(c.lens):
+            for p in range(max(0, n - t - window + 1) if window else 0, n):
+                seen[c.table[b, p // c.page], p % c.page] = True
+        for pool in (c.K, c.V):
+            pool.transpose(1, 2)[~seen] = math.nan
+        check_attention(c, window=window, note="unseen")
+        c.V[c.table[0, 88 // c.page], :, 88 % c.page, 5] = math.nan      # only the last two tokens of the first sequence see it
+        c.V[c.table[0, 85 // c.page], 0, 85 % c.page, 77] = math.inf
+        c.V[c.table[1, 199 // c.page], 1, 199 % c.page, 3] = -math.inf
+        out = check_attention(c, window=window, note="seen by some")
+        assert torch.isfinite(out[:15]).all() and not torch.isfinite(out[18:20]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_missing_pages_take_no_part(dtype):
+    with Cache([(1, 300), (40, 200), (1, 20)], dtype=dtype, seed=9) as c:
+        c.table[0, 3], c.table[0, 7], c.table[0, 18] = -1, c.n_pages, 2 ** 31 - 1       # the last: the page of the new token
+        c.table[1, 0], c.table[1, 11] = -2 ** 31, -5
+        c.table[2, :] = -1                                                               # nothing at all: zeros
+        out = check_attention(c)
+        assert (out[41] == 0).all()
+
+
+def test_a_sequence_longer_than_its_table():
+    with Cache([(4, 60), (1, 30)], seed=10, extra_width=0) as c:
+        c.lens = [(4, 90), (1, 30)]
+        c.len = torch.tensor([90, 30], dtype=torch.int32)
+        check_attention(c)
+
+
+def test_rows_of_no_sequence_stay_as_they_were():
+    with Cache([(3, 20), (0, 9), (2, 40)], seed=11, behind=30, gap=5) as c:
+        check_attention(c)
+
+
+def test_attention_of_large_scores():
+    """Scores of some thousands in both directions: the maximum moves by more than the exponents' range from key to key."""
+    for dtype in ("bf16", "f32"):
+        with Cache([(1, 500), (30, 100)], dtype=dtype, seed=12) as c:
+            c.K *= 64
+            check_attention(c, note="large")
+            c.K[:, :, ::2] = -c.K[:, :, ::2].abs()
+            check_attention(c, q=c.randn(c.T, c.hq, D).abs() * 30, note="large, of one sign")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_query_rows_may_be_a_slice_of_a_projection(dtype):
+    with Cache([(6, 50), (1, 20)], dtype=dtype, seed=13) as c:
+        fused = c.randn(c.T, (c.hq + 2 * c.hkv) * D)
+        q = fused[:, :c.hq * D].unflatten(1, (c.hq, D))
+        a, b = (torch.zeros(c.T, c.hq, D, dtype=c.dt, device="cuda") for _ in range(2))
+        pools, batch, dev = c.pools(), c.batch(), fused.cuda()
+        L.lvr_paged_attention(c.h, *pools, dev[:, :c.hq * D].unflatten(1, (c.hq, D)), *batch, a)
+        L.lvr_paged_attention(c.h, *pools, q.contiguous().cuda(), *batch, b)
+        assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------------ append
+def rotated(x, pos, inv_freq, axis, rot, pairs):
+    """64 bits: x [T][heads][D], pos [T][axes]; and the size of what a rotated value is summed from."""
+    y, size = x.double().clone(), x.double().abs()
+    angle = pos.double()[:, axis] * torch.tensor(inv_freq, dtype=torch.float64)
+    cs, sn = angle.cos()[:, None], angle.sin()[:, None]
+    a, b = (slice(0, rot // 2), slice(rot // 2, rot)) if pairs == L.LVR_ROT_HALVES else (slice(0, rot, 2), slice(1, rot, 2))
+    u, w = y[..., a].clone(), y[..., b].clone()
+    y[..., a], y[..., b] = u * cs - w * sn, u * sn + w * cs
+    size[..., a] = size[..., b] = u.abs() + w.abs()
+    return y, size
+
+
+def freqs(rot, base=10000.0):
+    return [base ** (-2 * c / rot) for c in range(rot // 2)]
+
+
+def check_append(c, inv_freq, axis, rot, pairs, positions, with_q=True, sliced=True):
+    say(f"append lens={c.lens} {c.dtype} heads={c.hq}/{c.hkv} page={c.page} {c.layout} rot={rot} pairs={pairs} q={with_q}")
+    fused = c.randn(c.T, (c.hq + 2 * c.hkv) * D)
+    q, k, v = (x.unflatten(1, (-1, D)) for x in fused.split([c.hq * D, c.hkv * D, c.hkv * D], dim=1))
+    dev = fused.cuda()
+    dq, dk, dv = (x.unflatten(1, (-1, D)) for x in dev.split([c.hq * D, c.hkv * D, c.hkv * D], dim=1))
+    if not sliced:
+        dq, dk, dv = dq.contiguous(), dk.contiguous(), dv.contiguous()
+    kp, vp = c.pools()
+    qo = torch.full((c.T, c.hq, D), 7.0, dtype=c.dt, device="cuda")
+    L.lvr_paged_append(c.h, kp, vp, dk, dv, *c.batch(), q=dq if with_q else None, q_out=qo if with_q else None,
+                       positions=None if positions is None else positions.cuda())
+    torch.cuda.synchronize()
+    K, V, qo = c.from_pool(kp).double(), c.from_pool(vp).double(), qo.cpu().double()
+    pos = torch.zeros(c.T, max(c.cfg.rot_axes, 1), dtype=torch.int64) if positions is None else positions.long()
+    if positions is None:
+        for b, (t, n) in enumerate(c.lens):
+            s0 = int(c.start[b])
+            pos[s0:s0 + t] = torch.arange(n - t, n)[:, None]
+    kr, ks = rotated(k, pos, inv_freq, axis, rot, pairs) if rot else (k.double(), 0 * k.double())
+    qr, qs = rotated(q, pos, inv_freq, axis, rot, pairs) if rot else (q.double(), 0 * q.double())
+    # a sine is off by its argument's rounding (2^-24 of at most pi / 4, three times), the series' end and the sums of it, five
+    # more steps of 2^-24; the rotation by two products and a sum
+    rel, off = HALF_STEP[c.dtype], 12 * 2.0 ** -24
+    want_k, want_v = c.K.double().clone(), c.V.double().clone()
+    tol_k = torch.zeros_like(want_k)
+    for b, (t, n) in enumerate(c.lens):
+        for i in range(t):
+            p, s = n - t + i, int(c.start[b]) + i
+            id = int(c.table[b, p // c.page]) if 0 <= p < c.width * c.page else -1
+            if not 0 <= id < c.n_pages:
+                continue
+            at = (id, slice(None), p % c.page)
+            want_k[at], want_v[at] = kr[s], v[s].double()
+            tol_k[at] = rel * kr[s].abs() + off * ks[s]
+            tol_k[at][:, rot:] = 0
+    assert ((K - want_k).abs() <= tol_k).all(), float(((K - want_k).abs() - tol_k).max())
+    assert torch.equal(V, want_v)
+    inside = torch.zeros(c.T, dtype=torch.bool)
+    inside[int(c.start[0]):int(c.start[-1])] = with_q
+    assert (qo[~inside] == 7).all()
+    tol_q = rel * qr.abs() + off * qs
+    tol_q[..., rot:] = 0
+    assert ((qo - qr).abs() <= tol_q)[inside].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", ["one_key", "single_tokens", "whole_prompts", "chunks", "tokens_before_the_cache"])
+def test_append_over_lengths(lens, dtype):
+    f = freqs(128)
+    with Cache(LENS[lens], dtype=dtype, rot_dim=128, inv_freq=f, seed=20) as c:
+        check_append(c, f, [0] * 64, 128, L.LVR_ROT_HALVES, None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs", [L.LVR_ROT_HALVES, L.LVR_ROT_NEIGHBOURS])
+@pytest.mark.parametrize("rot", [0, 16, 64, 96, 128])
+def test_append_over_rotations(rot, pairs, dtype):
+    f = freqs(rot) if rot else None
+    with Cache([(5, 9), (1, 100)], dtype=dtype, rot_dim=rot, pairs=pairs, inv_freq=f, seed=21, layout="token") as c:
+        check_append(c, f, [0] * (rot // 2), rot, pairs, None)
+
+
+@pytest.mark.parametrize("axes", [1, 2, 3, 4])
+@pytest.mark.parametrize("hq, hkv", [(1, 1), (3, 1), (24, 8), (71, 1)])
+def test_append_over_axes_and_heads(hq, hkv, axes):
+    f = freqs(128)
+    axis = torch.randint(0, axes, (64,), generator=torch.Generator().manual_seed(axes)).tolist()
+    with Cache([(5, 9), (0, 3), (12, 40)], hq=hq, hkv=hkv, rot_dim=128, rot_axes=axes, inv_freq=f, axis=axis, seed=22, behind=4, gap=2) as c:
+        pos = torch.randint(-50, 5000, (c.T, axes), generator=c.g).to(torch.int32)
+        check_append(c, f, axis, 128, L.LVR_ROT_HALVES, pos)
+
+
+def test_append_of_keys_alone_and_of_whole_arrays():
+    f = freqs(64)
+    for with_q in (False, True):
+        with Cache([(5, 9), (3, 40)], rot_dim=64, inv_freq=f, seed=23) as c:
+            check_append(c, f, [0] * 32, 64, L.LVR_ROT_HALVES, None, with_q=with_q, sliced=False)
+
+
+def test_positions_far_off_and_below_zero():
+    """Angles of up to 2^31 radians and of frequencies above a turn per position; the reference's own angle is exact to 2^-53 of them."""
+    f = freqs(128, base=500000.0)
+    f[3], f[4], f[5] = 0.0, -0.75, 9.5
+    with Cache([(8, 8)], dtype="f32", rot_dim=128, inv_freq=f, seed=24) as c:
+        pos = torch.tensor([[0], [1], [-1], [10 ** 6], [2 ** 24 + 1], [-(2 ** 24)], [10 ** 8 + 1], [1048577]], dtype=torch.int32)
+        check_append(c, f, [0] * 64, 128, L.LVR_ROT_HALVES, pos)
+
+
+def test_appends_to_missing_pages_are_dropped():
+    f = freqs(128)
+    with Cache([(30, 50), (3, 20)], rot_dim=128, inv_freq=f, seed=25) as c:
+        c.table[0, 1], c.table[0, 2], c.table[1, 1] = -1, c.n_pages, 2 ** 31 - 1
+        check_append(c, f, [0] * 64, 128, L.LVR_ROT_HALVES, None)
+
+
+def test_query_is_rotated_in_place():
+    f = freqs(128)
+    with Cache([(7, 30)], rot_dim=128, inv_freq=f, seed=26) as c:
+        k, q = c.randn(c.T, c.hkv, D).cuda(), c.randn(c.T, c.hq, D).cuda()
+        out, again = torch.empty_like(q), q.clone()
+        L.lvr_paged_append(c.h, *c.pools(), k, k, *c.batch(), q=q, q_out=out)
+        L.lvr_paged_append(c.h, *c.pools(), k, k, *c.batch(), q=again, q_out=again)
+        assert torch.equal(out, again) and not torch.equal(out, q)
+
+
+# ------------------------------------------------------------------------------------------------ gather
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page, layout", [(16, "head"), (16, "token"), (64, "head"), (256, "token")])
+def test_gather(page, layout, dtype):
+    for n in (1, 15, 16, 300, 333):
+        with Cache([(0, 300), (0, 0), (0, 17), (0, 64), (0, 90)], dtype=dtype, page=page, layout=layout, seed=30) as c:
+            c.table[4, 0] = -1
+            say(f"gather n={n} {dtype} page={page} {layout}")
+            K, V = (torch.full((5, c.hkv, n, D), 7.0, dtype=c.dt, device="cuda") for _ in range(2))
+            kp, vp = c.pools()
+            _, length, table = c.batch()
+            L.lvr_paged_gather(c.h, kp, vp, length, table, K, V)
+            for b, (_, held) in enumerate(c.lens):
+                Kr, Vr, has = c.rows(b, min(held, n))
+                for got, ref in ((K, Kr), (V, Vr)):
+                    want = torch.full((c.hkv, n, D), 7.0, dtype=torch.float64)
+                    want[:, :min(held, n)][:, has] = ref[:, has]
+                    assert torch.equal(got[b].cpu().double(), want)
+
+
+# ------------------------------------------------------------------------------------------------ refusals
+def test_calls_refuse_what_they_cannot_take():
+    with Cache([(2, 20), (1, 40)], rot_dim=128, inv_freq=freqs(128), seed=40) as c:
+        kp, vp = c.pools()
+        start, length, table = c.batch()
+        q, k = c.randn(c.T, c.hq, D).cuda(), c.randn(c.T, c.hkv, D).cuda()
+        out = torch.empty_like(q)
+        K = torch.zeros(2, c.hkv, 40, D, dtype=c.dt, device="cuda")
+        attend = lambda **o: L.lvr_paged_attention(**dict(dict(h=c.h, k_pages=kp, v_pages=vp, q=q, seq_start=start, seq_len=length, table=table, out=out), **o))   # noqa: E731
+        append = lambda **o: L.lvr_paged_append(**dict(dict(h=c.h, k_pages=kp, v_pages=vp, k_new=k, v_new=k, seq_start=start, seq_len=length, table=table, q=q, q_out=out), **o))   # noqa: E731
+        gather = lambda **o: L.lvr_paged_gather(**dict(dict(h=c.h, k_pages=kp, v_pages=vp, seq_len=length, table=table, K_out=K, V_out=K.clone()), **o))   # noqa: E731
+        for call in (attend, append, gather):
+            for bad in (dict(k_pages=kp[:-1]), dict(v_pages=vp.float()), dict(k_pages=kp[:, :, :, :64]), dict(v_pages=vp.cpu()), dict(k_pages=kp.transpose(1, 2)[:, :, :1]),
+                        dict(seq_len=length.long()), dict(seq_len=length[:1]), dict(table=table[0]), dict(table=table[:1]), dict(table=table.T)):
+                with pytest.raises(ValueError):
+                    call(**bad)
+        for call in (attend, append):
+            for bad in (dict(seq_start=start[:-1]), dict(seq_start=start.float()), dict(q=q[:, :4]), dict(q=q.float()), dict(q=q.transpose(0, 1)), dict(q=q[..., ::2])):
+                with pytest.raises(ValueError):
+                    call(**bad)
+        for bad in (dict(out=out[:1]), dict(out=out.float()), dict(out=out.cpu())):
+            with pytest.raises(ValueError):
+                attend(**bad)
+        for bad in (dict(q=None), dict(q_out=None), dict(v_new=k[:1]), dict(k_new=k[:, :1]), dict(positions=torch.zeros(c.T, 2, dtype=torch.int32, device="cuda")),
+                    dict(positions=torch.zeros(c.T, 1, dtype=torch.int64, device="cuda"))):
+            with pytest.raises(ValueError):
+                append(**bad)
+        for bad in (dict(K_out=K[:1]), dict(V_out=K[:, :, :3]), dict(K_out=K.float()), dict(K_out=K[0])):
+            with pytest.raises(ValueError):
+                gather(**bad)
+
+        def refused(code, call, *a):
+            assert call(*a) == code
+
+        lib, big = L.lib(), 1 << 40
+        p = lambda t, off=0: t.data_ptr() + off   # noqa: E731
+        st = lambda *s: (L.binding.C.c_int64 * 3)(*s)   # noqa: E731
+        hq, hk = c.hq * D, c.hkv * D
+        att = lambda k=p(kp), v=p(vp), q=p(q), qs=hq, s=p(start), n=p(length), t=p(table), w=c.width, b=2, T=c.T, win=0, o=p(out): lib.lvr_paged_attention(c.h, k, v, q, qs, s, n, t, w, b, T, win, o, None)   # noqa: E731
+        for kw in (dict(k=None), dict(v=None), dict(q=None), dict(s=None), dict(n=None), dict(t=None), dict(o=None), dict(qs=hq - 8), dict(qs=hq + 4), dict(q=p(q, 2)),
+                   dict(k=p(kp, 8)), dict(v=p(vp, 4)), dict(o=p(out, 8)), dict(s=p(start, 2)), dict(n=p(length, 1)), dict(t=p(table, 2)), dict(w=-1), dict(b=-1), dict(T=-1),
+                   dict(win=-1), dict(o=p(q)), dict(qs=-hq), dict(qs=big)):
+            assert att(**kw) == L.LVR_E_INVALID, kw
+        for kw in (dict(b=4097), dict(w=1 << 27), dict(T=1 << 25)):
+            assert att(**kw) == L.LVR_E_CAPACITY, kw
+        assert att(T=0, q=None, o=None) == L.LVR_OK and att(b=0) == L.LVR_OK and att() == L.LVR_OK
+        app = lambda k=p(k), v=p(k), q=p(q), o=p(out), s=st(hk, hk, hq), pos=None, T=c.T: lib.lvr_paged_append(c.h, p(kp), p(vp), k, v, q, o, s, pos, p(start), p(length), p(table), c.width, 2, T, None)   # noqa: E731
+        for kw in (dict(k=None), dict(v=None), dict(q=None), dict(o=None), dict(s=None), dict(s=st(hk - 8, hk, hq)), dict(s=st(hk, hk + 4, hq)), dict(s=st(hk, hk, hq - 128)),
+                   dict(k=p(k, 8)), dict(q=p(q, 2)), dict(o=p(out, 4)), dict(pos=p(start, 1)), dict(q=p(q), o=p(q), s=st(hk, hk, hq + 128))):
+            assert app(**kw) == L.LVR_E_INVALID, kw
+        assert app() == L.LVR_OK
+        gat = lambda K1=p(K), V1=p(K), n=40: lib.lvr_paged_gather(c.h, p(kp), p(vp), p(length), p(table), c.width, 2, n, K1, V1, None)   # noqa: E731
+        for kw in (dict(K1=None), dict(V1=None), dict(K1=p(K, 8)), dict(n=-1)):
+            assert gat(**kw) == L.LVR_E_INVALID, kw
+        assert gat(n=(1 << 30) + 1) == L.LVR_E_CAPACITY and gat(n=0, K1=None) == L.LVR_OK
+        torch.cuda.synchronize()
+
+
+def test_empty_batches():
+    with Cache([], seed=41) as c:
+        z = lambda *s: torch.zeros(s, dtype=c.dt, device="cuda")   # noqa: E731
+        L.lvr_paged_attention(c.h, *c.pools(), z(0, c.hq, D), *c.batch(), z(0, c.hq, D))
+        L.lvr_paged_append(c.h, *c.pools(), z(0, c.hkv, D), z(0, c.hkv, D), *c.batch())
+        L.lvr_paged_gather(c.h, *c.pools(), *c.batch()[1:], z(0, c.hkv, 4, D), z(0, c.hkv, 4, D))
+        torch.cuda.synchronize()
