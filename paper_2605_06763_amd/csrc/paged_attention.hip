@@ -338,6 +338,296 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------------------------
+// 128 rows to a tile, 32 to each of four waves.  K and V tiles pass through LDS, two of each: while one is worked on the next is on
+// its way through registers.
+//
+// Matrix operand lanes: n = lane & 31 (query row), h = lane >> 5.  Score tile: 32 keys, result row 8 i + 4 h + j is register 4 i + j.
+// bf16 (tiles of 64 keys): registers 8 t .. 8 t + 7 of a score tile are at once the second product's operand for 16 keys, of which lanes
+// (., h) contribute 8 h .. 8 h + 7; for that K row 16 (i / 2) + 8 h + 4 (i % 2) + j is stored as row 8 i + 4 h + j.  V is
+// read transposed (four keys of one coordinate per lane and read).
+// fp32 (tiles of 32 keys): register r is the operand for the keys 8 i + 4 h + j themselves, and a lane's 16-byte read of V holds
+// the coordinates 4 n .. 4 n + 3, one for each of four result tiles.
+// 16-byte pieces of a row are stored at their number xor something of the row's, so that rows do not meet in the same banks.
+// ---------------------------------------------------------------------------------------------------------------------------
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <typename KT>
+struct Rows128;
+
+template <>
+struct Rows128<lvr_bf16_t> {
+    static constexpr int ELT = 2, ROWB = 256, TK = 64, NT = 2, PIECES = 16;
+    typedef bf16x8 Q[8];
+    static __device__ __forceinline__ void load_q(const char *row, int h, Q &q) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            q[s] = row ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(row + (2 * s + h) * 16)) : bf16x8{};
+    }
+    static __device__ __forceinline__ int key_of_k_row(int r) { return (r & 35) | ((r & 16) ? 16 : 0) | ((r & 4) << 1) | ((r & 8) >> 1); }
+    static __device__ __forceinline__ int k_piece(int r, int c) { return c ^ (r & 15); }
+    static __device__ __forceinline__ int v_piece(int key, int c) { return c ^ ((key & 3) << 2); }
+    static __device__ __forceinline__ int key_of(int h, int kt, int r) { return 32 * kt + 16 * (r >> 3) + 8 * h + (r & 7); }
+    static __device__ __forceinline__ int coordinate(int h, int dt, int r) { return 32 * dt + 8 * (r >> 2) + 4 * h + (r & 3); }
+    static __device__ __forceinline__ void scores(const char *k, const Q &q, int n, int h, f32x16 (&s)[NT]) {
+#pragma unroll
+        for (int kt = 0; kt < NT; ++kt) {
+            f32x16 c = {0.f};
+            const char *row = k + (kt * 32 + n) * ROWB;
+#pragma unroll
+            for (int st = 0; st < 8; ++st) {
+                const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(row + k_piece(n, 2 * st + h) * 16));
+                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[st], c, 0, 0, 0);
+            }
+            s[kt] = c;
+        }
+    }
+    static __device__ __forceinline__ void add(const char *v, const f32x16 (&p)[NT], int lane, f32x16 (&o)[4], float &l) {
+        const int i16 = lane & 15, key = (lane >> 5) * 8 + (i16 >> 2);
+        const char *at = v + key * ROWB + (i16 & 1) * 8;
+        const int piece = ((lane >> 4) & 1) * 2 + ((i16 & 3) >> 1);
+#pragma unroll
+        for (int kt = 0; kt < NT; ++kt)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                uint32_t w[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    w[c] = pack_bf16(p[kt][8 * t + 2 * c], p[kt][8 * t + 2 * c + 1]);
+                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[c]), bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
+                }
+                const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) {
+                    const char *src = at + (32 * kt + 16 * t) * ROWB + v_piece(key, dt * 4 + piece) * 16;
+                    typedef __attribute__((address_space(3))) s16x4 *Lds;
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(src));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(src + 4 * ROWB));
+                    const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb, o[dt], 0, 0, 0);
+                }
+            }
+    }
+    static __device__ __forceinline__ bool odd(const uint4 &v) { return Rows16<lvr_bf16_t>::odd_v(v); }
+    static __device__ __forceinline__ float element(const char *v, int key, int c) {
+        return lvr_bf16_lo(*reinterpret_cast<const uint16_t *>(v + key * ROWB + v_piece(key, c >> 3) * 16 + (c & 7) * 2));
+    }
+};
+
+template <>
+struct Rows128<lvr_f32_t> {
+    static constexpr int ELT = 4, ROWB = 512, TK = 32, NT = 1, PIECES = 32;
+    typedef float4 Q[16];
+    static __device__ __forceinline__ void load_q(const char *row, int h, Q &q) {
+#pragma unroll
+        for (int s = 0; s < 16; ++s) q[s] = row ? *reinterpret_cast<const float4 *>(row + (2 * s + h) * 16) : make_float4(0, 0, 0, 0);
+    }
+    static __device__ __forceinline__ int key_of_k_row(int r) { return r; }
+    static __device__ __forceinline__ int k_piece(int r, int c) { return c ^ (r & 31); }
+    static __device__ __forceinline__ int v_piece(int, int c) { return c; }
+    static __device__ __forceinline__ int key_of(int h, int, int r) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+    static __device__ __forceinline__ int coordinate(int h, int dt, int r) { return 4 * (8 * (r >> 2) + 4 * h + (r & 3)) + dt; }
+    static __device__ __forceinline__ void scores(const char *k, const Q &q, int n, int h, f32x16 (&s)[NT]) {
+        f32x16 c = {0.f};
+        const char *row = k + n * ROWB;
+#pragma unroll
+        for (int st = 0; st < 16; ++st) {
+            const float4 a = *reinterpret_cast<const float4 *>(row + k_piece(n, 2 * st + h) * 16);
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, q[st].x, c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, q[st].y, c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, q[st].z, c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, q[st].w, c, 0, 0, 0);
+        }
+        s[0] = c;
+    }
+    static __device__ __forceinline__ void add(const char *v, const f32x16 (&p)[NT], int lane, f32x16 (&o)[4], float &l) {
+        const int n = lane & 31, h = lane >> 5;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            l += p[0][r];
+            const float4 a = *reinterpret_cast<const float4 *>(v + key_of(h, 0, r) * ROWB + n * 16);
+            o[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, p[0][r], o[0], 0, 0, 0);
+            o[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, p[0][r], o[1], 0, 0, 0);
+            o[2] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, p[0][r], o[2], 0, 0, 0);
+            o[3] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, p[0][r], o[3], 0, 0, 0);
+        }
+    }
+    static __device__ __forceinline__ bool odd(const uint4 &v) {
+        return (v.x & 0x7f800000u) == 0x7f800000u || (v.y & 0x7f800000u) == 0x7f800000u || (v.z & 0x7f800000u) == 0x7f800000u ||
+               (v.w & 0x7f800000u) == 0x7f800000u;
+    }
+    static __device__ __forceinline__ float element(const char *v, int key, int c) { return *reinterpret_cast<const float *>(v + key * ROWB + c * 4); }
+};
+
+template <typename KT>
+__global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArgs a, lvr_paged_batch bt) {
+    typedef Rows128<KT> R;
+    constexpr int TK = R::TK, LPR = R::PIECES, RPI = 64 / LPR;   // lanes to a row, rows to a load of the wave
+    enum { NONE = 1, ODD = 2 };
+    __shared__ __align__(16) char s_k[2][TK * R::ROWB], s_v[2][TK * R::ROWB];
+    __shared__ __align__(16) int s_flags[2][4];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = lvr_lane(), n = lane & 31, h = lane >> 5;
+    const int kvh = blockIdx.x % a.n_kv;
+    Tile t;
+    if (!find_tile<128>(bt, a.G, a.window, blockIdx.x / a.n_kv, t)) return;   // the whole workgroup
+
+    const int row0 = t.row0 + wave * 32, row = row0 + n;
+    const int token = row / a.G, head = kvh * a.G + row - token * a.G;
+    const bool has_row = row < t.rows;
+    const bool has_rows = row0 < t.rows;
+    typename R::Q q;
+    R::load_q(has_row ? a.q + (int64_t)(t.first_token + token) * a.q_stride + (int64_t)head * LVR_D * R::ELT : nullptr, h, q);
+    const int last = t.pos0 + token;                 // keys this row sees: first .. last
+    const int first = a.window && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
+    // the wave's rows: some of them see wlo .. whi - 1, all of them all_lo .. all_hi - 1; and the workgroup's
+    const int wlast = (row0 + 31 < t.rows ? row0 + 31 : t.rows - 1) / a.G, wfirst = row0 / a.G;
+    const int whi = has_rows ? t.pos0 + wlast + 1 : 0, wlo = a.window ? t.pos0 + wfirst - a.window + 1 : 0;
+    const int all_hi = t.pos0 + wfirst + 1, all_lo = a.window ? t.pos0 + wlast - a.window + 1 : 0;
+    const int tile_last = (t.row0 + 127 < t.rows ? t.row0 + 127 : t.rows - 1) / a.G;
+    const int tile_all_hi = t.pos0 + t.row0 / a.G + 1, tile_all_lo = a.window ? t.pos0 + tile_last - a.window + 1 : 0;
+
+    float m = -INFINITY, l = 0.f;
+    f32x16 o[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) o[dt] = f32x16{0.f};
+
+    // staging: this wave's rows of a tile lie in one page
+    uint4 kr[4], vr[4];
+    int flags = 0;
+    const int srow = wave * 4 * RPI + lane / LPR, piece = lane % LPR;
+    const int group = wave * 4 * RPI & ~15;
+    auto page_of = [&](int k0) { return k0 + group < t.hi ? __builtin_amdgcn_readfirstlane(lvr_page_of(bt, t.seq, k0 + group)) : -1; };
+    auto load = [&](int k0, int page) {
+        const int64_t at = page < 0 ? kvh * bt.head_stride : lvr_row_at(bt, page, kvh, k0 + group);   // no page: some memory of the pool
+        const char *kp = a.k_pages + at, *vp = a.v_pages + at;
+        const bool partly = k0 < tile_all_lo || k0 + TK > tile_all_hi;
+        flags = page < 0 ? NONE : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = srow + i * RPI;
+            kr[i] = *reinterpret_cast<const uint4 *>(kp + (R::key_of_k_row(r) - group) * bt.row_stride + R::k_piece(r, piece) * 16);
+            vr[i] = *reinterpret_cast<const uint4 *>(vp + (r - group) * bt.row_stride + R::v_piece(r, piece) * 16);
+        }
+        return partly;
+    };
+    auto store = [&](int buf, int k0, bool partly) {
+        if (partly || flags) {
+            // a row of V that no query row sees is memory nobody has written; one that some see meets the others with weight zero,
+            // which an infinity or a NaN would survive
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = k0 + srow + i * RPI;
+                if (flags || key < t.lo || key >= t.hi) vr[i] = make_uint4(0, 0, 0, 0);
+                odd |= R::odd(vr[i]);
+            }
+            if (__any(odd)) flags |= ODD;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            *reinterpret_cast<uint4 *>(s_k[buf] + (srow + i * RPI) * R::ROWB + piece * 16) = kr[i];
+            *reinterpret_cast<uint4 *>(s_v[buf] + (srow + i * RPI) * R::ROWB + piece * 16) = vr[i];
+        }
+        if (lane == 0) s_flags[buf][wave] = flags;
+    };
+
+    int k0 = t.lo & ~(TK - 1), buf = 0;
+    bool next_partly = false;
+    if (k0 < t.hi) {
+        next_partly = load(k0, page_of(k0));
+        store(0, k0, next_partly);
+    }
+    int page = page_of(k0 + TK);
+    __syncthreads();
+    for (; k0 < t.hi; k0 += TK, buf ^= 1) {   // uniform over the workgroup
+        const bool more = k0 + TK < t.hi;
+        if (more) {
+            next_partly = load(k0 + TK, page);
+            page = page_of(k0 + 2 * TK);
+        }
+        if (k0 < whi && k0 + TK > wlo) {
+            const int4 f4 = *reinterpret_cast<const int4 *>(s_flags[buf]);
+            const int f = __builtin_amdgcn_readfirstlane(f4.x | f4.y | f4.z | f4.w);
+            f32x16 p[R::NT];
+            R::scores(s_k[buf], q, n, h, p);
+            const bool partly = k0 < all_lo || k0 + TK > all_hi || (f & NONE);
+            if (partly) {
+#pragma unroll
+                for (int kt = 0; kt < R::NT; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = k0 + R::key_of(h, kt, r);
+                        bool hidden = key < first || key > last;
+                        if (f & NONE) hidden |= (s_flags[buf][(key - k0) / (TK / 4)] & NONE) != 0;
+                        if (hidden) p[kt][r] = -INFINITY;
+                    }
+            }
+            float top = p[0][0];
+#pragma unroll
+            for (int kt = 0; kt < R::NT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, p[kt][r]);
+            top *= a.unit;
+            if (__any(top > m + RAISE)) {
+                const float raised = fmaxf(m, fmaxf(top, __shfl_xor(top, 32, 64)));
+                const float scale = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - raised);
+                m = raised;
+                l *= scale;
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) o[dt] *= scale;
+            }
+            const float base = m == -INFINITY ? 0.f : m;   // nothing seen so far: every weight below is 2^-inf
+#pragma unroll
+            for (int kt = 0; kt < R::NT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[kt][r], a.unit, -base));
+            if (partly && (f & ODD)) {
+                // rare: key by key on the vector units, so that a row that does not see a key does not meet its value
+#pragma unroll 1
+                for (int c = 0; c < TK; ++c) {
+                    const int kt = c >> 5, r = (c & 31) >> 1, h2 = c & 1;
+                    float w = 0.f;
+#pragma unroll
+                    for (int kk = 0; kk < R::NT; ++kk)
+#pragma unroll
+                        for (int rr = 0; rr < 16; ++rr) w = kk == kt && rr == r ? p[kk][rr] : w;
+                    if (h == h2) l += w;
+                    w = __shfl(w, n + 32 * h2, 64);
+                    const int key = R::key_of(h2, kt, r);
+                    if (k0 + key < first || k0 + key > last || (s_flags[buf][key / (TK / 4)] & NONE)) continue;
+#pragma unroll
+                    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[dt][e] += w * R::element(s_v[buf], key, R::coordinate(h, dt, e));
+                }
+            } else {
+                R::add(s_v[buf], p, lane, o, l);
+            }
+        }
+        if (more) store(buf ^ 1, k0 + TK, next_partly);
+        __syncthreads();
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (!has_row) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;   // nothing seen: zeros
+    char *dst = a.out + ((int64_t)(t.first_token + token) * a.n_kv * a.G + head) * LVR_D * R::ELT;
+    if constexpr (R::ELT == 2) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<uint2 *>(dst + R::coordinate(h, dt, r) * 2) =
+                    make_uint2(pack_bf16(o[dt][r] * inv, o[dt][r + 1] * inv), pack_bf16(o[dt][r + 2] * inv, o[dt][r + 3] * inv));
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            *reinterpret_cast<float4 *>(dst + R::coordinate(h, 0, r) * 4) = make_float4(o[0][r] * inv, o[1][r] * inv, o[2][r] * inv, o[3][r] * inv);
+    }
+}
+
 }  // namespace
 
 hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
@@ -352,9 +642,15 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.G = pc->cfg.n_q_heads / pc->cfg.n_kv_heads;
     a.window = window;
     a.unit = pc->sigma * LOG2E;
-    const int64_t tiles = (int64_t)b.n_tokens * a.G / 16 + b.n_seqs;
+    const bool wide = (int64_t)b.n_tokens * a.G > 32 * (int64_t)b.n_seqs;
+    const int64_t tiles = (int64_t)b.n_tokens * a.G / (wide ? 128 : 16) + b.n_seqs;
     const dim3 grid((unsigned)(tiles * a.n_kv));
-    if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
-    else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
+    if (wide) {
+        if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_rows128_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
+        else hipLaunchKernelGGL(paged_attention_rows128_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
+    } else {
+        if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
+        else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
+    }
     return hipGetLastError();
 }
