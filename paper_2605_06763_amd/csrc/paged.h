@@ -10,6 +10,8 @@ struct lvr_paged {
     float sigma;
     uint64_t *turns;      // [64] turns per position of every pair, in units of 2^-64 turn (whole turns dropped)
     int32_t *axis;        // [64] axis of every pair
+    float *part;          // partial results of the attention
+    uint32_t *ticket;     // zero between calls
 };
 
 // What every kernel over a batch gets.
@@ -21,6 +23,9 @@ struct lvr_paged_batch {
     int64_t page_stride, head_stride, row_stride;   // bytes
 };
 
+// work space of the attention, whatever the batch
+size_t lvr_paged_partial_bytes();
+size_t lvr_paged_ticket_bytes();
 hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
                                       int64_t q_stride_bytes, int32_t window, void *out, hipStream_t st);
 

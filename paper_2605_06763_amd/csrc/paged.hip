@@ -241,14 +241,16 @@ void free_all(lvr_paged *pc) {
 }
 
 struct Sizes {
-    size_t turns, axis, total;
+    size_t turns, axis, ticket, part, total;
 };
 Sizes sizes_of(const lvr_paged_config *) {
     auto al = [](size_t b) { return (b + 255) / 256 * 256; };
     Sizes s;
     s.turns = al(PAIRS * sizeof(uint64_t));
     s.axis = al(PAIRS * sizeof(int32_t));
-    s.total = s.turns + s.axis;
+    s.ticket = al(lvr_paged_ticket_bytes());
+    s.part = al(lvr_paged_partial_bytes());
+    s.total = s.turns + s.axis + s.ticket + s.part;
     return s;
 }
 
@@ -289,8 +291,11 @@ int lvr_paged_create(const lvr_paged_config *cfg, const double *inv_freq, const 
     hipError_t e = hipGetDevice(&pc->device);
     if (e == hipSuccess) e = hipMalloc((void **)&pc->turns, s.total);
     if (e == hipSuccess) {
-        pc->axis = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(pc->turns) + s.turns);
-        e = hipMemset(pc->turns, 0, s.total);
+        char *at = reinterpret_cast<char *>(pc->turns) + s.turns;
+        pc->axis = reinterpret_cast<int32_t *>(at);
+        pc->ticket = reinterpret_cast<uint32_t *>(at + s.axis);
+        pc->part = reinterpret_cast<float *>(at + s.axis + s.ticket);
+        e = hipMemset(pc->turns, 0, s.turns + s.axis + s.ticket);
         if (e == hipSuccess) e = hipMemcpy(pc->turns, turns, sizeof(turns), hipMemcpyHostToDevice);
         if (e == hipSuccess) e = hipMemcpy(pc->axis, axes, sizeof(axes), hipMemcpyHostToDevice);
         if (e == hipSuccess) e = hipDeviceSynchronize();

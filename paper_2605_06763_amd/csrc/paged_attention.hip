@@ -15,6 +15,8 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
+// Pieces of work a launch aims at, over all KV heads (tiles of 16 rows, of 128 rows).
+constexpr int ROWS16_PIECES = 1024, ROWS128_PIECES = 512;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -31,48 +33,119 @@ struct AttnArgs {
     int64_t q_stride;    // bytes per token
     int32_t n_kv, G, window;
     float unit;          // sigma * log2 e
+    int32_t target;      // pieces of work to make of the batch per KV head; 0: tiles are not cut
+    float *part;
+    uint32_t *ticket;    // a line for each slot of a cut tile
 };
 
-// A tile of TM packed rows of one sequence: which, and what its rows see.
+// A piece of work: a tile of TM packed rows of one sequence against a run of the keys they see.
 struct Tile {
     int seq, row0, rows;       // first packed row within the sequence; rows of the sequence
     int first_token;           // of the sequence, in the packed arrays
     int pos0;                  // position of the sequence's first new token
     int lo, hi;                // keys that any row of the tile sees: lo .. hi - 1
+    int begin, end;            // the run
+    int split, splits;         // which run of how many
+    int slot;                  // where its partial result goes, if there is more than one run
 };
 
-// Tiles are numbered sequence by sequence: those of sequence b start at seq_start[b] * G / TM + b, which leaves at most
-// one number unused per sequence and needs no sum over the sequences before it.
-template <int TM>
-__device__ __forceinline__ bool find_tile(const lvr_paged_batch &b, int G, int window, int x, Tile &t) {
-    int before = 0;
-    for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
-        const int i = i0 + lvr_lane();
-        bool starts = false;
-        if (i < b.n_seqs) {
-            int s = b.seq_start[i];
-            s = s < 0 ? 0 : (s > b.n_tokens ? b.n_tokens : s);
-            starts = (s * G) / TM + i <= x;
-        }
-        before += __popcll(__ballot(starts));
-    }
-    if (before == 0) return false;
-    t.seq = before - 1;
-    int s0 = b.seq_start[t.seq], s1 = b.seq_start[t.seq + 1], n = b.seq_len[t.seq];
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+
+// What sequence i brings, by the arrays on the device; whatever they hold, rows stay within the packed arrays and the table.
+__device__ __forceinline__ void sequence(const lvr_paged_batch &b, int i, int &s0, int &s1, int &n) {
+    s0 = b.seq_start[i];
+    s1 = b.seq_start[i + 1];
+    n = b.seq_len[i];
     s0 = s0 < 0 ? 0 : (s0 > b.n_tokens ? b.n_tokens : s0);
     s1 = s1 < s0 ? s0 : (s1 > b.n_tokens ? b.n_tokens : s1);
     n = n < 0 ? 0 : n;
-    t.first_token = s0;
-    t.rows = (s1 - s0) * G;
-    t.row0 = (x - ((s0 * G) / TM + t.seq)) * TM;
-    if (t.row0 < 0 || t.row0 >= t.rows) return false;
-    t.pos0 = n - (s1 - s0);
-    const int last_row = (t.row0 + TM < t.rows ? t.row0 + TM : t.rows) - 1;
-    t.hi = t.pos0 + last_row / G + 1;
-    if (t.hi > b.table_width << b.page_shift) t.hi = b.table_width << b.page_shift;
-    t.lo = window ? t.pos0 + t.row0 / G - window + 1 : 0;
-    if (t.lo < 0) t.lo = 0;
-    return true;
+}
+
+// Piece x of the batch, for one KV head.  The host knows neither how many tokens a sequence brings nor how many keys it holds, so
+// every workgroup works out the division for itself, each wave on its own: a sequence's tiles are cut into runs of L
+// keys, L such that the batch makes about `target` pieces of the same size (but none under MIN_RUN keys; target 0: no cuts).  There are
+// at most target + n_tokens * G / TM + n_seqs pieces, and at most 2 * target of tiles that are cut: a cut sequence
+// has at most twice as many runs as its keys are times L, and all keys of all tiles are at most target times L.
+// The last tiles come first: in a prompt they see most keys.
+template <int TM, int MIN_RUN>
+__device__ __forceinline__ bool find_work(const lvr_paged_batch &b, int G, int window, int target, int x, Tile &t) {
+    const int lane = lvr_lane();
+    const int reach = window ? window + TM / G + 2 : 0;   // keys a tile can see
+    int tiles = 0, span = 0;
+    auto look = [&](int i) {
+        tiles = span = 0;
+        if (i < b.n_seqs) {
+            int s0, s1, n;
+            sequence(b, i, s0, s1, n);
+            tiles = ((s1 - s0) * G + TM - 1) / TM;
+            span = window && n > reach ? reach : (n > 0 ? n : 1);
+            return (float)(s1 - s0);
+        }
+        return 0.f;
+    };
+    float keys = 0.f, tokens = 0.f;
+    for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
+        tokens += look(i0 + lane);
+        keys += (float)tiles * (float)span;
+    }
+    tokens = wave_sum(tokens);
+    if (tokens > (float)b.n_tokens) return false;   // seq_start is not ascending: no piece is where another expects it
+    int L = 1 << 30;
+    if (target > 0) {
+        const float want = wave_sum(keys) * 1.001f / (float)target;   // (more than what the sum was rounded by)
+        L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? 1 << 30 : ((int)want + 64) & ~63);
+    }
+    int before = 0, cut_before = 0;
+    for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
+        if (i0 > 0 || b.n_seqs > 64) look(i0 + lane);
+        const int runs = (span + L - 1) / L, pieces = tiles * runs;
+        const int upto = before + lvr_wave_inclusive_sum(pieces), cut = runs > 1 ? pieces : 0;
+        const int cut_upto = cut_before + lvr_wave_inclusive_sum(cut);
+        const uint64_t past = __ballot(upto > x);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            const int seq_runs = __builtin_amdgcn_readlane(runs, at);
+            const int k = x - __builtin_amdgcn_readlane(upto - pieces, at);   // which of the sequence's pieces
+            const int tile = __builtin_amdgcn_readlane(tiles, at) - 1 - k / seq_runs;
+            t.slot = __builtin_amdgcn_readlane(cut_upto - cut, at) + k;
+            t.split = k % seq_runs;
+            t.seq = i0 + at;
+            int s0, s1, n;
+            sequence(b, t.seq, s0, s1, n);
+            t.first_token = s0;
+            t.rows = (s1 - s0) * G;
+            t.row0 = tile * TM;
+            t.pos0 = n - (s1 - s0);
+            const int last_row = (t.row0 + TM < t.rows ? t.row0 + TM : t.rows) - 1;
+            t.hi = t.pos0 + last_row / G + 1;
+            if (t.hi > b.table_width << b.page_shift) t.hi = b.table_width << b.page_shift;
+            t.lo = window ? t.pos0 + t.row0 / G - window + 1 : 0;
+            if (t.lo < 0) t.lo = 0;
+            const int from = t.lo & ~63;
+            t.splits = 1;
+            if (seq_runs > 1 && t.hi > from) {
+                t.splits = (t.hi - from - 1) / L + 1;
+                if (t.splits > seq_runs) t.splits = seq_runs;
+            }
+            if (t.split >= t.splits) return false;   // a run past what this tile sees
+            t.begin = from + t.split * L;
+            t.end = t.split + 1 < t.splits ? t.begin + L : t.hi;
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+        cut_before = __builtin_amdgcn_readlane(cut_upto, 63);
+    }
+    return false;
+}
+
+// Partial results of pieces: per slot and KV head TM rows of 128 sums, then TM pairs of maximum and weight.
+template <int TM>
+__device__ __forceinline__ float *partial(float *part, int slot, int n_kv, int kvh) {
+    return part + ((int64_t)slot * n_kv + kvh) * (TM * (LVR_D + 2));
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
@@ -196,16 +269,19 @@ struct Rows16<lvr_f32_t> {
     static __device__ __forceinline__ int coordinate(int r, int u) { return u < 4 ? 4 * r + u : 64 + 4 * r + u - 4; }
 };
 
+constexpr int ROWS16_MIN_RUN = 256, ROWS128_MIN_RUN = 256;
+
 template <typename KT>
 __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
     typedef Rows16<KT> R;
     __shared__ float s_m[4][16], s_l[4][16];
     __shared__ float s_o[4][16][LVR_D + 4];
+    __shared__ unsigned s_arrived;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = lvr_lane(), i = lane & 15, b = lane >> 4;
     const int kvh = blockIdx.x % a.n_kv;
     Tile t;
-    if (!find_tile<16>(bt, a.G, a.window, blockIdx.x / a.n_kv, t)) return;   // the whole workgroup
+    if (!find_work<16, ROWS16_MIN_RUN>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;   // the whole workgroup
 
     const int row = t.row0 + i;                      // this lane's query row (column i of the score tiles)
     const int token = row / a.G, head = kvh * a.G + row - token * a.G;
@@ -223,7 +299,7 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
 #pragma unroll
     for (int u = 0; u < 8; ++u) o[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    for (int k0 = (t.lo & ~31) + wave * 32; k0 < t.hi; k0 += 128) {   // uniform over the wave
+    for (int k0 = t.begin + wave * 32; k0 < t.end; k0 += 128) {   // uniform over the wave
         typename R::K k;
         typename R::V v;
         const char *vp[2];
@@ -313,8 +389,8 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
             *reinterpret_cast<float4 *>(&s_o[wave][i][R::coordinate(4 * b + c, u)]) = make_float4(o[u][c], o[u + 1][c], o[u + 2][c], o[u + 3][c]);
     __syncthreads();
     const int r = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 8;
-    if (t.row0 + r >= t.rows) return;
-    const float M = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+    const bool writes = t.row0 + r < t.rows;
+    float M = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
     float sum = 0.f, x[8];
     lvr_zero8(x);
 #pragma unroll
@@ -325,6 +401,60 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] += scale * s_o[w][r][c0 + e];
     }
+    if (t.splits > 1) {
+        // The last workgroup of the tile to end merges all of them.  Partials cross from one die to another: they are stored and read
+        // with accesses of device scope, and a workgroup waits for its own stores before it takes the ticket, which
+        // wraps at the tile's runs and so is zero again afterwards.
+        typedef unsigned long long u64;
+        float *mine = partial<16>(a.part, t.slot, a.n_kv, kvh);
+        if (writes) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2)
+                __hip_atomic_store(reinterpret_cast<u64 *>(mine + r * LVR_D + c0 + e), __builtin_bit_cast(u64, make_float2(x[e], x[e + 1])),
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (c0 == 0)
+                __hip_atomic_store(reinterpret_cast<u64 *>(mine + 16 * LVR_D + r * 2), __builtin_bit_cast(u64, make_float2(M, sum)), __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        const int slot0 = t.slot - t.split;
+        if (threadIdx.x == 0) s_arrived = atomicInc(a.ticket + ((int64_t)slot0 * a.n_kv + kvh) * LVR_CNT_STRIDE, (unsigned)t.splits - 1u);
+        __syncthreads();
+        if (s_arrived != (unsigned)t.splits - 1u || !writes) return;
+        auto load = [](const float *p) {
+            return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const u64 *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        };
+        const float *first_part = partial<16>(a.part, slot0, a.n_kv, kvh);
+        const int64_t step = (int64_t)a.n_kv * (16 * (LVR_D + 2));
+        M = -INFINITY;
+        sum = 0.f;
+        lvr_zero8(x);
+        for (int p0 = 0; p0 < t.splits; p0 += 4) {   // four partials in flight
+            float2 ml[4], v[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int p = p0 + i < t.splits ? p0 + i : t.splits - 1;
+                ml[i] = load(first_part + p * step + 16 * LVR_D + r * 2);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[i][e] = load(first_part + p * step + r * LVR_D + c0 + 2 * e);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (p0 + i >= t.splits || ml[i].x == -INFINITY) continue;   // nothing seen in that run
+                const float raised = fmaxf(M, ml[i].x);
+                const float old = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - raised), scale = __builtin_amdgcn_exp2f(ml[i].x - raised);
+                M = raised;
+                sum = sum * old + scale * ml[i].y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[2 * e] = x[2 * e] * old + scale * v[i][e].x;
+                    x[2 * e + 1] = x[2 * e + 1] * old + scale * v[i][e].y;
+                }
+            }
+        }
+    }
+    if (!writes) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;   // nothing seen: zeros
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= inv;
@@ -472,7 +602,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
     const int lane = lvr_lane(), n = lane & 31, h = lane >> 5;
     const int kvh = blockIdx.x % a.n_kv;
     Tile t;
-    if (!find_tile<128>(bt, a.G, a.window, blockIdx.x / a.n_kv, t)) return;   // the whole workgroup
+    if (!find_work<128, ROWS128_MIN_RUN>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;   // the whole workgroup
 
     const int row0 = t.row0 + wave * 32, row = row0 + n;
     const int token = row / a.G, head = kvh * a.G + row - token * a.G;
@@ -534,16 +664,16 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
         if (lane == 0) s_flags[buf][wave] = flags;
     };
 
-    int k0 = t.lo & ~(TK - 1), buf = 0;
+    int k0 = t.begin, buf = 0;
     bool next_partly = false;
-    if (k0 < t.hi) {
+    if (k0 < t.end) {
         next_partly = load(k0, page_of(k0));
         store(0, k0, next_partly);
     }
     int page = page_of(k0 + TK);
     __syncthreads();
-    for (; k0 < t.hi; k0 += TK, buf ^= 1) {   // uniform over the workgroup
-        const bool more = k0 + TK < t.hi;
+    for (; k0 < t.end; k0 += TK, buf ^= 1) {   // uniform over the workgroup
+        const bool more = k0 + TK < t.end;
         if (more) {
             next_partly = load(k0 + TK, page);
             page = page_of(k0 + 2 * TK);
@@ -612,6 +742,17 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
     }
     l += __shfl_xor(l, 32, 64);
     if (!has_row) return;
+    if (t.splits > 1) {
+        float *mine = partial<128>(a.part, t.slot, a.n_kv, kvh) + (wave * 32 + n) * LVR_D;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float4 v = R::ELT == 2 ? make_float4(o[i >> 2][(i & 3) * 4], o[i >> 2][(i & 3) * 4 + 1], o[i >> 2][(i & 3) * 4 + 2], o[i >> 2][(i & 3) * 4 + 3])
+                                         : make_float4(o[0][i], o[1][i], o[2][i], o[3][i]);
+            *reinterpret_cast<float4 *>(mine + (R::ELT == 2 ? R::coordinate(h, i >> 2, (i & 3) * 4) : R::coordinate(h, 0, i))) = v;
+        }
+        if (h == 0) *reinterpret_cast<float2 *>(partial<128>(a.part, t.slot, a.n_kv, kvh) + 128 * LVR_D + (wave * 32 + n) * 2) = make_float2(m, l);
+        return;
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;   // nothing seen: zeros
     char *dst = a.out + ((int64_t)(t.first_token + token) * a.n_kv * a.G + head) * LVR_D * R::ELT;
     if constexpr (R::ELT == 2) {
@@ -628,7 +769,52 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
     }
 }
 
+// Merges the runs of cut 128-row tiles: a workgroup takes 16 rows (blockIdx.y) of a piece's tile, 16 lanes to a row, where the
+// piece is the tile's first run.
+template <typename KT>
+__global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, lvr_paged_batch bt) {
+    constexpr int ELT = sizeof(KT) == 4 ? 4 : 2;
+    const int kvh = blockIdx.x % a.n_kv;
+    Tile t;
+    if (!find_work<128, ROWS128_MIN_RUN>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;
+    const int r = blockIdx.y * 16 + (threadIdx.x >> 4), c0 = (threadIdx.x & 15) * 8;
+    if (t.splits == 1 || t.split != 0 || t.row0 + r >= t.rows) return;
+    const float *first_part = partial<128>(a.part, t.slot, a.n_kv, kvh);
+    const int64_t step = (int64_t)a.n_kv * (128 * (LVR_D + 2));
+    float M = -INFINITY, sum = 0.f, x[8];
+    lvr_zero8(x);
+#pragma unroll 4
+    for (int p = 0; p < t.splits; ++p) {
+        const float2 ml = *reinterpret_cast<const float2 *>(first_part + p * step + 128 * LVR_D + r * 2);
+        const float4 v0 = *reinterpret_cast<const float4 *>(first_part + p * step + r * LVR_D + c0);
+        const float4 v1 = *reinterpret_cast<const float4 *>(first_part + p * step + r * LVR_D + c0 + 4);
+        const float raised = fmaxf(M, ml.x);
+        const float old = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - raised);
+        const float scale = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - raised);   // nothing seen in that run
+        M = raised;
+        sum = sum * old + scale * ml.y;
+        x[0] = x[0] * old + scale * v0.x; x[1] = x[1] * old + scale * v0.y; x[2] = x[2] * old + scale * v0.z; x[3] = x[3] * old + scale * v0.w;
+        x[4] = x[4] * old + scale * v1.x; x[5] = x[5] * old + scale * v1.y; x[6] = x[6] * old + scale * v1.z; x[7] = x[7] * old + scale * v1.w;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int token = (t.row0 + r) / a.G, head = kvh * a.G + t.row0 + r - token * a.G;
+    char *dst = a.out + (((int64_t)(t.first_token + token) * a.n_kv * a.G + head) * LVR_D + c0) * ELT;
+    if constexpr (ELT == 2) {
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv), pack_bf16(x[4] * inv, x[5] * inv),
+                                                     pack_bf16(x[6] * inv, x[7] * inv));
+    } else {
+        *reinterpret_cast<float4 *>(dst) = make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+        *reinterpret_cast<float4 *>(dst + 16) = make_float4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
+    }
+}
+
 }  // namespace
+
+size_t lvr_paged_partial_bytes() {
+    const size_t narrow = (size_t)2 * ROWS16_PIECES * 16 * (LVR_D + 2), wide = (size_t)2 * ROWS128_PIECES * 128 * (LVR_D + 2);
+    return (narrow > wide ? narrow : wide) * sizeof(float);
+}
+size_t lvr_paged_ticket_bytes() { return (size_t)2 * ROWS16_PIECES * LVR_CNT_STRIDE * sizeof(uint32_t); }
 
 hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
                                       int64_t q_stride_bytes, int32_t window, void *out, hipStream_t st) {
@@ -642,12 +828,22 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.G = pc->cfg.n_q_heads / pc->cfg.n_kv_heads;
     a.window = window;
     a.unit = pc->sigma * LOG2E;
+    a.part = pc->part;
+    a.ticket = pc->ticket;
     const bool wide = (int64_t)b.n_tokens * a.G > 32 * (int64_t)b.n_seqs;
     const int64_t tiles = (int64_t)b.n_tokens * a.G / (wide ? 128 : 16) + b.n_seqs;
-    const dim3 grid((unsigned)(tiles * a.n_kv));
+    const int pieces = wide ? ROWS128_PIECES : ROWS16_PIECES;
+    a.target = pieces / a.n_kv;   // n_kv is at most 256
+    if (wide && (int64_t)b.n_tokens * a.G / 128 * a.n_kv >= 2 * ROWS128_PIECES) a.target = 0;   // enough tiles to fill the device without cuts
+    const dim3 grid((unsigned)((tiles + a.target) * a.n_kv));
     if (wide) {
         if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_rows128_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
         else hipLaunchKernelGGL(paged_attention_rows128_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
+        if (a.target > 0) {
+            const dim3 merge(grid.x, 8);
+            if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_bf16_t>, merge, dim3(256), 0, st, a, b);
+            else hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_f32_t>, merge, dim3(256), 0, st, a, b);
+        }
     } else {
         if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
         else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
