@@ -418,7 +418,7 @@ typedef struct lvr_paged_config {
     int32_t rot_axes;     /* axes a position has, 1 .. 4 (a text's has one; time, row, column: three)  */
     int32_t rot_pairs;    /* lvr_rot_pairs                                                           */
     int64_t n_pages;      /* pages in each pool, 1 .. 2^30                                           */
-    int64_t page_strides[3]; /* element strides of the pools: page, kv head, token; head_dim is contiguous */
+    int64_t page_strides[3]; /* element strides of the pools: page, kv head, token (at most 2^24); head_dim is contiguous */
     float scale;          /* sigma; 0 means 1/sqrt(head_dim)                                         */
 } lvr_paged_config;
 

@@ -194,6 +194,7 @@ int check_config(const lvr_paged_config *c) {
     if (c->n_q_heads > 1024 || c->n_kv_heads > 256) return LVR_E_UNSUPPORTED;
     if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1))) return LVR_E_UNSUPPORTED;
     if (c->n_pages > (int64_t)1 << 30) return LVR_E_UNSUPPORTED;
+    if (c->page_strides[2] > (int64_t)1 << 24) return LVR_E_UNSUPPORTED;   // 16 rows of a page are told apart by 32-bit offsets
     return LVR_OK;
 }
 

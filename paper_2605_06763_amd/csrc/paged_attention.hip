@@ -148,6 +148,44 @@ __device__ __forceinline__ float *partial(float *part, int slot, int n_kv, int k
     return part + ((int64_t)slot * n_kv + kvh) * (TM * (LVR_D + 2));
 }
 
+// One query row over the keys k0 .. k0 + run - 1, then `step` further on, and so on before `end`, on the vector units: two coordinates a lane.
+// For rows whose neighbours in a tile do not see a value that is infinite or no number: in a matrix product it would reach them
+// with weight zero.
+struct RowSum {
+    float m, l, o0, o1;
+};
+template <int ELT>
+__device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, int kvh, int row, int k0, int run, int step) {
+    const int lane = lvr_lane(), token = row / a.G, head = kvh * a.G + row - token * a.G;
+    const int last = t.pos0 + token, first = a.window && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
+    auto pair = [&](const char *r) {
+        if constexpr (ELT == 2) {
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(r + lane * 4);
+            return make_float2(lvr_bf16_lo(w), lvr_bf16_hi(w));
+        } else {
+            return *reinterpret_cast<const float2 *>(r + lane * 8);
+        }
+    };
+    const float2 q = pair(a.q + (int64_t)(t.first_token + token) * a.q_stride + (int64_t)head * LVR_D * ELT);
+    RowSum s = {-INFINITY, 0.f, 0.f, 0.f};
+    for (; k0 < t.end; k0 += step)
+        for (int key = k0; key < k0 + run && key < t.end; ++key) {
+            const int page = key < first || key > last ? -1 : lvr_page_of(bt, t.seq, key);
+            if (page < 0) continue;
+            const int64_t at = lvr_row_at(bt, page, kvh, key);
+            const float2 k = pair(a.k_pages + at), v = pair(a.v_pages + at);
+            const float x = wave_sum(q.x * k.x + q.y * k.y) * a.unit;
+            const float raised = fmaxf(s.m, x);
+            const float old = s.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.m - raised);
+            const float w = __builtin_amdgcn_exp2f(x - (raised == -INFINITY ? 0.f : raised));
+            s.m = raised;
+            s.l = s.l * old + w;
+            s.o0 = s.o0 * old + w * v.x;
+            s.o1 = s.o1 * old + w * v.y;
+        }
+    return s;
+}
+
 // ---------------------------------------------------------------------------------------------------------------------------
 // 16 rows to a tile.  A workgroup of four waves; a wave takes 32 keys at a time straight into registers.
 //
@@ -191,7 +229,6 @@ struct Rows16<lvr_bf16_t> {
             s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[kk]), q[kk], s, 0, 0, 0);
         return s;
     }
-    static __device__ __forceinline__ float element(const char *row, int c) { return lvr_bf16_lo(*reinterpret_cast<const uint16_t *>(row + c * 2)); }
     // o[u] += V^T P^T over the 32 keys; l += the weights as rounded, which is what the second product sees
     static __device__ __forceinline__ void add(const V &v, const float (&p)[2][4], f32x4 (&o)[8], float &l) {
         uint32_t pw[4] = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
@@ -251,7 +288,6 @@ struct Rows16<lvr_f32_t> {
         }
         return s;
     }
-    static __device__ __forceinline__ float element(const char *row, int c) { return *reinterpret_cast<const float *>(row + c * 4); }
     static __device__ __forceinline__ float value(const Raw &v, int u) {
         const float4 &h = u < 4 ? v.a : v.b;
         return (u & 3) == 0 ? h.x : ((u & 3) == 1 ? h.y : ((u & 3) == 2 ? h.z : h.w));
@@ -294,6 +330,7 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
     const int last_pos = t.pos0 + ((t.row0 + 15 < t.rows ? t.row0 + 15 : t.rows - 1) / a.G);
     const int row_begin = a.window && last_pos - a.window + 1 > 0 ? last_pos - a.window + 1 : 0;
 
+    bool redo = false;
     float m = -INFINITY, l = 0.f;
     f32x4 o[8];
 #pragma unroll
@@ -302,7 +339,6 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
     for (int k0 = t.begin + wave * 32; k0 < t.end; k0 += 128) {   // uniform over the wave
         typename R::K k;
         typename R::V v;
-        const char *vp[2];
         bool none[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {   // 16 keys: one page
@@ -310,11 +346,10 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
             const int page = kt < t.hi ? __builtin_amdgcn_readfirstlane(lvr_page_of(bt, t.seq, kt)) : -1;
             none[h] = page < 0;
             const int64_t at = lvr_row_at(bt, none[h] ? 0 : page, kvh, none[h] ? 0 : kt);   // no page: some memory of the pool
-            const char *kp = a.k_pages + at;
-            vp[h] = a.v_pages + at;
+            const char *kp = a.k_pages + at, *vp = a.v_pages + at;
             R::load_k(kp + i * bt.row_stride, b, k[h]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) R::load_v(vp[h] + (4 * b + j) * bt.row_stride, i, v[h][j]);
+            for (int j = 0; j < 4; ++j) R::load_v(vp + (4 * b + j) * bt.row_stride, i, v[h][j]);
         }
         const bool partly = k0 < row_begin || k0 + 32 > row_end || none[0] || none[1];
         float p[2][4];
@@ -352,32 +387,22 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
         const float base = m == -INFINITY ? 0.f : m;   // nothing seen so far: every weight below is 2^-inf
 #pragma unroll
         for (int c = 0; c < 8; ++c) p[c >> 2][c & 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[c >> 2][c & 3], a.unit, -base));
-        if (__any(poison)) {
-            // rare: key by key on the vector units, so that a row that does not see a key does not meet its value
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    l += p[h][j];
-                    for (int b2 = 0; b2 < 4; ++b2) {
-                        const int key = k0 + h * 16 + 4 * b2 + j;
-                        const float w = __shfl(p[h][j], i + 16 * b2, 64);
-                        if (none[h] || key < first || key > last) continue;
-                        const char *vr = vp[h] + (4 * b2 + j) * bt.row_stride;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) o[u][c] += w * R::element(vr, R::coordinate(4 * b + c, u));
-                    }
-                }
-        } else {
-            R::add(v, p, o, l);
-        }
+        redo |= poison;
+        R::add(v, p, o, l);
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
 
     // the four waves' (m, l, o) become the rows' outputs
+    if (__any(redo)) {
+        for (int r = 0; r < 16 && t.row0 + r < t.rows; ++r) {
+            const RowSum s = one_row<R::ELT>(a, bt, t, kvh, t.row0 + r, t.begin + wave * 32, 32, 128);
+            s_m[wave][r] = s.m;
+            s_l[wave][r] = s.l;
+            s_o[wave][r][2 * lane] = s.o0;
+            s_o[wave][r][2 * lane + 1] = s.o1;
+        }
+    } else {
     if (b == 0) {
         s_m[wave][i] = m;
         s_l[wave][i] = l;
@@ -387,6 +412,7 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
 #pragma unroll
         for (int u = 0; u < 8; u += 4)
             *reinterpret_cast<float4 *>(&s_o[wave][i][R::coordinate(4 * b + c, u)]) = make_float4(o[u][c], o[u + 1][c], o[u + 2][c], o[u + 3][c]);
+    }
     __syncthreads();
     const int r = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 8;
     const bool writes = t.row0 + r < t.rows;
@@ -470,7 +496,7 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
 
 // ---------------------------------------------------------------------------------------------------------------------------
 // 128 rows to a tile, 32 to each of four waves.  K and V tiles pass through LDS, two of each: while one is worked on the next is on
-// its way through registers.
+// its way, past the registers.
 //
 // Matrix operand lanes: n = lane & 31 (query row), h = lane >> 5.  Score tile: 32 keys, result row 8 i + 4 h + j is register 4 i + j.
 // bf16 (tiles of 64 keys): registers 8 t .. 8 t + 7 of a score tile are at once the second product's operand for 16 keys, of which lanes
@@ -541,9 +567,6 @@ struct Rows128<lvr_bf16_t> {
             }
     }
     static __device__ __forceinline__ bool odd(const uint4 &v) { return Rows16<lvr_bf16_t>::odd_v(v); }
-    static __device__ __forceinline__ float element(const char *v, int key, int c) {
-        return lvr_bf16_lo(*reinterpret_cast<const uint16_t *>(v + key * ROWB + v_piece(key, c >> 3) * 16 + (c & 7) * 2));
-    }
 };
 
 template <>
@@ -588,16 +611,19 @@ struct Rows128<lvr_f32_t> {
         return (v.x & 0x7f800000u) == 0x7f800000u || (v.y & 0x7f800000u) == 0x7f800000u || (v.z & 0x7f800000u) == 0x7f800000u ||
                (v.w & 0x7f800000u) == 0x7f800000u;
     }
-    static __device__ __forceinline__ float element(const char *v, int key, int c) { return *reinterpret_cast<const float *>(v + key * ROWB + c * 4); }
 };
+
+// 16 bytes per lane from global memory into LDS, the wave's 1 KiB in a row from `to` on.  vmcnt counts it.
+__device__ __forceinline__ void load_to_lds(const char *from, uint32_t offset, char *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(from + offset),
+                                     (__attribute__((address_space(3))) uint32_t *)to, 16, 0, 0);
+}
 
 template <typename KT>
 __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArgs a, lvr_paged_batch bt) {
     typedef Rows128<KT> R;
     constexpr int TK = R::TK, LPR = R::PIECES, RPI = 64 / LPR;   // lanes to a row, rows to a load of the wave
-    enum { NONE = 1, ODD = 2 };
     __shared__ __align__(16) char s_k[2][TK * R::ROWB], s_v[2][TK * R::ROWB];
-    __shared__ __align__(16) int s_flags[2][4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = lvr_lane(), n = lane & 31, h = lane >> 5;
     const int kvh = blockIdx.x % a.n_kv;
@@ -607,92 +633,84 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
     const int row0 = t.row0 + wave * 32, row = row0 + n;
     const int token = row / a.G, head = kvh * a.G + row - token * a.G;
     const bool has_row = row < t.rows;
-    const bool has_rows = row0 < t.rows;
     typename R::Q q;
     R::load_q(has_row ? a.q + (int64_t)(t.first_token + token) * a.q_stride + (int64_t)head * LVR_D * R::ELT : nullptr, h, q);
     const int last = t.pos0 + token;                 // keys this row sees: first .. last
     const int first = a.window && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
-    // the wave's rows: some of them see wlo .. whi - 1, all of them all_lo .. all_hi - 1; and the workgroup's
-    const int wlast = (row0 + 31 < t.rows ? row0 + 31 : t.rows - 1) / a.G, wfirst = row0 / a.G;
-    const int whi = has_rows ? t.pos0 + wlast + 1 : 0, wlo = a.window ? t.pos0 + wfirst - a.window + 1 : 0;
-    const int all_hi = t.pos0 + wfirst + 1, all_lo = a.window ? t.pos0 + wlast - a.window + 1 : 0;
-    const int tile_last = (t.row0 + 127 < t.rows ? t.row0 + 127 : t.rows - 1) / a.G;
-    const int tile_all_hi = t.pos0 + t.row0 / a.G + 1, tile_all_lo = a.window ? t.pos0 + tile_last - a.window + 1 : 0;
+    // some of the wave's rows see wlo .. whi - 1, all of them all_lo .. all_hi - 1
+    const int wfirst = t.pos0 + row0 / a.G, wlast = t.pos0 + (row0 + 31 < t.rows ? row0 + 31 : t.rows - 1) / a.G;
+    const int whi = row0 < t.rows ? wlast + 1 : 0, wlo = a.window ? wfirst - a.window + 1 : 0;
+    const int all_hi = wfirst + 1, all_lo = a.window ? wlast - a.window + 1 : 0;
 
+    bool redo = false;   // a value that some rows must not meet
     float m = -INFINITY, l = 0.f;
     f32x16 o[4];
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) o[dt] = f32x16{0.f};
 
-    // staging: this wave's rows of a tile lie in one page
-    uint4 kr[4], vr[4];
-    int flags = 0;
-    const int srow = wave * 4 * RPI + lane / LPR, piece = lane % LPR;
-    const int group = wave * 4 * RPI & ~15;
-    auto page_of = [&](int k0) { return k0 + group < t.hi ? __builtin_amdgcn_readfirstlane(lvr_page_of(bt, t.seq, k0 + group)) : -1; };
-    auto load = [&](int k0, int page) {
-        const int64_t at = page < 0 ? kvh * bt.head_stride : lvr_row_at(bt, page, kvh, k0 + group);   // no page: some memory of the pool
-        const char *kp = a.k_pages + at, *vp = a.v_pages + at;
-        const bool partly = k0 < tile_all_lo || k0 + TK > tile_all_hi;
-        flags = page < 0 ? NONE : 0;
+    // A wave brings four loads' worth of rows of K and of V, which lie in one page; each lane's place within the page's 16 rows
+    // stays the same.  The lanes look up the pages of all groups of 16 keys of a tile at once, a tile ahead of the rows.
+    const int srow = wave * 4 * RPI + lane / LPR, piece = lane % LPR, group = wave * 4 * RPI & ~15;
+    uint32_t k_off[4], v_off[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = srow + i * RPI;
-            kr[i] = *reinterpret_cast<const uint4 *>(kp + (R::key_of_k_row(r) - group) * bt.row_stride + R::k_piece(r, piece) * 16);
-            vr[i] = *reinterpret_cast<const uint4 *>(vp + (r - group) * bt.row_stride + R::v_piece(r, piece) * 16);
-        }
-        return partly;
+    for (int i = 0; i < 4; ++i) {
+        const int r = srow + i * RPI;
+        k_off[i] = (uint32_t)(R::key_of_k_row(r) - group) * (uint32_t)bt.row_stride + R::k_piece(r, piece) * 16;
+        v_off[i] = (uint32_t)(r - group) * (uint32_t)bt.row_stride + R::v_piece(r, piece) * 16;
+    }
+    auto pages_of = [&](int k0) {
+        const int key = k0 + 16 * (lane % (TK / 16));
+        return key < t.hi ? lvr_page_of(bt, t.seq, key) : -1;
     };
-    auto store = [&](int buf, int k0, bool partly) {
-        if (partly || flags) {
-            // a row of V that no query row sees is memory nobody has written; one that some see meets the others with weight zero,
-            // which an infinity or a NaN would survive
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = k0 + srow + i * RPI;
-                if (flags || key < t.lo || key >= t.hi) vr[i] = make_uint4(0, 0, 0, 0);
-                odd |= R::odd(vr[i]);
-            }
-            if (__any(odd)) flags |= ODD;
-        }
+    auto load = [&](int k0, int pages, int buf) {
+        const int page = __builtin_amdgcn_readlane(pages, group / 16);
+        const int64_t at = page < 0 ? kvh * bt.head_stride : lvr_row_at(bt, page, kvh, k0 + group);   // no page: some memory of the pool
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<uint4 *>(s_k[buf] + (srow + i * RPI) * R::ROWB + piece * 16) = kr[i];
-            *reinterpret_cast<uint4 *>(s_v[buf] + (srow + i * RPI) * R::ROWB + piece * 16) = vr[i];
+            load_to_lds(a.k_pages + at, k_off[i], s_k[buf] + (wave * 4 + i) * 1024);
+            load_to_lds(a.v_pages + at, v_off[i], s_v[buf] + (wave * 4 + i) * 1024);
         }
-        if (lane == 0) s_flags[buf][wave] = flags;
+        return (uint32_t)__ballot(pages < 0) & ((1u << TK / 16) - 1u);   // groups without a page
+    };
+    auto arrived = [] {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
 
-    int k0 = t.begin, buf = 0;
-    bool next_partly = false;
-    if (k0 < t.end) {
-        next_partly = load(k0, page_of(k0));
-        store(0, k0, next_partly);
-    }
-    int page = page_of(k0 + TK);
-    __syncthreads();
-    for (; k0 < t.end; k0 += TK, buf ^= 1) {   // uniform over the workgroup
-        const bool more = k0 + TK < t.end;
-        if (more) {
-            next_partly = load(k0 + TK, page);
-            page = page_of(k0 + 2 * TK);
+    int buf = 0;
+    uint32_t none = 0, next_none = 0;
+    if (t.begin < t.end) none = load(t.begin, pages_of(t.begin), 0);
+    int pages = pages_of(t.begin + TK);
+    arrived();
+    for (int k0 = t.begin; k0 < t.end; k0 += TK, buf ^= 1, none = next_none) {   // uniform over the workgroup
+        if (k0 + TK < t.end) {
+            next_none = load(k0 + TK, pages, buf ^ 1);
+            pages = pages_of(k0 + 2 * TK);
+        }
+        if (k0 < t.lo || k0 + TK > t.hi || none != 0) {   // a row of V that no query row sees may be memory nobody has written
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = srow + i * RPI;
+                if (k0 + key < t.lo || k0 + key >= t.hi || (none >> (key >> 4) & 1))
+                    *reinterpret_cast<uint4 *>(s_v[buf] + key * R::ROWB + piece * 16) = make_uint4(0, 0, 0, 0);
+            }
+            arrived();
         }
         if (k0 < whi && k0 + TK > wlo) {
-            const int4 f4 = *reinterpret_cast<const int4 *>(s_flags[buf]);
-            const int f = __builtin_amdgcn_readfirstlane(f4.x | f4.y | f4.z | f4.w);
             f32x16 p[R::NT];
             R::scores(s_k[buf], q, n, h, p);
-            const bool partly = k0 < all_lo || k0 + TK > all_hi || (f & NONE);
+            const bool partly = k0 < all_lo || k0 + TK > all_hi || none != 0;
             if (partly) {
+                asm volatile("");   // a branch, not 32 selects in every tile
+#pragma unroll 1
+                for (int c = 0; c < TK * R::ROWB / 1024; ++c) redo |= R::odd(*reinterpret_cast<const uint4 *>(s_v[buf] + c * 1024 + lane * 16));
 #pragma unroll
                 for (int kt = 0; kt < R::NT; ++kt)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const int key = k0 + R::key_of(h, kt, r);
-                        bool hidden = key < first || key > last;
-                        if (f & NONE) hidden |= (s_flags[buf][(key - k0) / (TK / 4)] & NONE) != 0;
-                        if (hidden) p[kt][r] = -INFINITY;
+                        const int key = R::key_of(h, kt, r);
+                        if (k0 + key < first || k0 + key > last || (none >> (key >> 4) & 1)) p[kt][r] = -INFINITY;
                     }
             }
             float top = p[0][0];
@@ -714,33 +732,27 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
             for (int kt = 0; kt < R::NT; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) p[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[kt][r], a.unit, -base));
-            if (partly && (f & ODD)) {
-                // rare: key by key on the vector units, so that a row that does not see a key does not meet its value
-#pragma unroll 1
-                for (int c = 0; c < TK; ++c) {
-                    const int kt = c >> 5, r = (c & 31) >> 1, h2 = c & 1;
-                    float w = 0.f;
-#pragma unroll
-                    for (int kk = 0; kk < R::NT; ++kk)
-#pragma unroll
-                        for (int rr = 0; rr < 16; ++rr) w = kk == kt && rr == r ? p[kk][rr] : w;
-                    if (h == h2) l += w;
-                    w = __shfl(w, n + 32 * h2, 64);
-                    const int key = R::key_of(h2, kt, r);
-                    if (k0 + key < first || k0 + key > last || (s_flags[buf][key / (TK / 4)] & NONE)) continue;
-#pragma unroll
-                    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[dt][e] += w * R::element(s_v[buf], key, R::coordinate(h, dt, e));
-                }
-            } else {
-                R::add(s_v[buf], p, lane, o, l);
-            }
+            R::add(s_v[buf], p, lane, o, l);
         }
-        if (more) store(buf ^ 1, k0 + TK, next_partly);
-        __syncthreads();
+        arrived();
     }
     l += __shfl_xor(l, 32, 64);
+    if (__any(redo)) {
+        for (int r = row0; r < row0 + 32 && r < t.rows; ++r) {
+            RowSum s = one_row<R::ELT>(a, bt, t, kvh, r, t.begin, 1 << 30, 1 << 30);
+            if (t.splits > 1) {
+                float *mine = partial<128>(a.part, t.slot, a.n_kv, kvh);
+                *reinterpret_cast<float2 *>(mine + (r - t.row0) * LVR_D + 2 * lane) = make_float2(s.o0, s.o1);
+                *reinterpret_cast<float2 *>(mine + 128 * LVR_D + (r - t.row0) * 2) = make_float2(s.m, s.l);
+                continue;
+            }
+            const float inv = s.l == 0.f ? 0.f : 1.f / s.l;
+            char *dst = a.out + ((int64_t)(t.first_token + r / a.G) * a.n_kv * a.G + kvh * a.G + r % a.G) * LVR_D * R::ELT;
+            if constexpr (R::ELT == 2) *reinterpret_cast<uint32_t *>(dst + lane * 4) = pack_bf16(s.o0 * inv, s.o1 * inv);
+            else *reinterpret_cast<float2 *>(dst + lane * 8) = make_float2(s.o0 * inv, s.o1 * inv);
+        }
+        return;
+    }
     if (!has_row) return;
     if (t.splits > 1) {
         float *mine = partial<128>(a.part, t.slot, a.n_kv, kvh) + (wave * 32 + n) * LVR_D;

@@ -41,6 +41,7 @@ def test_config_struct_matches_header(L):
     (dict(head_dim=64, rot_dim=64), "UNSUPPORTED"), (dict(rot_dim=72), "UNSUPPORTED"), (dict(page_size=8), "UNSUPPORTED"),
     (dict(page_size=48), "UNSUPPORTED"), (dict(page_size=1 << 17), "UNSUPPORTED"), (dict(n_q_heads=2048), "UNSUPPORTED"),
     (dict(n_q_heads=512, n_kv_heads=512), "UNSUPPORTED"), (dict(n_pages=1 << 31), "UNSUPPORTED"),
+    (dict(page_strides=(8 * 16 * 128, 128, (1 << 24) + 8)), "UNSUPPORTED"),
 ])
 def test_bad_configurations_are_refused(L, bad, code):
     cfg = L.make_paged_config(**dict(OK, **bad))
