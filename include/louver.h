@@ -390,7 +390,7 @@ int lvr_length(const lvr_index *ix, int64_t *n_host, int64_t *n_indexed_host);
  *                 seq_start[b+1]-1 of the packed token arrays, perhaps none.  Tokens before
  *                 seq_start[0] and behind seq_start[n_seqs] belong to no sequence: nothing is stored
  *                 for them and their rows of the outputs stay as they were.
- *   seq_len_dev   [n_seqs] int32: keys the sequence holds, its new ones among them.  New token i of m
+ *   seq_len_dev   [n_seqs] int32, at most 2^30: keys the sequence holds, its new ones among them.  New token i of m
  *                 therefore sits at position seq_len - m + i.  A token at a negative position is
  *                 not stored and attends nothing.
  *   table_dev     [n_seqs][table_width] int32: the page of positions p * page_size ..

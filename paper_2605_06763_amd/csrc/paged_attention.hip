@@ -15,8 +15,11 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
-// Pieces of work a launch aims at, over all KV heads (tiles of 16 rows, of 128 rows).
-constexpr int ROWS16_PIECES = 1024, ROWS128_PIECES = 512;
+// Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.
+constexpr int ROWS16_PIECES = 2048, MIXED_PIECES = 1024;
+constexpr int MIN_RUN = 256, MAX_RUNS = 512;
+constexpr int NARROW = 32;    // rows of a sequence up to which it is taken in tiles of 16
+constexpr int FAN = 8;        // partial results of 16-row tiles merged at a time
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -40,6 +43,7 @@ struct AttnArgs {
 
 // A piece of work: a tile of TM packed rows of one sequence against a run of the keys they see.
 struct Tile {
+    int height;                // TM: 16 or 128
     int seq, row0, rows;       // first packed row within the sequence; rows of the sequence
     int first_token;           // of the sequence, in the packed arrays
     int pos0;                  // position of the sequence's first new token
@@ -62,27 +66,31 @@ __device__ __forceinline__ void sequence(const lvr_paged_batch &b, int i, int &s
     n = b.seq_len[i];
     s0 = s0 < 0 ? 0 : (s0 > b.n_tokens ? b.n_tokens : s0);
     s1 = s1 < s0 ? s0 : (s1 > b.n_tokens ? b.n_tokens : s1);
-    n = n < 0 ? 0 : n;
+    n = n < 0 ? 0 : (n > 1 << 30 ? 1 << 30 : n);
 }
 
 // Piece x of the batch, for one KV head.  The host knows neither how many tokens a sequence brings nor how many keys it holds, so
-// every workgroup works out the division for itself, each wave on its own: a sequence's tiles are cut into runs of L
-// keys, L such that the batch makes about `target` pieces of the same size (but none under MIN_RUN keys; target 0: no cuts).  There are
-// at most target + n_tokens * G / TM + n_seqs pieces, and at most 2 * target of tiles that are cut: a cut sequence
-// has at most twice as many runs as its keys are times L, and all keys of all tiles are at most target times L.
+// every workgroup works out the division for itself, each wave on its own.  MIXED: sequences of up to NARROW rows are
+// taken in tiles of 16, others in tiles of 128; else all in tiles of 16.  A sequence's tiles are cut into runs of L keys, L such that
+// the batch makes about `target` pieces of the same length (but none under MIN_RUN keys, and no more than MAX_RUNS of a tile;
+// target 0: no cuts).  There are at most `target` pieces more than tiles, and at most 2 * target pieces of tiles that are
+// cut: a cut tile has at most twice as many runs as its keys are times L, and all keys of all tiles are at most target times L.
 // The last tiles come first: in a prompt they see most keys.
-template <int TM, int MIN_RUN>
+template <bool MIXED>
 __device__ __forceinline__ bool find_work(const lvr_paged_batch &b, int G, int window, int target, int x, Tile &t) {
     const int lane = lvr_lane();
-    const int reach = window ? window + TM / G + 2 : 0;   // keys a tile can see
     int tiles = 0, span = 0;
     auto look = [&](int i) {
         tiles = span = 0;
         if (i < b.n_seqs) {
             int s0, s1, n;
             sequence(b, i, s0, s1, n);
-            tiles = ((s1 - s0) * G + TM - 1) / TM;
-            span = window && n > reach ? reach : (n > 0 ? n : 1);
+            const int rows = (s1 - s0) * G;
+            const bool wide = MIXED && rows > NARROW;
+            tiles = wide ? (rows + 127) / 128 : (rows + 15) / 16;
+            const int reach = window ? window + (wide ? 128 : 16) / G + 2 : n;   // keys a tile can see
+            span = n < reach ? n : reach;
+            if (span < 1) span = 1;
             return (float)(s1 - s0);
         }
         return 0.f;
@@ -101,14 +109,19 @@ __device__ __forceinline__ bool find_work(const lvr_paged_batch &b, int G, int w
     }
     int before = 0, cut_before = 0;
     for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
-        if (i0 > 0 || b.n_seqs > 64) look(i0 + lane);
-        const int runs = (span + L - 1) / L, pieces = tiles * runs;
+        if (b.n_seqs > 64) look(i0 + lane);
+        int run = L;
+        if (span > MAX_RUNS * (MIN_RUN / 2)) {
+            const int least = (span / MAX_RUNS + 64) & ~63;
+            if (run < least) run = least;
+        }
+        const int runs = (span + run - 1) / run, pieces = tiles * runs;
         const int upto = before + lvr_wave_inclusive_sum(pieces), cut = runs > 1 ? pieces : 0;
         const int cut_upto = cut_before + lvr_wave_inclusive_sum(cut);
         const uint64_t past = __ballot(upto > x);
         if (past) {
             const int at = __builtin_ctzll(past);
-            const int seq_runs = __builtin_amdgcn_readlane(runs, at);
+            const int seq_runs = __builtin_amdgcn_readlane(runs, at), seq_run = __builtin_amdgcn_readlane(run, at);
             const int k = x - __builtin_amdgcn_readlane(upto - pieces, at);   // which of the sequence's pieces
             const int tile = __builtin_amdgcn_readlane(tiles, at) - 1 - k / seq_runs;
             t.slot = __builtin_amdgcn_readlane(cut_upto - cut, at) + k;
@@ -118,9 +131,10 @@ __device__ __forceinline__ bool find_work(const lvr_paged_batch &b, int G, int w
             sequence(b, t.seq, s0, s1, n);
             t.first_token = s0;
             t.rows = (s1 - s0) * G;
-            t.row0 = tile * TM;
+            t.height = MIXED && t.rows > NARROW ? 128 : 16;
+            t.row0 = tile * t.height;
             t.pos0 = n - (s1 - s0);
-            const int last_row = (t.row0 + TM < t.rows ? t.row0 + TM : t.rows) - 1;
+            const int last_row = (t.row0 + t.height < t.rows ? t.row0 + t.height : t.rows) - 1;
             t.hi = t.pos0 + last_row / G + 1;
             if (t.hi > b.table_width << b.page_shift) t.hi = b.table_width << b.page_shift;
             t.lo = window ? t.pos0 + t.row0 / G - window + 1 : 0;
@@ -128,12 +142,12 @@ __device__ __forceinline__ bool find_work(const lvr_paged_batch &b, int G, int w
             const int from = t.lo & ~63;
             t.splits = 1;
             if (seq_runs > 1 && t.hi > from) {
-                t.splits = (t.hi - from - 1) / L + 1;
+                t.splits = (t.hi - from - 1) / seq_run + 1;
                 if (t.splits > seq_runs) t.splits = seq_runs;
             }
             if (t.split >= t.splits) return false;   // a run past what this tile sees
-            t.begin = from + t.split * L;
-            t.end = t.split + 1 < t.splits ? t.begin + L : t.hi;
+            t.begin = from + t.split * seq_run;
+            t.end = t.split + 1 < t.splits ? t.begin + seq_run : t.hi;
             return true;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
@@ -142,10 +156,52 @@ __device__ __forceinline__ bool find_work(const lvr_paged_batch &b, int G, int w
     return false;
 }
 
-// Partial results of pieces: per slot and KV head TM rows of 128 sums, then TM pairs of maximum and weight.
-template <int TM>
+// Partial results of pieces: per slot and KV head room for SLOT rows of 128 sums, then SLOT pairs of maximum and weight.
+template <int SLOT>
 __device__ __forceinline__ float *partial(float *part, int slot, int n_kv, int kvh) {
-    return part + ((int64_t)slot * n_kv + kvh) * (TM * (LVR_D + 2));
+    return part + ((int64_t)slot * n_kv + kvh) * (SLOT * (LVR_D + 2));
+}
+
+// Sums over several sets of keys, brought to a common maximum.
+struct Merged {
+    float m, l, o[8];
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY;
+        l = 0.f;
+        lvr_zero8(o);
+    }
+    __device__ __forceinline__ void add(float m2, float l2, const float (&v)[8]) {
+        const float raised = fmaxf(m, m2);
+        const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - raised);
+        const float scale = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - raised);   // nothing seen there: all of it is zero
+        m = raised;
+        l = l * old + scale * l2;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = o[e] * old + scale * v[e];
+    }
+};
+__device__ __forceinline__ void store_shared(float *p, float2 v) {
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_shared(const float *p) {
+    return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// Where a packed row's output lies.
+template <int ELT>
+__device__ __forceinline__ char *output_row(const AttnArgs &a, const Tile &t, int kvh, int row) {
+    const int token = row / a.G, head = kvh * a.G + row - token * a.G;
+    return a.out + ((int64_t)(t.first_token + token) * a.n_kv * a.G + head) * LVR_D * ELT;
+}
+template <int ELT>
+__device__ __forceinline__ void store_row(const AttnArgs &a, const Tile &t, int kvh, int row, int c0, const float (&y)[8]) {
+    char *dst = output_row<ELT>(a, t, kvh, row) + c0 * ELT;
+    if constexpr (ELT == 2) {
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+    } else {
+        *reinterpret_cast<float4 *>(dst) = make_float4(y[0], y[1], y[2], y[3]);
+        *reinterpret_cast<float4 *>(dst + 16) = make_float4(y[4], y[5], y[6], y[7]);
+    }
 }
 
 // One query row over the keys k0 .. k0 + run - 1, then `step` further on, and so on before `end`, on the vector units: two coordinates a lane.
@@ -305,19 +361,17 @@ struct Rows16<lvr_f32_t> {
     static __device__ __forceinline__ int coordinate(int r, int u) { return u < 4 ? 4 * r + u : 64 + 4 * r + u - 4; }
 };
 
-constexpr int ROWS16_MIN_RUN = 256, ROWS128_MIN_RUN = 256;
+struct Rows16Lds {
+    float m[4][16], l[4][16];
+    float o[4][16][LVR_D + 4];
+    unsigned arrived;
+};
 
-template <typename KT>
-__global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
+template <typename KT, int SLOT>
+__device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, Rows16Lds &lds) {
     typedef Rows16<KT> R;
-    __shared__ float s_m[4][16], s_l[4][16];
-    __shared__ float s_o[4][16][LVR_D + 4];
-    __shared__ unsigned s_arrived;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = lvr_lane(), i = lane & 15, b = lane >> 4;
-    const int kvh = blockIdx.x % a.n_kv;
-    Tile t;
-    if (!find_work<16, ROWS16_MIN_RUN>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;   // the whole workgroup
 
     const int row = t.row0 + i;                      // this lane's query row (column i of the score tiles)
     const int token = row / a.G, head = kvh * a.G + row - token * a.G;
@@ -397,101 +451,90 @@ __global__ void __launch_bounds__(256) paged_attention_rows16_kernel(AttnArgs a,
     if (__any(redo)) {
         for (int r = 0; r < 16 && t.row0 + r < t.rows; ++r) {
             const RowSum s = one_row<R::ELT>(a, bt, t, kvh, t.row0 + r, t.begin + wave * 32, 32, 128);
-            s_m[wave][r] = s.m;
-            s_l[wave][r] = s.l;
-            s_o[wave][r][2 * lane] = s.o0;
-            s_o[wave][r][2 * lane + 1] = s.o1;
+            lds.m[wave][r] = s.m;
+            lds.l[wave][r] = s.l;
+            lds.o[wave][r][2 * lane] = s.o0;
+            lds.o[wave][r][2 * lane + 1] = s.o1;
         }
     } else {
-    if (b == 0) {
-        s_m[wave][i] = m;
-        s_l[wave][i] = l;
-    }
+        if (b == 0) {
+            lds.m[wave][i] = m;
+            lds.l[wave][i] = l;
+        }
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int u = 0; u < 8; u += 4)
-            *reinterpret_cast<float4 *>(&s_o[wave][i][R::coordinate(4 * b + c, u)]) = make_float4(o[u][c], o[u + 1][c], o[u + 2][c], o[u + 3][c]);
+            for (int u = 0; u < 8; u += 4)
+                *reinterpret_cast<float4 *>(&lds.o[wave][i][R::coordinate(4 * b + c, u)]) = make_float4(o[u][c], o[u + 1][c], o[u + 2][c], o[u + 3][c]);
     }
     __syncthreads();
     const int r = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 8;
     const bool writes = t.row0 + r < t.rows;
-    float M = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
-    float sum = 0.f, x[8];
-    lvr_zero8(x);
+    Merged x;
+    x.clear();
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        const float scale = s_m[w][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][r] - M);
-        if (scale == 0.f && s_l[w][r] == 0.f) continue;
-        sum += scale * s_l[w][r];
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += scale * s_o[w][r][c0 + e];
+        for (int e = 0; e < 8; ++e) v[e] = lds.o[w][r][c0 + e];
+        x.add(lds.m[w][r], lds.l[w][r], v);
     }
     if (t.splits > 1) {
-        // The last workgroup of the tile to end merges all of them.  Partials cross from one die to another: they are stored and read
-        // with accesses of device scope, and a workgroup waits for its own stores before it takes the ticket, which
-        // wraps at the tile's runs and so is zero again afterwards.
-        typedef unsigned long long u64;
-        float *mine = partial<16>(a.part, t.slot, a.n_kv, kvh);
-        if (writes) {
+        // The last workgroup to end of every FAN of a tile's runs merges those, and the last of these merges what they made: one
+        // compute unit reads some 30 GB/s, so nobody is left with all of them.  Partials cross from one die to another: they are
+        // stored and read with accesses of device scope, and a workgroup waits for its own stores before it takes a ticket, which
+        // wraps at the number of those who take it and so is zero again afterwards.
+        const int slot0 = t.slot - t.split, fans = (t.splits + FAN - 1) / FAN, fan = t.split / FAN;
+        const int in_fan = fan + 1 < fans ? FAN : t.splits - fan * FAN;
+        float *first_part = partial<SLOT>(a.part, slot0, a.n_kv, kvh);
+        const int64_t step = (int64_t)a.n_kv * (SLOT * (LVR_D + 2));
+        auto put = [&](float *p) {
+            if (!writes) return;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2)
-                __hip_atomic_store(reinterpret_cast<u64 *>(mine + r * LVR_D + c0 + e), __builtin_bit_cast(u64, make_float2(x[e], x[e + 1])),
-                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (c0 == 0)
-                __hip_atomic_store(reinterpret_cast<u64 *>(mine + 16 * LVR_D + r * 2), __builtin_bit_cast(u64, make_float2(M, sum)), __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_AGENT);
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        const int slot0 = t.slot - t.split;
-        if (threadIdx.x == 0) s_arrived = atomicInc(a.ticket + ((int64_t)slot0 * a.n_kv + kvh) * LVR_CNT_STRIDE, (unsigned)t.splits - 1u);
-        __syncthreads();
-        if (s_arrived != (unsigned)t.splits - 1u || !writes) return;
-        auto load = [](const float *p) {
-            return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const u64 *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            for (int e = 0; e < 8; e += 2) store_shared(p + r * LVR_D + c0 + e, make_float2(x.o[e], x.o[e + 1]));
+            if (c0 == 0) store_shared(p + SLOT * LVR_D + r * 2, make_float2(x.m, x.l));
         };
-        const float *first_part = partial<16>(a.part, slot0, a.n_kv, kvh);
-        const int64_t step = (int64_t)a.n_kv * (16 * (LVR_D + 2));
-        M = -INFINITY;
-        sum = 0.f;
-        lvr_zero8(x);
-        for (int p0 = 0; p0 < t.splits; p0 += 4) {   // four partials in flight
-            float2 ml[4], v[4][4];
+        auto last_of = [&](int slot, int word, int n) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (threadIdx.x == 0) lds.arrived = atomicInc(a.ticket + ((int64_t)slot * a.n_kv + kvh) * LVR_CNT_STRIDE + word, (unsigned)n - 1u);
+            __syncthreads();
+            return lds.arrived == (unsigned)n - 1u;
+        };
+        auto merge = [&](const float *p, int64_t apart, int n) {
+            x.clear();
+            for (int p0 = 0; p0 < n; p0 += FAN) {
+                float2 ml[FAN], v[FAN][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int p = p0 + i < t.splits ? p0 + i : t.splits - 1;
-                ml[i] = load(first_part + p * step + 16 * LVR_D + r * 2);
+                for (int k = 0; k < FAN; ++k) {   // all in flight; past the last one the last once more
+                    const float *from = p + (p0 + k < n ? p0 + k : n - 1) * apart;
+                    ml[k] = load_shared(from + SLOT * LVR_D + r * 2);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[i][e] = load(first_part + p * step + r * LVR_D + c0 + 2 * e);
-            }
+                    for (int e = 0; e < 4; ++e) v[k][e] = load_shared(from + r * LVR_D + c0 + 2 * e);
+                }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (p0 + i >= t.splits || ml[i].x == -INFINITY) continue;   // nothing seen in that run
-                const float raised = fmaxf(M, ml[i].x);
-                const float old = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - raised), scale = __builtin_amdgcn_exp2f(ml[i].x - raised);
-                M = raised;
-                sum = sum * old + scale * ml[i].y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[2 * e] = x[2 * e] * old + scale * v[i][e].x;
-                    x[2 * e + 1] = x[2 * e + 1] * old + scale * v[i][e].y;
+                for (int k = 0; k < FAN; ++k) {
+                    if (p0 + k >= n) continue;
+                    const float y[8] = {v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y, v[k][2].x, v[k][2].y, v[k][3].x, v[k][3].y};
+                    x.add(ml[k].x, ml[k].y, y);
                 }
             }
+        };
+        put(first_part + t.split * step);
+        if (!last_of(slot0 + fan * FAN, 0, in_fan)) return;
+        merge(first_part + fan * FAN * step, step, in_fan);
+        if (fans > 1) {
+            put(first_part + fan * FAN * step);
+            if (!last_of(slot0, 1, fans)) return;
+            merge(first_part, FAN * step, fans);
         }
     }
     if (!writes) return;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;   // nothing seen: zeros
+    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;   // nothing seen: zeros
+    float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= inv;
-    const int otok = (t.row0 + r) / a.G, ohead = kvh * a.G + t.row0 + r - otok * a.G;
-    char *dst = a.out + (((int64_t)(t.first_token + otok) * a.n_kv * a.G + ohead) * LVR_D + c0) * R::ELT;
-    if constexpr (R::ELT == 2) {
-        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-    } else {
-        *reinterpret_cast<float4 *>(dst) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4 *>(dst + 16) = make_float4(x[4], x[5], x[6], x[7]);
-    }
+    for (int e = 0; e < 8; ++e) y[e] = x.o[e] * inv;
+    store_row<R::ELT>(a, t, kvh, t.row0 + r, c0, y);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
@@ -620,15 +663,16 @@ __device__ __forceinline__ void load_to_lds(const char *from, uint32_t offset, c
 }
 
 template <typename KT>
-__global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArgs a, lvr_paged_batch bt) {
+struct Rows128Lds {
+    __align__(16) char k[2][Rows128<KT>::TK * Rows128<KT>::ROWB], v[2][Rows128<KT>::TK * Rows128<KT>::ROWB];
+};
+
+template <typename KT>
+__device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, Rows128Lds<KT> &lds) {
     typedef Rows128<KT> R;
     constexpr int TK = R::TK, LPR = R::PIECES, RPI = 64 / LPR;   // lanes to a row, rows to a load of the wave
-    __shared__ __align__(16) char s_k[2][TK * R::ROWB], s_v[2][TK * R::ROWB];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = lvr_lane(), n = lane & 31, h = lane >> 5;
-    const int kvh = blockIdx.x % a.n_kv;
-    Tile t;
-    if (!find_work<128, ROWS128_MIN_RUN>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;   // the whole workgroup
 
     const int row0 = t.row0 + wave * 32, row = row0 + n;
     const int token = row / a.G, head = kvh * a.G + row - token * a.G;
@@ -667,8 +711,8 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
         const int64_t at = page < 0 ? kvh * bt.head_stride : lvr_row_at(bt, page, kvh, k0 + group);   // no page: some memory of the pool
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            load_to_lds(a.k_pages + at, k_off[i], s_k[buf] + (wave * 4 + i) * 1024);
-            load_to_lds(a.v_pages + at, v_off[i], s_v[buf] + (wave * 4 + i) * 1024);
+            load_to_lds(a.k_pages + at, k_off[i], lds.k[buf] + (wave * 4 + i) * 1024);
+            load_to_lds(a.v_pages + at, v_off[i], lds.v[buf] + (wave * 4 + i) * 1024);
         }
         return (uint32_t)__ballot(pages < 0) & ((1u << TK / 16) - 1u);   // groups without a page
     };
@@ -693,18 +737,18 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
             for (int i = 0; i < 4; ++i) {
                 const int key = srow + i * RPI;
                 if (k0 + key < t.lo || k0 + key >= t.hi || (none >> (key >> 4) & 1))
-                    *reinterpret_cast<uint4 *>(s_v[buf] + key * R::ROWB + piece * 16) = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(lds.v[buf] + key * R::ROWB + piece * 16) = make_uint4(0, 0, 0, 0);
             }
             arrived();
         }
         if (k0 < whi && k0 + TK > wlo) {
             f32x16 p[R::NT];
-            R::scores(s_k[buf], q, n, h, p);
+            R::scores(lds.k[buf], q, n, h, p);
             const bool partly = k0 < all_lo || k0 + TK > all_hi || none != 0;
             if (partly) {
                 asm volatile("");   // a branch, not 32 selects in every tile
 #pragma unroll 1
-                for (int c = 0; c < TK * R::ROWB / 1024; ++c) redo |= R::odd(*reinterpret_cast<const uint4 *>(s_v[buf] + c * 1024 + lane * 16));
+                for (int c = 0; c < TK * R::ROWB / 1024; ++c) redo |= R::odd(*reinterpret_cast<const uint4 *>(lds.v[buf] + c * 1024 + lane * 16));
 #pragma unroll
                 for (int kt = 0; kt < R::NT; ++kt)
 #pragma unroll
@@ -732,7 +776,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
             for (int kt = 0; kt < R::NT; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) p[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[kt][r], a.unit, -base));
-            R::add(s_v[buf], p, lane, o, l);
+            R::add(lds.v[buf], p, lane, o, l);
         }
         arrived();
     }
@@ -747,7 +791,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
                 continue;
             }
             const float inv = s.l == 0.f ? 0.f : 1.f / s.l;
-            char *dst = a.out + ((int64_t)(t.first_token + r / a.G) * a.n_kv * a.G + kvh * a.G + r % a.G) * LVR_D * R::ELT;
+            char *dst = output_row<R::ELT>(a, t, kvh, r);
             if constexpr (R::ELT == 2) *reinterpret_cast<uint32_t *>(dst + lane * 4) = pack_bf16(s.o0 * inv, s.o1 * inv);
             else *reinterpret_cast<float2 *>(dst + lane * 8) = make_float2(s.o0 * inv, s.o1 * inv);
         }
@@ -766,7 +810,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;   // nothing seen: zeros
-    char *dst = a.out + ((int64_t)(t.first_token + token) * a.n_kv * a.G + head) * LVR_D * R::ELT;
+    char *dst = output_row<R::ELT>(a, t, kvh, row);
     if constexpr (R::ELT == 2) {
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
@@ -781,52 +825,63 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows128_kernel(AttnArg
     }
 }
 
+// Tiles of 16 rows alone: batches in which every sequence brings a token or so.
+template <typename KT>
+__global__ void __launch_bounds__(256, 2) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
+    __shared__ Rows16Lds lds;
+    const int kvh = blockIdx.x % a.n_kv;
+    Tile t;
+    if (find_work<false>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) rows16_piece<KT, 16>(a, bt, t, kvh, lds);
+}
+
+// Any batch: every sequence in the tiles that suit it.
+template <typename KT>
+__global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs a, lvr_paged_batch bt) {
+    __shared__ union { Rows16Lds narrow; Rows128Lds<KT> wide; } lds;
+    const int kvh = blockIdx.x % a.n_kv;
+    Tile t;
+    if (!find_work<true>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;
+    if (t.height == 128) rows128_piece<KT>(a, bt, t, kvh, lds.wide);
+    else rows16_piece<KT, 128>(a, bt, t, kvh, lds.narrow);
+}
+
 // Merges the runs of cut 128-row tiles: a workgroup takes 16 rows (blockIdx.y) of a piece's tile, 16 lanes to a row, where the
 // piece is the tile's first run.
 template <typename KT>
 __global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, lvr_paged_batch bt) {
-    constexpr int ELT = sizeof(KT) == 4 ? 4 : 2;
     const int kvh = blockIdx.x % a.n_kv;
     Tile t;
-    if (!find_work<128, ROWS128_MIN_RUN>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;
+    if (!find_work<true>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;
     const int r = blockIdx.y * 16 + (threadIdx.x >> 4), c0 = (threadIdx.x & 15) * 8;
-    if (t.splits == 1 || t.split != 0 || t.row0 + r >= t.rows) return;
+    if (t.height != 128 || t.splits == 1 || t.split != 0 || t.row0 + r >= t.rows) return;
     const float *first_part = partial<128>(a.part, t.slot, a.n_kv, kvh);
     const int64_t step = (int64_t)a.n_kv * (128 * (LVR_D + 2));
-    float M = -INFINITY, sum = 0.f, x[8];
-    lvr_zero8(x);
+    Merged x;
+    x.clear();
 #pragma unroll 4
     for (int p = 0; p < t.splits; ++p) {
         const float2 ml = *reinterpret_cast<const float2 *>(first_part + p * step + 128 * LVR_D + r * 2);
         const float4 v0 = *reinterpret_cast<const float4 *>(first_part + p * step + r * LVR_D + c0);
         const float4 v1 = *reinterpret_cast<const float4 *>(first_part + p * step + r * LVR_D + c0 + 4);
-        const float raised = fmaxf(M, ml.x);
-        const float old = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - raised);
-        const float scale = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - raised);   // nothing seen in that run
-        M = raised;
-        sum = sum * old + scale * ml.y;
-        x[0] = x[0] * old + scale * v0.x; x[1] = x[1] * old + scale * v0.y; x[2] = x[2] * old + scale * v0.z; x[3] = x[3] * old + scale * v0.w;
-        x[4] = x[4] * old + scale * v1.x; x[5] = x[5] * old + scale * v1.y; x[6] = x[6] * old + scale * v1.z; x[7] = x[7] * old + scale * v1.w;
+        const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+        x.add(ml.x, ml.y, v);
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int token = (t.row0 + r) / a.G, head = kvh * a.G + t.row0 + r - token * a.G;
-    char *dst = a.out + (((int64_t)(t.first_token + token) * a.n_kv * a.G + head) * LVR_D + c0) * ELT;
-    if constexpr (ELT == 2) {
-        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv), pack_bf16(x[4] * inv, x[5] * inv),
-                                                     pack_bf16(x[6] * inv, x[7] * inv));
-    } else {
-        *reinterpret_cast<float4 *>(dst) = make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-        *reinterpret_cast<float4 *>(dst + 16) = make_float4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
-    }
+    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = x.o[e] * inv;
+    store_row<sizeof(KT) == 4 ? 4 : 2>(a, t, kvh, t.row0 + r, c0, y);
 }
 
 }  // namespace
 
 size_t lvr_paged_partial_bytes() {
-    const size_t narrow = (size_t)2 * ROWS16_PIECES * 16 * (LVR_D + 2), wide = (size_t)2 * ROWS128_PIECES * 128 * (LVR_D + 2);
+    const size_t narrow = (size_t)2 * ROWS16_PIECES * 16 * (LVR_D + 2), wide = (size_t)2 * MIXED_PIECES * 128 * (LVR_D + 2);
     return (narrow > wide ? narrow : wide) * sizeof(float);
 }
-size_t lvr_paged_ticket_bytes() { return (size_t)2 * ROWS16_PIECES * LVR_CNT_STRIDE * sizeof(uint32_t); }
+size_t lvr_paged_ticket_bytes() {
+    return (size_t)2 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES) * LVR_CNT_STRIDE * sizeof(uint32_t);
+}
 
 hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
                                       int64_t q_stride_bytes, int32_t window, void *out, hipStream_t st) {
@@ -842,23 +897,25 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.unit = pc->sigma * LOG2E;
     a.part = pc->part;
     a.ticket = pc->ticket;
-    const bool wide = (int64_t)b.n_tokens * a.G > 32 * (int64_t)b.n_seqs;
-    const int64_t tiles = (int64_t)b.n_tokens * a.G / (wide ? 128 : 16) + b.n_seqs;
-    const int pieces = wide ? ROWS128_PIECES : ROWS16_PIECES;
-    a.target = pieces / a.n_kv;   // n_kv is at most 256
-    if (wide && (int64_t)b.n_tokens * a.G / 128 * a.n_kv >= 2 * ROWS128_PIECES) a.target = 0;   // enough tiles to fill the device without cuts
-    const dim3 grid((unsigned)((tiles + a.target) * a.n_kv));
-    if (wide) {
-        if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_rows128_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
-        else hipLaunchKernelGGL(paged_attention_rows128_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
-        if (a.target > 0) {
-            const dim3 merge(grid.x, 8);
-            if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_bf16_t>, merge, dim3(256), 0, st, a, b);
-            else hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_f32_t>, merge, dim3(256), 0, st, a, b);
-        }
-    } else {
-        if (pc->cfg.kv_dtype == LVR_BF16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
+    const bool bf16 = pc->cfg.kv_dtype == LVR_BF16;
+    const int64_t rows = (int64_t)b.n_tokens * a.G;
+    if (b.n_tokens <= b.n_seqs || rows <= NARROW) {
+        a.target = ROWS16_PIECES / a.n_kv;   // n_kv is at most 256
+        const dim3 grid((unsigned)((rows / 16 + b.n_seqs + a.target) * a.n_kv));
+        if (bf16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
         else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
+        return hipGetLastError();
+    }
+    a.target = MIXED_PIECES / a.n_kv;
+    if (rows / 128 * a.n_kv >= 4 * MIXED_PIECES) a.target = 0;   // tiles enough to fill the device without cuts
+    // tiles: a sequence's rows over 128 and one more, or at most NARROW / 16
+    const dim3 grid((unsigned)((rows / 128 + (int64_t)(NARROW / 16) * b.n_seqs + a.target) * a.n_kv));
+    if (bf16) hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
+    else hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
+    if (a.target > 0) {
+        const dim3 merge(grid.x, 8);
+        if (bf16) hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_bf16_t>, merge, dim3(256), 0, st, a, b);
+        else hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_f32_t>, merge, dim3(256), 0, st, a, b);
     }
     return hipGetLastError();
 }

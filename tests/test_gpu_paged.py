@@ -148,6 +148,8 @@ LENS = {
     "one_chunk": [(130, 130)],
     "late_chunk": [(70, 700), (3, 3)],
     "beside_decodes": [(200, 333), (1, 90), (1, 1), (1, 513)],
+    "many": [(1 + (i * 7) % 3, 3 + (i * 37) % 90) for i in range(70)] + [(0, 12)] * 70 + [(40, 300), (1, 600)],
+    "many_single_tokens": [(1, 1 + (i * 53) % 400) for i in range(131)],
     "tokens_before_the_cache": [(5, 3), (1, 0), (4, 0), (2, 40)],
 }
 
