@@ -16,9 +16,10 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
 // Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.
-constexpr int ROWS16_PIECES = 2048, MIXED_PIECES = 1024;
+constexpr int ROWS16_PIECES = 768, MIXED_PIECES = 1024;
 constexpr int MIN_RUN = 256, MAX_RUNS = 512;
 constexpr int NARROW = 32;    // rows of a sequence up to which it is taken in tiles of 16
+constexpr int MERGE_WGS = 1024;
 constexpr int FAN = 8;        // partial results of 16-row tiles merged at a time
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -59,102 +60,120 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// What sequence i brings, by the arrays on the device; whatever they hold, rows stay within the packed arrays and the table.
-__device__ __forceinline__ void sequence(const lvr_paged_batch &b, int i, int &s0, int &s1, int &n) {
-    s0 = b.seq_start[i];
-    s1 = b.seq_start[i + 1];
-    n = b.seq_len[i];
-    s0 = s0 < 0 ? 0 : (s0 > b.n_tokens ? b.n_tokens : s0);
-    s1 = s1 < s0 ? s0 : (s1 > b.n_tokens ? b.n_tokens : s1);
-    n = n < 0 ? 0 : (n > 1 << 30 ? 1 << 30 : n);
-}
-
-// Piece x of the batch, for one KV head.  The host knows neither how many tokens a sequence brings nor how many keys it holds, so
-// every workgroup works out the division for itself, each wave on its own.  MIXED: sequences of up to NARROW rows are
-// taken in tiles of 16, others in tiles of 128; else all in tiles of 16.  A sequence's tiles are cut into runs of L keys, L such that
-// the batch makes about `target` pieces of the same length (but none under MIN_RUN keys, and no more than MAX_RUNS of a tile;
-// target 0: no cuts).  There are at most `target` pieces more than tiles, and at most 2 * target pieces of tiles that are
-// cut: a cut tile has at most twice as many runs as its keys are times L, and all keys of all tiles are at most target times L.
-// The last tiles come first: in a prompt they see most keys.
+// How a batch is divided into pieces, for one KV head.  The host knows neither how many tokens a sequence brings nor how many keys it
+// holds, so every workgroup works it out for itself, each wave on its own, a lane to a sequence (64 at a time).  MIXED: sequences of
+// up to NARROW rows are taken in tiles of 16, others in tiles of 128; else all in tiles of 16.  A sequence's tiles are cut
+// into runs of keys, L such that the batch makes about `target` pieces of the same length (but none under MIN_RUN keys, and
+// no more than MAX_RUNS of a tile; target 0: no cuts).  There are at most `target` pieces more than tiles, and at most
+// 2 * target pieces of tiles that are cut: a cut tile has at most twice as many runs as its keys are times L, and all keys
+// of all tiles are at most target times L.
 template <bool MIXED>
-__device__ __forceinline__ bool find_work(const lvr_paged_batch &b, int G, int window, int target, int x, Tile &t) {
-    const int lane = lvr_lane();
-    int tiles = 0, span = 0;
-    auto look = [&](int i) {
-        tiles = span = 0;
-        if (i < b.n_seqs) {
-            int s0, s1, n;
-            sequence(b, i, s0, s1, n);
+struct Division {
+    const lvr_paged_batch &b;
+    int G, window, L;
+    int s0, s1, n, tiles, span, run, runs;   // this lane's sequence
+
+    __device__ __forceinline__ static bool wide(int rows) { return MIXED && rows > NARROW; }
+    __device__ __forceinline__ void look(int i) {
+        s0 = s1 = n = tiles = span = 0;
+        if (i < b.n_seqs) {   // whatever the arrays hold, rows stay within the packed arrays and the table
+            s0 = b.seq_start[i];
+            s1 = b.seq_start[i + 1];
+            n = b.seq_len[i];
+            s0 = s0 < 0 ? 0 : (s0 > b.n_tokens ? b.n_tokens : s0);
+            s1 = s1 < s0 ? s0 : (s1 > b.n_tokens ? b.n_tokens : s1);
+            n = n < 0 ? 0 : (n > 1 << 30 ? 1 << 30 : n);
             const int rows = (s1 - s0) * G;
-            const bool wide = MIXED && rows > NARROW;
-            tiles = wide ? (rows + 127) / 128 : (rows + 15) / 16;
-            const int reach = window ? window + (wide ? 128 : 16) / G + 2 : n;   // keys a tile can see
+            tiles = wide(rows) ? (rows + 127) / 128 : (rows + 15) / 16;
+            const int reach = window ? window + (wide(rows) ? 128 : 16) / G + 2 : n;   // keys a tile can see
             span = n < reach ? n : reach;
             if (span < 1) span = 1;
-            return (float)(s1 - s0);
         }
-        return 0.f;
-    };
-    float keys = 0.f, tokens = 0.f;
-    for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
-        tokens += look(i0 + lane);
-        keys += (float)tiles * (float)span;
     }
-    tokens = wave_sum(tokens);
-    if (tokens > (float)b.n_tokens) return false;   // seq_start is not ascending: no piece is where another expects it
-    int L = 1 << 30;
-    if (target > 0) {
-        const float want = wave_sum(keys) * 1.001f / (float)target;   // (more than what the sum was rounded by)
-        L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? 1 << 30 : ((int)want + 64) & ~63);
-    }
-    int before = 0, cut_before = 0;
-    for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
-        if (b.n_seqs > 64) look(i0 + lane);
-        int run = L;
+    __device__ __forceinline__ void cut() {
+        run = L;
         if (span > MAX_RUNS * (MIN_RUN / 2)) {
             const int least = (span / MAX_RUNS + 64) & ~63;
             if (run < least) run = least;
         }
-        const int runs = (span + run - 1) / run, pieces = tiles * runs;
-        const int upto = before + lvr_wave_inclusive_sum(pieces), cut = runs > 1 ? pieces : 0;
-        const int cut_upto = cut_before + lvr_wave_inclusive_sum(cut);
-        const uint64_t past = __ballot(upto > x);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            const int seq_runs = __builtin_amdgcn_readlane(runs, at), seq_run = __builtin_amdgcn_readlane(run, at);
-            const int k = x - __builtin_amdgcn_readlane(upto - pieces, at);   // which of the sequence's pieces
-            const int tile = __builtin_amdgcn_readlane(tiles, at) - 1 - k / seq_runs;
-            t.slot = __builtin_amdgcn_readlane(cut_upto - cut, at) + k;
-            t.split = k % seq_runs;
-            t.seq = i0 + at;
-            int s0, s1, n;
-            sequence(b, t.seq, s0, s1, n);
-            t.first_token = s0;
-            t.rows = (s1 - s0) * G;
-            t.height = MIXED && t.rows > NARROW ? 128 : 16;
-            t.row0 = tile * t.height;
-            t.pos0 = n - (s1 - s0);
-            const int last_row = (t.row0 + t.height < t.rows ? t.row0 + t.height : t.rows) - 1;
-            t.hi = t.pos0 + last_row / G + 1;
-            if (t.hi > b.table_width << b.page_shift) t.hi = b.table_width << b.page_shift;
-            t.lo = window ? t.pos0 + t.row0 / G - window + 1 : 0;
-            if (t.lo < 0) t.lo = 0;
-            const int from = t.lo & ~63;
-            t.splits = 1;
-            if (seq_runs > 1 && t.hi > from) {
-                t.splits = (t.hi - from - 1) / seq_run + 1;
-                if (t.splits > seq_runs) t.splits = seq_runs;
-            }
-            if (t.split >= t.splits) return false;   // a run past what this tile sees
-            t.begin = from + t.split * seq_run;
-            t.end = t.split + 1 < t.splits ? t.begin + seq_run : t.hi;
-            return true;
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
-        cut_before = __builtin_amdgcn_readlane(cut_upto, 63);
+        runs = (span + run - 1) / run;
     }
-    return false;
-}
+    // false: seq_start is not ascending, no piece is where another expects it
+    __device__ __forceinline__ Division(const lvr_paged_batch &bt, int G_, int window_) : b(bt), G(G_), window(window_) {}
+    __device__ __forceinline__ bool divide(int target) {
+        float keys = 0.f;
+        int64_t tokens = 0;
+        for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
+            look(i0 + lvr_lane());
+            tokens += s1 - s0;
+            keys += (float)tiles * (float)span;
+        }
+        if (b.n_seqs > 1) {
+            if (wave_sum((float)tokens) > (float)b.n_tokens) return false;   // whole numbers below 2^24 where it matters
+            keys = wave_sum(keys);
+        } else {
+            keys = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(keys)));
+        }
+        L = 1 << 30;
+        if (target > 0) {
+            const float want = keys * 1.001f / (float)target;   // (more than what the sum was rounded by)
+            L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? 1 << 30 : ((int)want + 64) & ~63);
+        }
+        cut();
+        return true;
+    }
+    // Piece x, or for CUT tile x of the 128-row tiles that are cut (its first run).  The last tiles come first: in a prompt
+    // they see most keys.
+    template <bool CUT>
+    __device__ __forceinline__ bool locate(int x, Tile &t) {
+        int before = 0, cut_before = 0;
+        for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
+            if (b.n_seqs > 64) {
+                look(i0 + lvr_lane());
+                cut();
+            }
+            const int pieces = tiles * runs, of_cut = runs > 1 ? pieces : 0;
+            const int count = CUT ? (runs > 1 && wide((s1 - s0) * G) ? tiles : 0) : pieces;
+            const int upto = before + lvr_wave_inclusive_sum(count);
+            const int cut_upto = cut_before + lvr_wave_inclusive_sum(of_cut);
+            const uint64_t past = __ballot(upto > x);
+            if (past) {
+                const int at = __builtin_ctzll(past);
+                auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+                const int seq_runs = of(runs), seq_run = of(run);
+                const int k = (x - of(upto - count)) * (CUT ? seq_runs : 1);   // which of the sequence's pieces
+                const int tile = of(tiles) - 1 - k / seq_runs;
+                t.slot = of(cut_upto - of_cut) + k;
+                t.split = k % seq_runs;
+                t.seq = i0 + at;
+                const int first = of(s0), tokens = of(s1) - first;
+                t.first_token = first;
+                t.rows = tokens * G;
+                t.height = wide(t.rows) ? 128 : 16;
+                t.row0 = tile * t.height;
+                t.pos0 = of(n) - tokens;
+                const int last_row = (t.row0 + t.height < t.rows ? t.row0 + t.height : t.rows) - 1;
+                t.hi = t.pos0 + last_row / G + 1;
+                if (t.hi > b.table_width << b.page_shift) t.hi = b.table_width << b.page_shift;
+                t.lo = window ? t.pos0 + t.row0 / G - window + 1 : 0;
+                if (t.lo < 0) t.lo = 0;
+                const int from = t.lo & ~63;
+                t.splits = 1;
+                if (seq_runs > 1 && t.hi > from) {
+                    t.splits = (t.hi - from - 1) / seq_run + 1;
+                    if (t.splits > seq_runs) t.splits = seq_runs;
+                }
+                if (t.split >= t.splits) return false;   // a run past what this tile sees
+                t.begin = from + t.split * seq_run;
+                t.end = t.split + 1 < t.splits ? t.begin + seq_run : t.hi;
+                return true;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+            cut_before = __builtin_amdgcn_readlane(cut_upto, 63);
+        }
+        return false;
+    }
+};
 
 // Partial results of pieces: per slot and KV head room for SLOT rows of 128 sums, then SLOT pairs of maximum and weight.
 template <int SLOT>
@@ -831,7 +850,8 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows16_kernel(AttnArgs
     __shared__ Rows16Lds lds;
     const int kvh = blockIdx.x % a.n_kv;
     Tile t;
-    if (find_work<false>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) rows16_piece<KT, 16>(a, bt, t, kvh, lds);
+    Division<false> d(bt, a.G, a.window);
+    if (d.divide(a.target) && d.template locate<false>(blockIdx.x / a.n_kv, t)) rows16_piece<KT, 16>(a, bt, t, kvh, lds);
 }
 
 // Any batch: every sequence in the tiles that suit it.
@@ -840,37 +860,41 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
     __shared__ union { Rows16Lds narrow; Rows128Lds<KT> wide; } lds;
     const int kvh = blockIdx.x % a.n_kv;
     Tile t;
-    if (!find_work<true>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;
+    Division<true> d(bt, a.G, a.window);
+    if (!d.divide(a.target) || !d.template locate<false>(blockIdx.x / a.n_kv, t)) return;
     if (t.height == 128) rows128_piece<KT>(a, bt, t, kvh, lds.wide);
     else rows16_piece<KT, 128>(a, bt, t, kvh, lds.narrow);
 }
 
-// Merges the runs of cut 128-row tiles: a workgroup takes 16 rows (blockIdx.y) of a piece's tile, 16 lanes to a row, where the
-// piece is the tile's first run.
+// Merges the runs of cut 128-row tiles.  16 rows of a tile at a time, 16 lanes to a row; the workgroups share them out.
 template <typename KT>
 __global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, lvr_paged_batch bt) {
-    const int kvh = blockIdx.x % a.n_kv;
-    Tile t;
-    if (!find_work<true>(bt, a.G, a.window, a.target, blockIdx.x / a.n_kv, t)) return;
-    const int r = blockIdx.y * 16 + (threadIdx.x >> 4), c0 = (threadIdx.x & 15) * 8;
-    if (t.height != 128 || t.splits == 1 || t.split != 0 || t.row0 + r >= t.rows) return;
-    const float *first_part = partial<128>(a.part, t.slot, a.n_kv, kvh);
+    Division<true> d(bt, a.G, a.window);
+    if (!d.divide(a.target)) return;
+    const int c0 = (threadIdx.x & 15) * 8;
     const int64_t step = (int64_t)a.n_kv * (128 * (LVR_D + 2));
-    Merged x;
-    x.clear();
+    for (int item = blockIdx.x;; item += gridDim.x) {
+        const int kvh = item % a.n_kv, r = item / a.n_kv % 8 * 16 + (threadIdx.x >> 4);
+        Tile t;
+        if (!d.template locate<true>(item / a.n_kv / 8, t)) return;
+        if (t.splits == 1 || t.row0 + r >= t.rows) continue;
+        const float *first_part = partial<128>(a.part, t.slot, a.n_kv, kvh);
+        Merged x;
+        x.clear();
 #pragma unroll 4
-    for (int p = 0; p < t.splits; ++p) {
-        const float2 ml = *reinterpret_cast<const float2 *>(first_part + p * step + 128 * LVR_D + r * 2);
-        const float4 v0 = *reinterpret_cast<const float4 *>(first_part + p * step + r * LVR_D + c0);
-        const float4 v1 = *reinterpret_cast<const float4 *>(first_part + p * step + r * LVR_D + c0 + 4);
-        const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-        x.add(ml.x, ml.y, v);
-    }
-    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
-    float y[8];
+        for (int p = 0; p < t.splits; ++p) {
+            const float2 ml = *reinterpret_cast<const float2 *>(first_part + p * step + 128 * LVR_D + r * 2);
+            const float4 v0 = *reinterpret_cast<const float4 *>(first_part + p * step + r * LVR_D + c0);
+            const float4 v1 = *reinterpret_cast<const float4 *>(first_part + p * step + r * LVR_D + c0 + 4);
+            const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+            x.add(ml.x, ml.y, v);
+        }
+        const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
+        float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = x.o[e] * inv;
-    store_row<sizeof(KT) == 4 ? 4 : 2>(a, t, kvh, t.row0 + r, c0, y);
+        for (int e = 0; e < 8; ++e) y[e] = x.o[e] * inv;
+        store_row<sizeof(KT) == 4 ? 4 : 2>(a, t, kvh, t.row0 + r, c0, y);
+    }
 }
 
 }  // namespace
@@ -907,13 +931,14 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
         return hipGetLastError();
     }
     a.target = MIXED_PIECES / a.n_kv;
-    if (rows / 128 * a.n_kv >= 4 * MIXED_PIECES) a.target = 0;   // tiles enough to fill the device without cuts
+    // tiles enough to fill the device without cuts, or none longer than the shortest run
+    if (rows / 128 * a.n_kv >= 4 * MIXED_PIECES || b.table_width <= MIN_RUN >> b.page_shift) a.target = 0;
     // tiles: a sequence's rows over 128 and one more, or at most NARROW / 16
     const dim3 grid((unsigned)((rows / 128 + (int64_t)(NARROW / 16) * b.n_seqs + a.target) * a.n_kv));
     if (bf16) hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
     else hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
     if (a.target > 0) {
-        const dim3 merge(grid.x, 8);
+        const dim3 merge(MERGE_WGS);
         if (bf16) hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_bf16_t>, merge, dim3(256), 0, st, a, b);
         else hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_f32_t>, merge, dim3(256), 0, st, a, b);
     }
