@@ -16,7 +16,7 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
 // Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.
-constexpr int ROWS16_PIECES = 768, MIXED_PIECES = 1024;
+constexpr int ROWS16_PIECES = 768, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 1024;
 constexpr int MIN_RUN = 256, MAX_RUNS = 512;
 constexpr int NARROW = 32;    // rows of a sequence up to which it is taken in tiles of 16
 constexpr int MERGE_WGS = 1024;
@@ -924,7 +924,7 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     const bool bf16 = pc->cfg.kv_dtype == LVR_BF16;
     const int64_t rows = (int64_t)b.n_tokens * a.G;
     if (b.n_tokens <= b.n_seqs || rows <= NARROW) {
-        a.target = ROWS16_PIECES / a.n_kv;   // n_kv is at most 256
+        a.target = (b.n_seqs * a.n_kv <= 32 ? ROWS16_PIECES_FEW : ROWS16_PIECES) / a.n_kv;   // n_kv is at most 256
         const dim3 grid((unsigned)((rows / 16 + b.n_seqs + a.target) * a.n_kv));
         if (bf16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
         else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
