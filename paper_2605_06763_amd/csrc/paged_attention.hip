@@ -16,9 +16,13 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
 // Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.
-constexpr int ROWS16_PIECES = 768, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 1024;
+constexpr int ROWS16_PIECES = 768, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 512;
 constexpr int MIN_RUN = 256, MAX_RUNS = 512;
-constexpr int NARROW = 32;    // rows of a sequence up to which it is taken in tiles of 16
+// Rows of a sequence up to which it is taken in tiles of 16.  A wave of a 128-row tile works on 32 of them however many there are, and on
+// fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 57 in a tile of 128 / 46 in four of 16,
+// eight such sequences of 4096 keys 41 / 58; fp32 171 / 98).
+constexpr int NARROW_BF16 = 32, NARROW_F32 = 64;
+constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);
 constexpr int MERGE_WGS = 1024;
 constexpr int FAN = 8;        // partial results of 16-row tiles merged at a time
 
@@ -37,6 +41,7 @@ struct AttnArgs {
     int64_t q_stride;    // bytes per token
     int32_t n_kv, G, window;
     float unit;          // sigma * log2 e
+    int32_t narrow;      // rows of a sequence up to which it is taken in tiles of 16
     int32_t target;      // pieces of work to make of the batch per KV head; 0: tiles are not cut
     float *part;
     uint32_t *ticket;    // a line for each slot of a cut tile
@@ -62,18 +67,23 @@ __device__ __forceinline__ float wave_sum(float v) {
 
 // How a batch is divided into pieces, for one KV head.  The host knows neither how many tokens a sequence brings nor how many keys it
 // holds, so every workgroup works it out for itself, each wave on its own, a lane to a sequence (64 at a time).  MIXED: sequences of
-// up to NARROW rows are taken in tiles of 16, others in tiles of 128; else all in tiles of 16.  A sequence's tiles are cut
-// into runs of keys, L such that the batch makes about `target` pieces of the same length (but none under MIN_RUN keys, and
-// no more than MAX_RUNS of a tile; target 0: no cuts).  There are at most `target` pieces more than tiles, and at most
-// 2 * target pieces of tiles that are cut: a cut tile has at most twice as many runs as its keys are times L, and all keys
-// of all tiles are at most target times L.
+// up to a.narrow rows are taken in tiles of 16, others in tiles of 128; else all in tiles of 16.
+//
+// A sequence's tiles are cut into runs of keys of one length, as many as make about `target` pieces of the batch (but none under
+// MIN_RUN keys, and no more than MAX_RUNS of a tile; target 0: no cuts).  L is the keys of all tiles over target, where a tile
+// sees half of the sequence's own new keys.  Tiles of 128 rows are cut into span / L runs, rounded, so that equal ones fill whole
+// rounds of workgroups; beside them tiles of 16 rows, whose partial results are small, into runs of a quarter of that.  Without
+// tiles of 128 rows the number is rounded up.  There is room for the partial results of 2 * target pieces of cut 128-row tiles and
+// for 3 * target pieces of cut tiles altogether, and the launch has as many workgroups beside one for each tile: should there
+// be more, L grows until there are not.
 template <bool MIXED>
 struct Division {
     const lvr_paged_batch &b;
-    int G, window, L;
+    int G, window, narrow, L, n_wide;              // pieces of 128-row tiles, which come first
+    bool any_wide;
     int s0, s1, n, tiles, span, run, runs;   // this lane's sequence
 
-    __device__ __forceinline__ static bool wide(int rows) { return MIXED && rows > NARROW; }
+    __device__ __forceinline__ bool wide(int rows) const { return MIXED && rows > narrow; }
     __device__ __forceinline__ void look(int i) {
         s0 = s1 = n = tiles = span = 0;
         if (i < b.n_seqs) {   // whatever the arrays hold, rows stay within the packed arrays and the table
@@ -90,26 +100,33 @@ struct Division {
             if (span < 1) span = 1;
         }
     }
+    __device__ __forceinline__ bool is_wide() const { return wide((s1 - s0) * G); }
     __device__ __forceinline__ void cut() {
-        run = L;
+        int L1 = L;
         if (span > MAX_RUNS * (MIN_RUN / 2)) {
             const int least = (span / MAX_RUNS + 64) & ~63;
-            if (run < least) run = least;
+            if (L1 < least) L1 = least;
         }
+        if (MIXED && any_wide && !is_wide()) L1 = L1 > 4 * MIN_RUN ? L1 >> 2 : (L1 < MIN_RUN ? L1 : MIN_RUN);
+        runs = (span + (MIXED && is_wide() ? L1 >> 1 : L1 - 1)) / L1;
+        if (runs < 1) runs = 1;
+        run = ((span + runs - 1) / runs + 63) & ~63;
         runs = (span + run - 1) / run;
     }
+    __device__ __forceinline__ Division(const AttnArgs &a, const lvr_paged_batch &bt) : b(bt), G(a.G), window(a.window), narrow(a.narrow) {}
     // false: seq_start is not ascending, no piece is where another expects it
-    __device__ __forceinline__ Division(const lvr_paged_batch &bt, int G_, int window_) : b(bt), G(G_), window(window_) {}
     __device__ __forceinline__ bool divide(int target) {
-        float keys = 0.f;
-        int64_t tokens = 0;
+        float keys = 0.f, tokens = 0.f;
+        any_wide = false;
         for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
             look(i0 + lvr_lane());
-            tokens += s1 - s0;
-            keys += (float)tiles * (float)span;
+            const int own = (s1 - s0 < n ? s1 - s0 : n) / 2;
+            tokens += (float)(s1 - s0);
+            any_wide |= __any(is_wide());
+            keys += (float)tiles * (float)(window || !MIXED ? span : span - own);
         }
         if (b.n_seqs > 1) {
-            if (wave_sum((float)tokens) > (float)b.n_tokens) return false;   // whole numbers below 2^24 where it matters
+            if (wave_sum(tokens) > (float)b.n_tokens) return false;   // whole numbers below 2^24 where it matters
             keys = wave_sum(keys);
         } else {
             keys = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(keys)));
@@ -117,23 +134,39 @@ struct Division {
         L = 1 << 30;
         if (target > 0) {
             const float want = keys * 1.001f / (float)target;   // (more than what the sum was rounded by)
-            L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? 1 << 30 : ((int)want + 64) & ~63);
+            L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? 1 << 30 : ((int)want + 63) & ~63);
         }
-        cut();
+        for (;; L = L < 1 << 28 ? (L + L / 2) & ~63 : 1 << 30) {
+            int cut_wide = 0, cut_narrow = 0;
+            n_wide = 0;
+            for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
+                if (b.n_seqs > 64) look(i0 + lvr_lane());
+                cut();
+                const int cut_here = runs > 1 ? tiles * runs : 0;
+                if (MIXED) {
+                    n_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? tiles * runs : 0), 63);
+                    cut_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? cut_here : 0), 63);
+                }
+                cut_narrow += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? 0 : cut_here), 63);
+            }
+            if ((cut_wide <= 2 * target && cut_wide + cut_narrow <= 3 * target) || L == 1 << 30) break;
+        }
         return true;
     }
-    // Piece x, or for CUT tile x of the 128-row tiles that are cut (its first run).  The last tiles come first: in a prompt
-    // they see most keys.
+    // Piece x, or for CUT tile x of the 128-row tiles that are cut (its first run).  Long pieces come first: those of 128-row tiles, and of
+    // a sequence's tiles the last ones.
     template <bool CUT>
     __device__ __forceinline__ bool locate(int x, Tile &t) {
         int before = 0, cut_before = 0;
+        const bool in_wide = CUT || x < n_wide;
+        if (!in_wide) x -= n_wide;
         for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
             if (b.n_seqs > 64) {
                 look(i0 + lvr_lane());
                 cut();
             }
-            const int pieces = tiles * runs, of_cut = runs > 1 ? pieces : 0;
-            const int count = CUT ? (runs > 1 && wide((s1 - s0) * G) ? tiles : 0) : pieces;
+            const int pieces = is_wide() == in_wide ? tiles * runs : 0, of_cut = runs > 1 ? pieces : 0;
+            const int count = CUT ? (of_cut ? tiles : 0) : pieces;
             const int upto = before + lvr_wave_inclusive_sum(count);
             const int cut_upto = cut_before + lvr_wave_inclusive_sum(of_cut);
             const uint64_t past = __ballot(upto > x);
@@ -175,10 +208,12 @@ struct Division {
     }
 };
 
-// Partial results of pieces: per slot and KV head room for SLOT rows of 128 sums, then SLOT pairs of maximum and weight.
-template <int SLOT>
+// Partial results of pieces of cut tiles of HEIGHT rows: per slot and KV head HEIGHT rows of 128 sums, then HEIGHT pairs of maximum
+// and weight.  Those of 128-row tiles first.
+template <int HEIGHT>
 __device__ __forceinline__ float *partial(float *part, int slot, int n_kv, int kvh) {
-    return part + ((int64_t)slot * n_kv + kvh) * (SLOT * (LVR_D + 2));
+    if (HEIGHT == 16) part += (int64_t)WIDE_ROOM * 128 * (LVR_D + 2);
+    return part + ((int64_t)slot * n_kv + kvh) * (HEIGHT * (LVR_D + 2));
 }
 
 // Sums over several sets of keys, brought to a common maximum.
@@ -386,7 +421,7 @@ struct Rows16Lds {
     unsigned arrived;
 };
 
-template <typename KT, int SLOT>
+template <typename KT>
 __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, Rows16Lds &lds) {
     typedef Rows16<KT> R;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -505,13 +540,13 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
         // wraps at the number of those who take it and so is zero again afterwards.
         const int slot0 = t.slot - t.split, fans = (t.splits + FAN - 1) / FAN, fan = t.split / FAN;
         const int in_fan = fan + 1 < fans ? FAN : t.splits - fan * FAN;
-        float *first_part = partial<SLOT>(a.part, slot0, a.n_kv, kvh);
-        const int64_t step = (int64_t)a.n_kv * (SLOT * (LVR_D + 2));
+        float *first_part = partial<16>(a.part, slot0, a.n_kv, kvh);
+        const int64_t step = (int64_t)a.n_kv * (16 * (LVR_D + 2));
         auto put = [&](float *p) {
             if (!writes) return;
 #pragma unroll
             for (int e = 0; e < 8; e += 2) store_shared(p + r * LVR_D + c0 + e, make_float2(x.o[e], x.o[e + 1]));
-            if (c0 == 0) store_shared(p + SLOT * LVR_D + r * 2, make_float2(x.m, x.l));
+            if (c0 == 0) store_shared(p + 16 * LVR_D + r * 2, make_float2(x.m, x.l));
         };
         auto last_of = [&](int slot, int word, int n) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -527,7 +562,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 #pragma unroll
                 for (int k = 0; k < FAN; ++k) {   // all in flight; past the last one the last once more
                     const float *from = p + (p0 + k < n ? p0 + k : n - 1) * apart;
-                    ml[k] = load_shared(from + SLOT * LVR_D + r * 2);
+                    ml[k] = load_shared(from + 16 * LVR_D + r * 2);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[k][e] = load_shared(from + r * LVR_D + c0 + 2 * e);
                 }
@@ -850,8 +885,8 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows16_kernel(AttnArgs
     __shared__ Rows16Lds lds;
     const int kvh = blockIdx.x % a.n_kv;
     Tile t;
-    Division<false> d(bt, a.G, a.window);
-    if (d.divide(a.target) && d.template locate<false>(blockIdx.x / a.n_kv, t)) rows16_piece<KT, 16>(a, bt, t, kvh, lds);
+    Division<false> d(a, bt);
+    if (d.divide(a.target) && d.template locate<false>(blockIdx.x / a.n_kv, t)) rows16_piece<KT>(a, bt, t, kvh, lds);
 }
 
 // Any batch: every sequence in the tiles that suit it.
@@ -860,16 +895,16 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
     __shared__ union { Rows16Lds narrow; Rows128Lds<KT> wide; } lds;
     const int kvh = blockIdx.x % a.n_kv;
     Tile t;
-    Division<true> d(bt, a.G, a.window);
+    Division<true> d(a, bt);
     if (!d.divide(a.target) || !d.template locate<false>(blockIdx.x / a.n_kv, t)) return;
     if (t.height == 128) rows128_piece<KT>(a, bt, t, kvh, lds.wide);
-    else rows16_piece<KT, 128>(a, bt, t, kvh, lds.narrow);
+    else rows16_piece<KT>(a, bt, t, kvh, lds.narrow);
 }
 
 // Merges the runs of cut 128-row tiles.  16 rows of a tile at a time, 16 lanes to a row; the workgroups share them out.
 template <typename KT>
 __global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, lvr_paged_batch bt) {
-    Division<true> d(bt, a.G, a.window);
+    Division<true> d(a, bt);
     if (!d.divide(a.target)) return;
     const int c0 = (threadIdx.x & 15) * 8;
     const int64_t step = (int64_t)a.n_kv * (128 * (LVR_D + 2));
@@ -899,13 +934,8 @@ __global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, 
 
 }  // namespace
 
-size_t lvr_paged_partial_bytes() {
-    const size_t narrow = (size_t)2 * ROWS16_PIECES * 16 * (LVR_D + 2), wide = (size_t)2 * MIXED_PIECES * 128 * (LVR_D + 2);
-    return (narrow > wide ? narrow : wide) * sizeof(float);
-}
-size_t lvr_paged_ticket_bytes() {
-    return (size_t)2 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES) * LVR_CNT_STRIDE * sizeof(uint32_t);
-}
+size_t lvr_paged_partial_bytes() { return ((size_t)WIDE_ROOM * 128 + (size_t)NARROW_ROOM * 16) * (LVR_D + 2) * sizeof(float); }
+size_t lvr_paged_ticket_bytes() { return (size_t)NARROW_ROOM * LVR_CNT_STRIDE * sizeof(uint32_t); }
 
 hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
                                       int64_t q_stride_bytes, int32_t window, void *out, hipStream_t st) {
@@ -923,7 +953,8 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.ticket = pc->ticket;
     const bool bf16 = pc->cfg.kv_dtype == LVR_BF16;
     const int64_t rows = (int64_t)b.n_tokens * a.G;
-    if (b.n_tokens <= b.n_seqs || rows <= NARROW) {
+    a.narrow = bf16 ? NARROW_BF16 : NARROW_F32;
+    if (b.n_tokens <= b.n_seqs || rows <= a.narrow) {
         a.target = (b.n_seqs * a.n_kv <= 32 ? ROWS16_PIECES_FEW : ROWS16_PIECES) / a.n_kv;   // n_kv is at most 256
         const dim3 grid((unsigned)((rows / 16 + b.n_seqs + a.target) * a.n_kv));
         if (bf16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
@@ -932,9 +963,9 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     }
     a.target = MIXED_PIECES / a.n_kv;
     // tiles enough to fill the device without cuts, or none longer than the shortest run
-    if (rows / 128 * a.n_kv >= 4 * MIXED_PIECES || b.table_width <= MIN_RUN >> b.page_shift) a.target = 0;
-    // tiles: a sequence's rows over 128 and one more, or at most NARROW / 16
-    const dim3 grid((unsigned)((rows / 128 + (int64_t)(NARROW / 16) * b.n_seqs + a.target) * a.n_kv));
+    if (rows / 128 * a.n_kv >= 8 * MIXED_PIECES || b.table_width <= MIN_RUN >> b.page_shift) a.target = 0;
+    // tiles: a sequence's rows over 128 and one more, or at most narrow / 16
+    const dim3 grid((unsigned)((rows / 128 + (int64_t)(a.narrow / 16) * b.n_seqs + 3 * a.target) * a.n_kv));
     if (bf16) hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
     else hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
     if (a.target > 0) {
