@@ -21,6 +21,8 @@ if os.path.exists(CALL_PATH):
         from . import _call
         if _call.TORCH_VERSION != re.match(r"[\d.]*\d", torch.__version__).group():
             raise ImportError(f"built for torch {_call.TORCH_VERSION}, this is {torch.__version__}")
+        if not hasattr(_call, "paged_gather"):
+            raise ImportError("built from other sources")
     except ImportError as e:
         _call = None
         warnings.warn(f"{os.path.basename(CALL_PATH)} does not load, calls go through ctypes; build it again "
@@ -149,7 +151,7 @@ def lib():
     L.lvr_last_hip_error.restype = C.c_int
     if _call is not None:
         for name in ("lvr_decode_step", "lvr_append_decode_step", "lvr_query", "lvr_sparse_attention", "lvr_sparse_attention_static",
-                     "lvr_dense_attention"):
+                     "lvr_dense_attention", "lvr_paged_append", "lvr_paged_attention", "lvr_paged_gather"):
             _call.bind(name, C.cast(getattr(L, name), vp).value)
     _lib = L
     return L
@@ -453,6 +455,7 @@ def lvr_export_index(h, cfg: lvr_config):
 class PagedHandle(C.c_void_p):
     """What lvr_paged_create returns: the C handle, with what the calls check tensors against."""
     cfg: lvr_paged_config
+    cfg_at: int          # its address, for the compiled calls
     dtype: torch.dtype
 
 
@@ -485,6 +488,7 @@ def lvr_paged_create(cfg: lvr_paged_config, inv_freq=None, axis=None) -> PagedHa
     h = PagedHandle()
     _check(lib().lvr_paged_create(C.byref(cfg), freq, ax, C.byref(h)), "lvr_paged_create")
     h.cfg = lvr_paged_config.from_buffer_copy(cfg)
+    h.cfg_at = C.addressof(h.cfg)
     h.dtype = torch.bfloat16 if cfg.kv_dtype == LVR_BF16 else torch.float32
     return h
 
@@ -493,11 +497,17 @@ def lvr_paged_destroy(h) -> None:
     _check(lib().lvr_paged_destroy(h), "lvr_paged_destroy")
 
 
-def _pool(h, t: torch.Tensor, name: str):
-    """A pool of pages: [page][head][token][head_dim] or [page][token][head][head_dim] with the strides of the configuration."""
-    c = h.cfg
+def _tensor(t, name: str) -> torch.Tensor:
+    if type(t) is DeviceArg:
+        t = t.tensor
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    return t
+
+
+def _pool(h, t, name: str):
+    """A pool of pages: [page][head][token][head_dim] or [page][token][head][head_dim] with the strides of the configuration."""
+    c, t = h.cfg, _tensor(t, name)
     if t.dtype != h.dtype:
         raise ValueError(f"{name} must be {h.dtype}, got {t.dtype}")
     want, shape = tuple(c.page_strides), tuple(t.shape)
@@ -511,26 +521,23 @@ def _pool(h, t: torch.Tensor, name: str):
                      f"{want} (page, head, token), got {shape} with strides {tuple(t.stride())}")
 
 
-def _tokens(h, t: torch.Tensor, heads: int, n, name: str):
-    """Rows of new tokens [n_tokens][heads][head_dim], the heads of a token contiguous.  Returns pointer and token stride."""
-    c = h.cfg
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
+def _tokens(h, t, heads: int, n, name: str):
+    """Rows of new tokens [n_tokens][heads][head_dim], the heads of a token contiguous.  Returns pointer, token stride and n_tokens."""
+    c, t = h.cfg, _tensor(t, name)
     if t.dtype != h.dtype:
         raise ValueError(f"{name} must be {h.dtype}, got {t.dtype}")
     if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != c.head_dim or (n is not None and t.shape[0] != n):
         raise ValueError(f"{name} must be [{'n_tokens' if n is None else n}][{heads}][{c.head_dim}], got {tuple(t.shape)}")
     if t.shape[0] == 0:
-        return t.data_ptr(), heads * c.head_dim
+        return t.data_ptr(), heads * c.head_dim, 0
     if t.stride(2) != 1 or (heads > 1 and t.stride(1) != c.head_dim):
         raise ValueError(f"the heads of a token in {name} must be contiguous")
     # (the stride of one token's array says nothing)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * c.head_dim
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * c.head_dim, t.shape[0]
 
 
-def _whole(t: torch.Tensor, dtype, shape, name: str):
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
+def _whole(t, dtype, shape, name: str):
+    t = _tensor(t, name)
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if tuple(t.shape) != shape or not t.is_contiguous():
@@ -539,6 +546,7 @@ def _whole(t: torch.Tensor, dtype, shape, name: str):
 
 
 def _batch(seq_start, seq_len, table):
+    table = _tensor(table, "table")
     if table.dim() != 2:
         raise ValueError("table must be [n_seqs][table_width]")
     n, width = table.shape
@@ -549,41 +557,56 @@ def _batch(seq_start, seq_len, table):
 def lvr_paged_append(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q=None, q_out=None, positions=None, stream=None) -> None:
     """k_new, v_new [n_tokens][n_kv_heads][128], q and q_out [n_tokens][n_q_heads][128] (q_out contiguous, or q itself);
     positions [n_tokens][rot_axes] int32, None: the token's position in its sequence; seq_start, seq_len, table: int32."""
-    kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
-    k, ks = _tokens(h, k_new, h.cfg.n_kv_heads, None, "k_new")
-    n = k_new.shape[0]
-    v, vs = _tokens(h, v_new, h.cfg.n_kv_heads, n, "v_new")
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out go together")
-    qp = qo = None
-    qs = 0
-    if q is not None:
-        qp, qs = _tokens(h, q, h.cfg.n_q_heads, n, "q")
-        qo = _whole(q_out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "q_out")
-    pos = None if positions is None else _whole(positions, torch.int32, (n, max(h.cfg.rot_axes, 1)), "positions")
-    start, length, tab, width, seqs = _batch(seq_start, seq_len, table)
-    _check(lib().lvr_paged_append(h, kp, vp, k, v, qp, qo, (C.c_int64 * 3)(ks, vs, qs), pos, start, length, tab, width, seqs, n,
-                                  _stream(stream)), "lvr_paged_append")
+    st = _early_stream(stream)
+    code = _call.paged_append(h, h.cfg_at, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, st) if st is not None else None
+    if code is None:   # not all plain tensors of the right kind, or the first call
+        kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
+        k, ks, n = _tokens(h, k_new, h.cfg.n_kv_heads, None, "k_new")
+        v, vs, _ = _tokens(h, v_new, h.cfg.n_kv_heads, n, "v_new")
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        qp = qo = None
+        qs = 0
+        if q is not None:
+            qp, qs, _ = _tokens(h, q, h.cfg.n_q_heads, n, "q")
+            qo = _whole(q_out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "q_out")
+        pos = None if positions is None else _whole(positions, torch.int32, (n, max(h.cfg.rot_axes, 1)), "positions")
+        start, length, tab, width, seqs = _batch(seq_start, seq_len, table)
+        code = lib().lvr_paged_append(h, kp, vp, k, v, qp, qo, (C.c_int64 * 3)(ks, vs, qs), pos, start, length, tab, width, seqs, n,
+                                      _stream(stream))
+    if code != LVR_OK:
+        raise LouverError(code, "lvr_paged_append")
 
 
 def lvr_paged_attention(h, k_pages, v_pages, q, seq_start, seq_len, table, out, window=0, stream=None) -> None:
     """q [n_tokens][n_q_heads][128], out the same and contiguous; seq_start, seq_len, table: int32."""
-    kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
-    qp, qs = _tokens(h, q, h.cfg.n_q_heads, None, "q")
-    n = q.shape[0]
-    o = _whole(out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "out")
-    start, length, tab, width, seqs = _batch(seq_start, seq_len, table)
-    _check(lib().lvr_paged_attention(h, kp, vp, qp, qs, start, length, tab, width, seqs, n, int(window), o, _stream(stream)),
-           "lvr_paged_attention")
+    st = _early_stream(stream)
+    code = _call.paged_attention(h, h.cfg_at, k_pages, v_pages, q, seq_start, seq_len, table, out, window, st) if st is not None else None
+    if code is None:   # not all plain tensors of the right kind, or the first call
+        kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
+        qp, qs, n = _tokens(h, q, h.cfg.n_q_heads, None, "q")
+        o = _whole(out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "out")
+        start, length, tab, width, seqs = _batch(seq_start, seq_len, table)
+        if not 0 <= int(window) < 1 << 31:
+            raise ValueError("window must be 0 (all keys) or a number of keys below 2^31")
+        code = lib().lvr_paged_attention(h, kp, vp, qp, qs, start, length, tab, width, seqs, n, int(window), o, _stream(stream))
+    if code != LVR_OK:
+        raise LouverError(code, "lvr_paged_attention")
 
 
 def lvr_paged_gather(h, k_pages, v_pages, seq_len, table, K_out, V_out, stream=None) -> None:
     """K_out, V_out: contiguous device tensors [n_seqs][n_kv_heads][n][128]; rows past a sequence's end stay as they are."""
-    kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
-    _, length, tab, width, seqs = _batch(None, seq_len, table)
-    if K_out.dim() != 4:
-        raise ValueError("K_out must be [n_seqs][n_kv_heads][n][head_dim]")
-    n = K_out.shape[2]
-    shape = (seqs, h.cfg.n_kv_heads, n, h.cfg.head_dim)
-    ko, vo = _whole(K_out, h.dtype, shape, "K_out"), _whole(V_out, h.dtype, shape, "V_out")
-    _check(lib().lvr_paged_gather(h, kp, vp, length, tab, width, seqs, n, ko, vo, _stream(stream)), "lvr_paged_gather")
+    st = _early_stream(stream)
+    code = _call.paged_gather(h, h.cfg_at, k_pages, v_pages, seq_len, table, K_out, V_out, st) if st is not None else None
+    if code is None:   # not all plain tensors of the right kind, or the first call
+        kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
+        _, length, tab, width, seqs = _batch(None, seq_len, table)
+        K = _tensor(K_out, "K_out")
+        if K.dim() != 4:
+            raise ValueError("K_out must be [n_seqs][n_kv_heads][n][head_dim]")
+        n = K.shape[2]
+        shape = (seqs, h.cfg.n_kv_heads, n, h.cfg.head_dim)
+        ko, vo = _whole(K, h.dtype, shape, "K_out"), _whole(V_out, h.dtype, shape, "V_out")
+        code = lib().lvr_paged_gather(h, kp, vp, length, tab, width, seqs, n, ko, vo, _stream(stream))
+    if code != LVR_OK:
+        raise LouverError(code, "lvr_paged_gather")

@@ -84,6 +84,9 @@ struct {
     decltype(&lvr_sparse_attention) sparse_attention;
     decltype(&lvr_sparse_attention_static) sparse_attention_static;
     decltype(&lvr_dense_attention) dense_attention;
+    decltype(&lvr_paged_append) paged_append;
+    decltype(&lvr_paged_attention) paged_attention;
+    decltype(&lvr_paged_gather) paged_gather;
 } lib;
 
 // Runs `call` (which returns an error code) without the GIL.
@@ -97,9 +100,9 @@ PyObject *result_of(F call) {
 }
 
 #define LVR_NOT_PLAIN(COND) do { if (!(COND)) Py_RETURN_NONE; } while (0)
-#define LVR_PLAIN(BODY)                             \
+#define LVR_PLAIN(...)                              \
     try {                                           \
-        BODY                                        \
+        __VA_ARGS__                                 \
     } catch (...) {   /* a tensor without memory */ \
         PyErr_Clear();                              \
         Py_RETURN_NONE;                             \
@@ -190,6 +193,128 @@ PyObject *sparse_attention_static(PyObject *, PyObject *const *a, Py_ssize_t n) 
     });
 }
 
+// ---- the paged cache.  What binding.py checks, with the same outcome: anything else goes there and is refused.
+
+const at::Tensor *device_tensor(PyObject *o, int type) {
+    if (PyObject_TypeCheck(o, &ArgType)) o = reinterpret_cast<Arg *>(o)->tensor;
+    if (!o || !THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && (int)t.scalar_type() == type ? &t : nullptr;
+}
+
+struct Paged {
+    lvr_paged *h;
+    const lvr_paged_config *c;
+    void *stream;
+    int type;
+    void *k_pages, *v_pages, *start, *len, *table;
+    int64_t width, seqs;
+
+    bool pool(PyObject *o, void *&p) const {   // [page][head][token][head_dim], or token before head
+        const at::Tensor *t = device_tensor(o, type);
+        if (!t || t->dim() != 4 || t->stride(3) != 1 || t->size(0) != c->n_pages || t->size(3) != c->head_dim || t->stride(0) != c->page_strides[0])
+            return false;
+        const bool heads_first = t->size(1) == c->n_kv_heads && t->size(2) == c->page_size && t->stride(1) == c->page_strides[1] && t->stride(2) == c->page_strides[2];
+        const bool tokens_first = t->size(2) == c->n_kv_heads && t->size(1) == c->page_size && t->stride(2) == c->page_strides[1] && t->stride(1) == c->page_strides[2];
+        p = t->data_ptr();
+        return heads_first || tokens_first;
+    }
+    // rows of new tokens, a token's heads contiguous; n < 0: as many as there are
+    bool tokens(PyObject *o, int64_t heads, int64_t &n, void *&p, int64_t &stride) const {
+        const at::Tensor *t = device_tensor(o, type);
+        if (!t || t->dim() != 3 || t->size(1) != heads || t->size(2) != c->head_dim || (n >= 0 && t->size(0) != n)) return false;
+        n = t->size(0);
+        if (n > 0 && (t->stride(2) != 1 || (heads > 1 && t->stride(1) != c->head_dim))) return false;
+        stride = n > 1 ? t->stride(0) : heads * c->head_dim;
+        p = t->data_ptr();
+        return true;
+    }
+    bool whole(PyObject *o, int want, c10::IntArrayRef shape, void *&p) const {
+        const at::Tensor *t = device_tensor(o, want);
+        if (!t || t->sizes() != shape || !t->is_contiguous()) return false;
+        p = t->data_ptr();
+        return true;
+    }
+    bool batch(PyObject *o_start, PyObject *o_len, PyObject *o_table) {
+        const at::Tensor *t = device_tensor(o_table, (int)at::kInt);
+        if (!t || t->dim() != 2 || !t->is_contiguous()) return false;
+        seqs = t->size(0);
+        width = t->size(1);
+        table = t->data_ptr();
+        start = nullptr;
+        return whole(o_len, (int)at::kInt, {seqs}, len) && (!o_start || whole(o_start, (int)at::kInt, {seqs + 1}, start));
+    }
+    // (h, address of its configuration, ..., stream)
+    bool begin(PyObject *o_h, PyObject *o_cfg, PyObject *o_stream) {
+        void *hp;
+        if (!address(o_h, hp) || !PyLong_CheckExact(o_cfg) || !address(o_stream, stream)) return false;
+        h = static_cast<lvr_paged *>(hp);
+        c = static_cast<const lvr_paged_config *>(PyLong_AsVoidPtr(o_cfg));
+        if (!c || PyErr_Occurred()) {
+            PyErr_Clear();
+            return false;
+        }
+        type = (int)(c->kv_dtype == LVR_BF16 ? at::kBFloat16 : at::kFloat);
+        return true;
+    }
+};
+
+// (h, cfg, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, stream)
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    Paged p;
+    void *k, *v, *q = nullptr, *q_out = nullptr, *pos = nullptr;
+    int64_t tokens = -1, strides[3] = {0, 0, 0};
+    LVR_PLAIN(
+        LVR_NOT_PLAIN(n == 13 && lib.paged_append && p.begin(a[0], a[1], a[12]) && p.pool(a[2], p.k_pages) && p.pool(a[3], p.v_pages) &&
+                      p.tokens(a[4], p.c->n_kv_heads, tokens, k, strides[0]) && p.tokens(a[5], p.c->n_kv_heads, tokens, v, strides[1]) &&
+                      p.batch(a[6], a[7], a[8]) && (a[9] == Py_None) == (a[10] == Py_None));
+        if (a[9] != Py_None)
+            LVR_NOT_PLAIN(p.tokens(a[9], p.c->n_q_heads, tokens, q, strides[2]) &&
+                          p.whole(a[10], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, q_out));
+        if (a[11] != Py_None) LVR_NOT_PLAIN(p.whole(a[11], I32, {tokens, (int64_t)(p.c->rot_axes > 1 ? p.c->rot_axes : 1)}, pos));)
+    return result_of([&] {
+        return lib.paged_append(p.h, p.k_pages, p.v_pages, k, v, q, q_out, strides, (const int32_t *)pos, (const int32_t *)p.start,
+                                (const int32_t *)p.len, (const int32_t *)p.table, p.width, p.seqs, tokens, p.stream);
+    });
+}
+
+// (h, cfg, k_pages, v_pages, q, seq_start, seq_len, table, out, window, stream)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    Paged p;
+    void *q, *out;
+    int64_t tokens = -1, stride;
+    long window = 0;
+    LVR_PLAIN(
+        LVR_NOT_PLAIN(n == 11 && lib.paged_attention && p.begin(a[0], a[1], a[10]) && p.pool(a[2], p.k_pages) && p.pool(a[3], p.v_pages) &&
+                      p.tokens(a[4], p.c->n_q_heads, tokens, q, stride) && p.batch(a[5], a[6], a[7]) &&
+                      p.whole(a[8], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, out) && PyLong_CheckExact(a[9]));
+        window = PyLong_AsLong(a[9]);
+        if (PyErr_Occurred()) PyErr_Clear(), window = -1;
+        LVR_NOT_PLAIN(window >= 0 && window <= INT32_MAX);)
+    return result_of([&] {
+        return lib.paged_attention(p.h, p.k_pages, p.v_pages, q, stride, (const int32_t *)p.start, (const int32_t *)p.len, (const int32_t *)p.table,
+                                   p.width, p.seqs, tokens, (int32_t)window, out, p.stream);
+    });
+}
+
+// (h, cfg, k_pages, v_pages, seq_len, table, K_out, V_out, stream)
+PyObject *paged_gather(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    Paged p;
+    void *K, *V;
+    int64_t rows = 0;
+    LVR_PLAIN(
+        LVR_NOT_PLAIN(n == 9 && lib.paged_gather && p.begin(a[0], a[1], a[8]) && p.pool(a[2], p.k_pages) && p.pool(a[3], p.v_pages) &&
+                      p.batch(nullptr, a[4], a[5]));
+        const at::Tensor *t = device_tensor(a[6], p.type);
+        LVR_NOT_PLAIN(t && t->dim() == 4);
+        rows = t->size(2);
+        const int64_t shape[4] = {p.seqs, p.c->n_kv_heads, rows, p.c->head_dim};
+        LVR_NOT_PLAIN(p.whole(a[6], p.type, shape, K) && p.whole(a[7], p.type, shape, V));)
+    return result_of([&] {
+        return lib.paged_gather(p.h, p.k_pages, p.v_pages, (const int32_t *)p.len, (const int32_t *)p.table, p.width, p.seqs, rows, K, V, p.stream);
+    });
+}
+
 // bind(name, address): the library's function of that name
 PyObject *bind(PyObject *, PyObject *args) {
     const char *name;
@@ -198,7 +323,9 @@ PyObject *bind(PyObject *, PyObject *args) {
     struct { const char *name; void **slot; } all[] = {
         {"lvr_decode_step", (void **)&lib.decode_step}, {"lvr_append_decode_step", (void **)&lib.append_decode_step},
         {"lvr_query", (void **)&lib.query}, {"lvr_sparse_attention", (void **)&lib.sparse_attention},
-        {"lvr_sparse_attention_static", (void **)&lib.sparse_attention_static}, {"lvr_dense_attention", (void **)&lib.dense_attention}};
+        {"lvr_sparse_attention_static", (void **)&lib.sparse_attention_static}, {"lvr_dense_attention", (void **)&lib.dense_attention},
+        {"lvr_paged_append", (void **)&lib.paged_append}, {"lvr_paged_attention", (void **)&lib.paged_attention},
+        {"lvr_paged_gather", (void **)&lib.paged_gather}};
     for (auto &f : all)
         if (!strcmp(f.name, name)) {
             *f.slot = (void *)(uintptr_t)at;
@@ -280,6 +407,9 @@ PyMethodDef methods[] = {{"decode_step", (PyCFunction)(void (*)())decode_step, M
                          {"sparse_attention", (PyCFunction)(void (*)())sparse_attention, METH_FASTCALL, nullptr},
                          {"sparse_attention_static", (PyCFunction)(void (*)())sparse_attention_static, METH_FASTCALL, nullptr},
                          {"dense_attention", (PyCFunction)(void (*)())dense_attention, METH_FASTCALL, nullptr},
+                         {"paged_append", (PyCFunction)(void (*)())paged_append, METH_FASTCALL, nullptr},
+                         {"paged_attention", (PyCFunction)(void (*)())paged_attention, METH_FASTCALL, nullptr},
+                         {"paged_gather", (PyCFunction)(void (*)())paged_gather, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 

@@ -413,7 +413,7 @@ def test_calls_refuse_what_they_cannot_take():
             for bad in (dict(seq_start=start[:-1]), dict(seq_start=start.float()), dict(q=q[:, :4]), dict(q=q.float()), dict(q=q.transpose(0, 1)), dict(q=q[..., ::2])):
                 with pytest.raises(ValueError):
                     call(**bad)
-        for bad in (dict(out=out[:1]), dict(out=out.float()), dict(out=out.cpu())):
+        for bad in (dict(out=out[:1]), dict(out=out.float()), dict(out=out.cpu()), dict(window=-1), dict(window=1 << 31), dict(window=1 << 70)):
             with pytest.raises(ValueError):
                 attend(**bad)
         for bad in (dict(q=None), dict(q_out=None), dict(v_new=k[:1]), dict(k_new=k[:, :1]), dict(positions=torch.zeros(c.T, 2, dtype=torch.int32, device="cuda")),
@@ -449,6 +449,29 @@ def test_calls_refuse_what_they_cannot_take():
             assert gat(**kw) == L.LVR_E_INVALID, kw
         assert gat(n=(1 << 30) + 1) == L.LVR_E_CAPACITY and gat(n=0, K1=None) == L.LVR_OK
         torch.cuda.synchronize()
+
+
+def test_marshalled_arguments_and_plain_ones_give_the_same(monkeypatch):
+    """Tensors, tensors marshalled once, and the general binding without the compiled calls."""
+    f = freqs(64)
+    with Cache([(5, 40), (1, 20)], rot_dim=64, inv_freq=f, seed=42) as c:
+        results = []
+        for way in ("tensors", "arguments", "general"):
+            A = L.tensor_arg if way == "arguments" else (lambda t: t)
+            if way == "general":
+                monkeypatch.setattr(L.binding, "_call", None)
+            kp, vp = c.pools()
+            g = torch.Generator().manual_seed(1)
+            q, k, v = (torch.randn(c.T, n, D, generator=g).to(c.dt).cuda() for n in (c.hq, c.hkv, c.hkv))
+            start, length, table = (A(x) for x in c.batch())
+            qo, out = torch.zeros_like(q), torch.zeros_like(q)
+            K, V = (torch.zeros(2, c.hkv, 40, D, dtype=c.dt, device="cuda") for _ in range(2))
+            L.lvr_paged_append(c.h, A(kp), A(vp), A(k), A(v), start, length, table, q=A(q), q_out=A(qo))
+            L.lvr_paged_attention(c.h, A(kp), A(vp), A(qo), start, length, table, A(out), window=30)
+            L.lvr_paged_gather(c.h, A(kp), A(vp), length, table, A(K), A(V))
+            results.append([x.clone() for x in (kp, vp, qo, out, K, V)])
+        for other in results[1:]:
+            assert all(torch.equal(x, y) for x, y in zip(results[0], other))
 
 
 def test_empty_batches():
