@@ -16,7 +16,7 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
 // Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.
-constexpr int ROWS16_PIECES = 768, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 512;
+constexpr int ROWS16_PIECES = 512, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 512;
 constexpr int MIN_RUN = 256, MAX_RUNS = 512;
 // Rows of a sequence up to which it is taken in tiles of 16.  A wave of a 128-row tile works on 32 of them however many there are, and on
 // fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 57 in a tile of 128 / 46 in four of 16,
@@ -40,6 +40,8 @@ struct AttnArgs {
     char *out;
     int64_t q_stride;    // bytes per token
     int32_t n_kv, G, window;
+    uint32_t g_mul;      // row / G = row * g_mul >> g_shift
+    int32_t g_shift;
     float unit;          // sigma * log2 e
     int32_t narrow;      // rows of a sequence up to which it is taken in tiles of 16
     int32_t target;      // pieces of work to make of the batch per KV head; 0: tiles are not cut
@@ -59,11 +61,33 @@ struct Tile {
     int slot;                  // where its partial result goes, if there is more than one run
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_or_zero(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
 }
+__device__ __forceinline__ float wave_sum(float v) {   // as lvr_wave_inclusive_sum; every lane gets the total
+    v += dpp_or_zero<0x111, 0xf>(v);
+    v += dpp_or_zero<0x112, 0xf>(v);
+    v += dpp_or_zero<0x114, 0xf>(v);
+    v += dpp_or_zero<0x118, 0xf>(v);
+    v += dpp_or_zero<0x142, 0xa>(v);
+    v += dpp_or_zero<0x143, 0xc>(v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// The division of the batch stands before everything else a workgroup does, in code that is fetched anew by every launch: it is
+// kept short.  a / b is a handful of instructions less where it may be off by one,
+__device__ __forceinline__ int about(int a, int b) { return (int)((float)a * __builtin_amdgcn_rcpf((float)b)); }
+// for quotients below 2^21 one comparison either way puts that right,
+__device__ __forceinline__ int divide_small(int a, int b) {
+    int q = about(a, b);
+    const int r = a - q * b;
+    q += r >= b;
+    q -= r < 0;
+    return q;
+}
+// and for the query heads of a KV head the host has the reciprocal (rows are fewer than 2^28).
+__device__ __forceinline__ int token_of(const AttnArgs &a, int row) { return (int)((uint64_t)(uint32_t)row * a.g_mul >> a.g_shift); }
 
 // How a batch is divided into pieces, for one KV head.  The host knows neither how many tokens a sequence brings nor how many keys it
 // holds, so every workgroup works it out for itself, each wave on its own, a lane to a sequence (64 at a time).  MIXED: sequences of
@@ -78,8 +102,10 @@ __device__ __forceinline__ float wave_sum(float v) {
 // be more, L grows until there are not.
 template <bool MIXED>
 struct Division {
+    const AttnArgs &a;
     const lvr_paged_batch &b;
-    int G, window, narrow, L, n_wide;              // pieces of 128-row tiles, which come first
+    int G, window, narrow, L;
+    int n_wide;                              // pieces of 128-row tiles, which come first
     bool any_wide;
     int s0, s1, n, tiles, span, run, runs;   // this lane's sequence
 
@@ -95,7 +121,7 @@ struct Division {
             n = n < 0 ? 0 : (n > 1 << 30 ? 1 << 30 : n);
             const int rows = (s1 - s0) * G;
             tiles = wide(rows) ? (rows + 127) / 128 : (rows + 15) / 16;
-            const int reach = window ? window + (wide(rows) ? 128 : 16) / G + 2 : n;   // keys a tile can see
+            const int reach = window ? window + 128 : n;   // keys a tile can see, at most
             span = n < reach ? n : reach;
             if (span < 1) span = 1;
         }
@@ -108,12 +134,16 @@ struct Division {
             if (L1 < least) L1 = least;
         }
         if (MIXED && any_wide && !is_wide()) L1 = L1 > 4 * MIN_RUN ? L1 >> 2 : (L1 < MIN_RUN ? L1 : MIN_RUN);
-        runs = (span + (MIXED && is_wide() ? L1 >> 1 : L1 - 1)) / L1;
-        if (runs < 1) runs = 1;
-        run = ((span + runs - 1) / runs + 63) & ~63;
-        runs = (span + run - 1) / run;
+        if (MIXED) {
+            runs = about(span + (is_wide() ? L1 >> 1 : L1 - 1), L1);
+            if (runs < 1) runs = 1;
+        } else {   // rounded up, and never more than that
+            runs = about(span - 1, L1) + 1;
+            runs -= (runs - 1) * L1 >= span;
+        }
+        run = (about(span, runs) + 64) & ~63;   // the last run takes what is left, whatever was rounded
     }
-    __device__ __forceinline__ Division(const AttnArgs &a, const lvr_paged_batch &bt) : b(bt), G(a.G), window(a.window), narrow(a.narrow) {}
+    __device__ __forceinline__ Division(const AttnArgs &args, const lvr_paged_batch &bt) : a(args), b(bt), G(a.G), window(a.window), narrow(a.narrow) {}
     // false: seq_start is not ascending, no piece is where another expects it
     __device__ __forceinline__ bool divide(int target) {
         float keys = 0.f, tokens = 0.f;
@@ -136,6 +166,11 @@ struct Division {
             const float want = keys * 1.001f / (float)target;   // (more than what the sum was rounded by)
             L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? 1 << 30 : ((int)want + 63) & ~63);
         }
+        if (!MIXED) {   // at most target pieces more than tiles, and at most 2 * target of cut tiles, since L is all keys over target
+            n_wide = 0;
+            if (b.n_seqs <= 64) cut();
+            return true;
+        }
         for (;; L = L < 1 << 28 ? (L + L / 2) & ~63 : 1 << 30) {
             int cut_wide = 0, cut_narrow = 0;
             n_wide = 0;
@@ -143,10 +178,8 @@ struct Division {
                 if (b.n_seqs > 64) look(i0 + lvr_lane());
                 cut();
                 const int cut_here = runs > 1 ? tiles * runs : 0;
-                if (MIXED) {
-                    n_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? tiles * runs : 0), 63);
-                    cut_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? cut_here : 0), 63);
-                }
+                n_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? tiles * runs : 0), 63);
+                cut_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? cut_here : 0), 63);
                 cut_narrow += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? 0 : cut_here), 63);
             }
             if ((cut_wide <= 2 * target && cut_wide + cut_narrow <= 3 * target) || L == 1 << 30) break;
@@ -175,9 +208,10 @@ struct Division {
                 auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
                 const int seq_runs = of(runs), seq_run = of(run);
                 const int k = (x - of(upto - count)) * (CUT ? seq_runs : 1);   // which of the sequence's pieces
-                const int tile = of(tiles) - 1 - k / seq_runs;
+                const int from_last = seq_runs == 1 ? k : divide_small(k, seq_runs);
+                const int tile = of(tiles) - 1 - from_last;
                 t.slot = of(cut_upto - of_cut) + k;
-                t.split = k % seq_runs;
+                t.split = k - from_last * seq_runs;
                 t.seq = i0 + at;
                 const int first = of(s0), tokens = of(s1) - first;
                 t.first_token = first;
@@ -186,14 +220,14 @@ struct Division {
                 t.row0 = tile * t.height;
                 t.pos0 = of(n) - tokens;
                 const int last_row = (t.row0 + t.height < t.rows ? t.row0 + t.height : t.rows) - 1;
-                t.hi = t.pos0 + last_row / G + 1;
+                t.hi = t.pos0 + token_of(a, last_row) + 1;
                 if (t.hi > b.table_width << b.page_shift) t.hi = b.table_width << b.page_shift;
-                t.lo = window ? t.pos0 + t.row0 / G - window + 1 : 0;
+                t.lo = window ? t.pos0 + token_of(a, t.row0) - window + 1 : 0;
                 if (t.lo < 0) t.lo = 0;
                 const int from = t.lo & ~63;
                 t.splits = 1;
                 if (seq_runs > 1 && t.hi > from) {
-                    t.splits = (t.hi - from - 1) / seq_run + 1;
+                    t.splits = about(t.hi - from - 1, seq_run) + 1;   // the same for all pieces of the tile
                     if (t.splits > seq_runs) t.splits = seq_runs;
                 }
                 if (t.split >= t.splits) return false;   // a run past what this tile sees
@@ -244,7 +278,7 @@ __device__ __forceinline__ float2 load_shared(const float *p) {
 // Where a packed row's output lies.
 template <int ELT>
 __device__ __forceinline__ char *output_row(const AttnArgs &a, const Tile &t, int kvh, int row) {
-    const int token = row / a.G, head = kvh * a.G + row - token * a.G;
+    const int token = token_of(a, row), head = kvh * a.G + row - token * a.G;
     return a.out + ((int64_t)(t.first_token + token) * a.n_kv * a.G + head) * LVR_D * ELT;
 }
 template <int ELT>
@@ -266,7 +300,7 @@ struct RowSum {
 };
 template <int ELT>
 __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, int kvh, int row, int k0, int run, int step) {
-    const int lane = lvr_lane(), token = row / a.G, head = kvh * a.G + row - token * a.G;
+    const int lane = lvr_lane(), token = token_of(a, row), head = kvh * a.G + row - token * a.G;
     const int last = t.pos0 + token, first = a.window && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
     auto pair = [&](const char *r) {
         if constexpr (ELT == 2) {
@@ -428,14 +462,14 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     const int lane = lvr_lane(), i = lane & 15, b = lane >> 4;
 
     const int row = t.row0 + i;                      // this lane's query row (column i of the score tiles)
-    const int token = row / a.G, head = kvh * a.G + row - token * a.G;
+    const int token = token_of(a, row), head = kvh * a.G + row - token * a.G;
     const bool has_row = row < t.rows;
     typename R::Q q;
     R::load_q(has_row ? a.q + (int64_t)(t.first_token + token) * a.q_stride + (int64_t)head * LVR_D * R::ELT : nullptr, b, q);
     const int last = t.pos0 + token;                 // keys this row sees: first .. last
     const int first = a.window && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
-    const int row_end = t.pos0 + t.row0 / a.G + 1;   // keys before it, from row_begin on, are seen by every row of the tile
-    const int last_pos = t.pos0 + ((t.row0 + 15 < t.rows ? t.row0 + 15 : t.rows - 1) / a.G);
+    const int row_end = t.pos0 + token_of(a, t.row0) + 1;   // keys before it, from row_begin on, are seen by every row of the tile
+    const int last_pos = t.pos0 + token_of(a, t.row0 + 15 < t.rows ? t.row0 + 15 : t.rows - 1);
     const int row_begin = a.window && last_pos - a.window + 1 > 0 ? last_pos - a.window + 1 : 0;
 
     bool redo = false;
@@ -729,14 +763,14 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
     const int lane = lvr_lane(), n = lane & 31, h = lane >> 5;
 
     const int row0 = t.row0 + wave * 32, row = row0 + n;
-    const int token = row / a.G, head = kvh * a.G + row - token * a.G;
+    const int token = token_of(a, row), head = kvh * a.G + row - token * a.G;
     const bool has_row = row < t.rows;
     typename R::Q q;
     R::load_q(has_row ? a.q + (int64_t)(t.first_token + token) * a.q_stride + (int64_t)head * LVR_D * R::ELT : nullptr, h, q);
     const int last = t.pos0 + token;                 // keys this row sees: first .. last
     const int first = a.window && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
     // some of the wave's rows see wlo .. whi - 1, all of them all_lo .. all_hi - 1
-    const int wfirst = t.pos0 + row0 / a.G, wlast = t.pos0 + (row0 + 31 < t.rows ? row0 + 31 : t.rows - 1) / a.G;
+    const int wfirst = t.pos0 + token_of(a, row0), wlast = t.pos0 + token_of(a, row0 + 31 < t.rows ? row0 + 31 : t.rows - 1);
     const int whi = row0 < t.rows ? wlast + 1 : 0, wlo = a.window ? wfirst - a.window + 1 : 0;
     const int all_hi = wfirst + 1, all_lo = a.window ? wlast - a.window + 1 : 0;
 
@@ -879,24 +913,32 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
     }
 }
 
+// Launches are n_kv x pieces workgroups: those of a KV head follow each other on one die where there are eight of them (a die has its
+// own cache, and workgroups go to the eight dies in turn).
+constexpr int GRID_Y = 32768;
+__device__ __forceinline__ int piece_of_block() { return blockIdx.z * GRID_Y + blockIdx.y; }
+inline dim3 grid_of(int n_kv, int64_t pieces) {
+    return dim3((unsigned)n_kv, (unsigned)(pieces < GRID_Y ? pieces : GRID_Y), (unsigned)((pieces + GRID_Y - 1) / GRID_Y));
+}
+
 // Tiles of 16 rows alone: batches in which every sequence brings a token or so.
 template <typename KT>
 __global__ void __launch_bounds__(256, 2) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
     __shared__ Rows16Lds lds;
-    const int kvh = blockIdx.x % a.n_kv;
+    const int kvh = blockIdx.x;
     Tile t;
     Division<false> d(a, bt);
-    if (d.divide(a.target) && d.template locate<false>(blockIdx.x / a.n_kv, t)) rows16_piece<KT>(a, bt, t, kvh, lds);
+    if (d.divide(a.target) && d.template locate<false>(piece_of_block(), t)) rows16_piece<KT>(a, bt, t, kvh, lds);
 }
 
 // Any batch: every sequence in the tiles that suit it.
 template <typename KT>
 __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs a, lvr_paged_batch bt) {
     __shared__ union { Rows16Lds narrow; Rows128Lds<KT> wide; } lds;
-    const int kvh = blockIdx.x % a.n_kv;
+    const int kvh = blockIdx.x;
     Tile t;
     Division<true> d(a, bt);
-    if (!d.divide(a.target) || !d.template locate<false>(blockIdx.x / a.n_kv, t)) return;
+    if (!d.divide(a.target) || !d.template locate<false>(piece_of_block(), t)) return;
     if (t.height == 128) rows128_piece<KT>(a, bt, t, kvh, lds.wide);
     else rows16_piece<KT>(a, bt, t, kvh, lds.narrow);
 }
@@ -947,7 +989,10 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.q_stride = q_stride_bytes;
     a.n_kv = pc->cfg.n_kv_heads;
     a.G = pc->cfg.n_q_heads / pc->cfg.n_kv_heads;
-    a.window = window;
+    a.window = window < 1 << 30 ? window : 0;   // no sequence is longer
+    a.g_shift = 28;
+    while (1 << (a.g_shift - 28) < a.G) ++a.g_shift;
+    a.g_mul = (uint32_t)((((uint64_t)1 << a.g_shift) + a.G - 1) / a.G);
     a.unit = pc->sigma * LOG2E;
     a.part = pc->part;
     a.ticket = pc->ticket;
@@ -956,7 +1001,7 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.narrow = bf16 ? NARROW_BF16 : NARROW_F32;
     if (b.n_tokens <= b.n_seqs || rows <= a.narrow) {
         a.target = (b.n_seqs * a.n_kv <= 32 ? ROWS16_PIECES_FEW : ROWS16_PIECES) / a.n_kv;   // n_kv is at most 256
-        const dim3 grid((unsigned)((rows / 16 + b.n_seqs + a.target) * a.n_kv));
+        const dim3 grid = grid_of(a.n_kv, rows / 16 + b.n_seqs + a.target);
         if (bf16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
         else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
         return hipGetLastError();
@@ -965,7 +1010,7 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     // tiles enough to fill the device without cuts, or none longer than the shortest run
     if (rows / 128 * a.n_kv >= 8 * MIXED_PIECES || b.table_width <= MIN_RUN >> b.page_shift) a.target = 0;
     // tiles: a sequence's rows over 128 and one more, or at most narrow / 16
-    const dim3 grid((unsigned)((rows / 128 + (int64_t)(a.narrow / 16) * b.n_seqs + 3 * a.target) * a.n_kv));
+    const dim3 grid = grid_of(a.n_kv, rows / 128 + (int64_t)(a.narrow / 16) * b.n_seqs + 3 * a.target);
     if (bf16) hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
     else hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
     if (a.target > 0) {
