@@ -24,7 +24,7 @@ constexpr int MIN_RUN = 256, MAX_RUNS = 512;
 constexpr int NARROW_BF16 = 32, NARROW_F32 = 64;
 constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);
 constexpr int MERGE_WGS = 1024;
-constexpr int FAN = 8;        // partial results of 16-row tiles merged at a time
+constexpr int FAN = 8;        // partial results of 16-row tiles that a wave merges at a time
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -559,21 +559,25 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     const int r = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 8;
     const bool writes = t.row0 + r < t.rows;
     Merged x;
-    x.clear();
+    auto from_lds = [&](int n) {   // the sums of n sets of keys
+        x.clear();
+        for (int w = 0; w < n; ++w) {
+            float v[8];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = lds.o[w][r][c0 + e];
-        x.add(lds.m[w][r], lds.l[w][r], v);
-    }
+            for (int e = 0; e < 8; ++e) v[e] = lds.o[w][r][c0 + e];
+            x.add(lds.m[w][r], lds.l[w][r], v);
+        }
+    };
+    from_lds(4);
     if (t.splits > 1) {
-        // The last workgroup to end of every FAN of a tile's runs merges those, and the last of these merges what they made: one
-        // compute unit reads some 30 GB/s, so nobody is left with all of them.  Partials cross from one die to another: they are
-        // stored and read with accesses of device scope, and a workgroup waits for its own stores before it takes a ticket, which
-        // wraps at the number of those who take it and so is zero again afterwards.
-        const int slot0 = t.slot - t.split, fans = (t.splits + FAN - 1) / FAN, fan = t.split / FAN;
-        const int in_fan = fan + 1 < fans ? FAN : t.splits - fan * FAN;
+        // The last workgroup to end of every `fan` of a tile's runs merges those, and the last of these merges what they made: one
+        // compute unit reads some 30 GB/s, so nobody is left with all of them.  Four rows fill a wave, and where a tile has no
+        // more the waves share the partials out; each takes up to FAN of them with all their loads in flight.  Partials cross
+        // from one die to another: they are stored and read with accesses of device scope, and a workgroup waits for its own stores
+        // before it takes a ticket, which wraps at the number of those who take it and so is zero again afterwards.
+        const int rows = t.rows - t.row0, sharers = rows <= 4 ? 4 : (rows <= 8 ? 2 : 1), fan = FAN * sharers;
+        const int slot0 = t.slot - t.split, fans = (t.splits + fan - 1) / fan, mine = t.split / fan;
+        const int in_mine = mine + 1 < fans ? fan : t.splits - mine * fan;
         float *first_part = partial<16>(a.part, slot0, a.n_kv, kvh);
         const int64_t step = (int64_t)a.n_kv * (16 * (LVR_D + 2));
         auto put = [&](float *p) {
@@ -590,31 +594,41 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
             return lds.arrived == (unsigned)n - 1u;
         };
         auto merge = [&](const float *p, int64_t apart, int n) {
+            const int share = wave * sharers / 4, mr = (wave & (4 / sharers - 1)) * 4 + (lane >> 4);   // whose turn, which row
             x.clear();
-            for (int p0 = 0; p0 < n; p0 += FAN) {
+            for (int p0 = share; p0 < n; p0 += fan) {
                 float2 ml[FAN], v[FAN][4];
 #pragma unroll
-                for (int k = 0; k < FAN; ++k) {   // all in flight; past the last one the last once more
-                    const float *from = p + (p0 + k < n ? p0 + k : n - 1) * apart;
-                    ml[k] = load_shared(from + 16 * LVR_D + r * 2);
+                for (int k = 0; k < FAN; ++k) {   // past the last one the last once more
+                    const float *from = p + (p0 + k * sharers < n ? p0 + k * sharers : n - 1) * apart;
+                    ml[k] = load_shared(from + 16 * LVR_D + mr * 2);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[k][e] = load_shared(from + r * LVR_D + c0 + 2 * e);
+                    for (int e = 0; e < 4; ++e) v[k][e] = load_shared(from + mr * LVR_D + c0 + 2 * e);
                 }
 #pragma unroll
                 for (int k = 0; k < FAN; ++k) {
-                    if (p0 + k >= n) continue;
+                    if (p0 + k * sharers >= n || mr >= rows) continue;   // (rows that are none hold anything)
                     const float y[8] = {v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y, v[k][2].x, v[k][2].y, v[k][3].x, v[k][3].y};
                     x.add(ml[k].x, ml[k].y, y);
                 }
             }
+            if (sharers == 1) return;
+            if (c0 == 0) {
+                lds.m[share][mr] = x.m;
+                lds.l[share][mr] = x.l;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) lds.o[share][mr][c0 + e] = x.o[e];
+            __syncthreads();
+            from_lds(sharers);
         };
         put(first_part + t.split * step);
-        if (!last_of(slot0 + fan * FAN, 0, in_fan)) return;
-        merge(first_part + fan * FAN * step, step, in_fan);
+        if (!last_of(slot0 + mine * fan, 0, in_mine)) return;
+        merge(first_part + mine * fan * step, step, in_mine);
         if (fans > 1) {
-            put(first_part + fan * FAN * step);
+            put(first_part + mine * fan * step);
             if (!last_of(slot0, 1, fans)) return;
-            merge(first_part, FAN * step, fans);
+            merge(first_part, fan * step, fans);
         }
     }
     if (!writes) return;
