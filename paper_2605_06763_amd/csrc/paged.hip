@@ -19,6 +19,8 @@ namespace {
     } while (0)
 
 constexpr int PAIRS = LVR_D / 2;
+constexpr int64_t APPEND_MANY = 32768;        // rows of a call
+constexpr int64_t GATHER_STREAM = 4 << 20;   // bytes of each of K and V
 
 // sin and cos of a fraction of a turn, given in units of 2^-32.  The nearest quarter turn is split off exactly (integers), the
 // rest lies within an eighth of a turn, where the Taylor series to x^9 and x^10 are off by less than 2^-28.
@@ -36,32 +38,36 @@ __device__ __forceinline__ void sincos_turn(uint32_t phase, float &sn, float &cs
     if ((quarter + 1) & 2) cs = -cs;
 }
 
-// Eight elements of a row from element `at` on, as they are stored.
-__device__ __forceinline__ void load_raw8(const char *row, int at, lvr_raw8<lvr_bf16_t> &r) {
-    r.a = *reinterpret_cast<const uint4 *>(row + at * 2);
-}
-__device__ __forceinline__ void load_raw8(const char *row, int at, lvr_raw8<lvr_f32_t> &r) {
-    r.a = *reinterpret_cast<const float4 *>(row + at * 4);
-    r.b = *reinterpret_cast<const float4 *>(row + at * 4 + 16);
-}
-__device__ __forceinline__ void store_raw8(char *row, int at, const lvr_raw8<lvr_bf16_t> &r) {
-    *reinterpret_cast<uint4 *>(row + at * 2) = r.a;
-}
-__device__ __forceinline__ void store_raw8(char *row, int at, const lvr_raw8<lvr_f32_t> &r) {
-    *reinterpret_cast<float4 *>(row + at * 4) = r.a;
-    *reinterpret_cast<float4 *>(row + at * 4 + 16) = r.b;
+// 16 bytes of a row, as elements and back.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 load_piece(const char *p) { return *reinterpret_cast<const u32x4 *>(p); }
+// STREAM: past the caches, which the rows would only pass through
+template <bool STREAM>
+__device__ __forceinline__ void store_piece(char *p, u32x4 v) {
+    if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+    else *reinterpret_cast<u32x4 *>(p) = v;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const bf16x2 v = {(__bf16)lo, (__bf16)hi};   // rounds to nearest even, NaN stays NaN
     return __builtin_bit_cast(uint32_t, v);
 }
-__device__ __forceinline__ void pack8(const float (&x)[8], lvr_raw8<lvr_bf16_t> &r) {
-    r.a = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+__device__ __forceinline__ void elements(u32x4 r, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = lvr_bf16_lo(r[i]);
+        x[2 * i + 1] = lvr_bf16_hi(r[i]);
+    }
 }
-__device__ __forceinline__ void pack8(const float (&x)[8], lvr_raw8<lvr_f32_t> &r) {
-    r.a = make_float4(x[0], x[1], x[2], x[3]);
-    r.b = make_float4(x[4], x[5], x[6], x[7]);
+__device__ __forceinline__ void elements(u32x4 r, float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ u32x4 piece_of(const float (&x)[8]) {
+    return u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+}
+__device__ __forceinline__ u32x4 piece_of(const float (&x)[4]) {
+    return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
 }
 
 struct AppendArgs {
@@ -71,82 +77,102 @@ struct AppendArgs {
     const int32_t *positions;
     const uint64_t *turns;
     const int32_t *axis;
-    int32_t n_kv, n_rows, chunks;           // rows of a token: n_kv of K, n_kv of V, then q's; chunks of eight rows
+    int32_t n_kv, n_rows, groups;           // rows of a token: n_kv of K, n_kv of V, then q's; waves to a token
     int32_t rot, axes;
 };
 
-// A wave takes eight rows of one token, eight lanes to a row.  A lane holds 16 elements in two runs of eight that are rotated with
-// each other (HALVES: the same run of both halves; NEIGHBOURS: 16 in a row), and so the sines and cosines of eight pairs; past
-// the rotated coordinates it copies 16 in a row.  The angle is position times turns per position modulo one turn, which in
-// 64-bit integers is one product with the overflow dropped: no far position loses anything.
-template <typename KT, bool NEIGHBOURS>
+// A wave takes PER times ROWS rows of one token.  A lane holds two pieces of a row, of E elements each: HALVES: the same one of both
+// halves, rotated with each other; NEIGHBOURS: one in each half of the row, rotated within themselves; past the rotated coordinates two that are
+// copied.  The lanes of a row touch neighbouring pieces in every access.  A lane needs the sines and cosines of E pairs, for all
+// of its rows.  The angle is position times turns per position modulo one turn, which in 64-bit integers is one product with the
+// overflow dropped: no far position loses anything.
+template <typename KT, bool NEIGHBOURS, int PER, bool STREAM>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_paged_batch b) {
+    constexpr int ELT = sizeof(KT) == 4 ? 4 : 2, E = 16 / ELT, LANES = PAIRS / E, ROWS = 64 / LANES;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lane = lvr_lane(), li = lane & 7;
+    const int lane = lvr_lane(), li = lane % LANES;
     const uint32_t w = blockIdx.x * 4u + wave;
-    const int t = (int)(w / (uint32_t)a.chunks), row = (int)(w % (uint32_t)a.chunks) * 8 + (lane >> 3);
+    const int t = (int)(w / (uint32_t)a.groups), row0 = (int)(w % (uint32_t)a.groups) * (ROWS * PER) + lane / LANES;
     if (t >= b.n_tokens) return;   // the whole wave
 
-    constexpr int ELT = sizeof(KT) == 4 ? 4 : 2;
-    const int half = a.rot / 2;
-    const bool rotates = li * 16 < a.rot && !(row >= a.n_kv && row < 2 * a.n_kv);
-    int at0 = li * 16, at1 = at0 + 8;
-    if (!NEIGHBOURS && li * 16 < a.rot) {
-        at0 = li * 8;
-        at1 = half + at0;
+    int at0 = E * li, at1 = PAIRS + E * li;
+    bool rot0 = at0 < a.rot, rot1 = at1 < a.rot;
+    if (!NEIGHBOURS) {
+        const int half = a.rot / 2, copied = li - half / E;
+        rot0 = rot1 = copied < 0;
+        at0 = rot0 ? E * li : a.rot + E * copied;
+        at1 = rot0 ? half + E * li : at0 + E * (LANES - half / E);
     }
-    const int head = row < a.n_kv ? row : (row < 2 * a.n_kv ? row - a.n_kv : row - 2 * a.n_kv);
-    const char *src = row < a.n_kv ? a.k + t * a.k_stride : (row < 2 * a.n_kv ? a.v + t * a.v_stride : a.q + t * a.q_stride);
-    lvr_raw8<KT> r0, r1;
-    if (row < a.n_rows) {
-        load_raw8(src + (int64_t)head * LVR_D * ELT, at0, r0);
-        load_raw8(src + (int64_t)head * LVR_D * ELT, at1, r1);
+    u32x4 r0[PER], r1[PER];
+#pragma unroll
+    for (int c = 0; c < PER; ++c) {
+        int row = row0 + c * ROWS;
+        if (row >= a.n_rows) row = a.n_rows - 1;   // nothing is made of it
+        const char *src = row < a.n_kv ? a.k + t * a.k_stride + (int64_t)row * (LVR_D * ELT)
+                          : row < 2 * a.n_kv ? a.v + t * a.v_stride + (int64_t)(row - a.n_kv) * (LVR_D * ELT)
+                                             : a.q + t * a.q_stride + (int64_t)(row - 2 * a.n_kv) * (LVR_D * ELT);
+        r0[c] = load_piece(src + at0 * ELT);
+        r1[c] = load_piece(src + at1 * ELT);
     }
 
     const int seq = lvr_seq_of(b, t);
-    if (seq < 0 || seq >= b.n_seqs || row >= a.n_rows) return;
+    if (seq < 0 || seq >= b.n_seqs) return;
     const int64_t slot = (int64_t)b.seq_len[seq] - b.seq_start[seq + 1] + t;
-    char *dst = nullptr;
-    if (row >= 2 * a.n_kv) {
-        dst = a.q_out + ((int64_t)t * (a.n_rows - 2 * a.n_kv) + head) * LVR_D * ELT;
-    } else {
-        const int page = lvr_page_of(b, seq, slot);
-        if (page >= 0) dst = (row < a.n_kv ? a.k_pages : a.v_pages) + lvr_row_at(b, page, head, slot);
-    }
-    if (!dst) return;
-
-    if (rotates) {
-        float x[8], y[8];
-        lvr_unpack(r0, x);
-        lvr_unpack(r1, y);
-        int pos[4];
+    const int page = lvr_page_of(b, seq, slot);
+    float sn[E], cs[E];
+    if (rot0 || rot1) {
+        int pos[4] = {(int)slot, (int)slot, (int)slot, (int)slot};
+        if (a.positions)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pos[i] = a.positions ? (i < a.axes ? a.positions[(int64_t)t * a.axes + i] : 0) : (int)slot;
+            for (int i = 0; i < 4; ++i) pos[i] = i < a.axes ? a.positions[(int64_t)t * a.axes + i] : 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int ax = a.axis[li * 8 + e];
-            const int p = ax < 2 ? (ax == 0 ? pos[0] : pos[1]) : (ax == 2 ? pos[2] : pos[3]);
-            float sn, cs;
-            sincos_turn((uint32_t)(((uint64_t)(int64_t)p * a.turns[li * 8 + e]) >> 32), sn, cs);
-            float &u = NEIGHBOURS ? (e < 4 ? x[2 * (e & 3)] : y[2 * (e & 3)]) : x[e];
-            float &z = NEIGHBOURS ? (e < 4 ? x[2 * (e & 3) + 1] : y[2 * (e & 3) + 1]) : y[e];
-            const float first = u * cs - z * sn, second = u * sn + z * cs;
-            u = first;
-            z = second;
+        for (int e = 0; e < E; ++e) {
+            const int pair = NEIGHBOURS ? (e < E / 2 ? 0 : PAIRS / 2 - E / 2) + E * li / 2 + e : E * li + e;
+            int p = pos[0];
+            if (a.axes > 1) {
+                const int ax = a.axis[pair];
+                p = ax < 2 ? (ax == 0 ? pos[0] : pos[1]) : (ax == 2 ? pos[2] : pos[3]);
+            }
+            // the upper half of the product's lower 64 bits
+            const uint32_t lo = (uint32_t)a.turns[pair], hi = (uint32_t)(a.turns[pair] >> 32);
+            sincos_turn((uint32_t)p * hi + __umulhi((uint32_t)p, lo) - (p < 0 ? lo : 0u), sn[e], cs[e]);
         }
-        pack8(x, r0);
-        pack8(y, r1);
     }
-    store_raw8(dst, at0, r0);
-    store_raw8(dst, at1, r1);
+#pragma unroll
+    for (int c = 0; c < PER; ++c) {
+        const int row = row0 + c * ROWS;
+        const bool of_q = row >= 2 * a.n_kv, of_v = row >= a.n_kv && !of_q;
+        if (row >= a.n_rows || (!of_q && page < 0)) continue;
+        if ((rot0 || rot1) && !of_v) {
+            float x[E], y[E];
+            elements(r0[c], x);
+            elements(r1[c], y);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool second = e >= E / 2;
+                float &u = NEIGHBOURS ? (second ? y : x)[2 * (e % (E / 2))] : x[e];
+                float &z = NEIGHBOURS ? (second ? y : x)[2 * (e % (E / 2)) + 1] : y[e];
+                const float first = u * cs[e] - z * sn[e];
+                z = u * sn[e] + z * cs[e];
+                u = first;
+            }
+            if (rot0) r0[c] = piece_of(x);
+            if (rot1) r1[c] = piece_of(y);
+        }
+        char *dst = of_q ? a.q_out + ((int64_t)t * (a.n_rows - 2 * a.n_kv) + row - 2 * a.n_kv) * (LVR_D * ELT)
+                         : (of_v ? a.v_pages : a.k_pages) + lvr_row_at(b, page, of_v ? row - a.n_kv : row, slot);
+        store_piece<STREAM>(dst + at0 * ELT, r0[c]);
+        store_piece<STREAM>(dst + at1 * ELT, r1[c]);
+    }
 }
 
-// A wave takes 16 rows of one head, which lie in one page: one table entry, then every row in one access of 16 lanes (fp32: two).
-template <typename KT>
+// A wave takes 16 rows of one head, which lie in one page: one table entry, then 64 pieces of 16 bytes to an access, one behind the other
+// where the rows are.
+template <typename KT, bool STREAM>
 __global__ void __launch_bounds__(256) paged_gather_kernel(const char *k_pages, const char *v_pages, char *K, char *V, int64_t n,
                                                            int32_t n_kv, lvr_paged_batch b) {
-    constexpr int ROW = LVR_D * (sizeof(KT) == 4 ? 4 : 2);
-    const int lane = lvr_lane(), sub = lane >> 4, li = lane & 15;
+    constexpr int ROW = LVR_D * (sizeof(KT) == 4 ? 4 : 2), LANES = ROW / 16, ROWS = 64 / LANES, N = 16 / ROWS;
+    const int lane = lvr_lane(), r0 = lane / LANES, at = lane % LANES * 16;
     const int64_t groups = (n + 15) / 16, total = groups * n_kv * b.n_seqs;
     const int64_t step = (int64_t)gridDim.x * 4;
     for (int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); w < total; w += step) {
@@ -158,21 +184,21 @@ __global__ void __launch_bounds__(256) paged_gather_kernel(const char *k_pages, 
         if (row0 >= end) continue;
         const int page = lvr_page_of(b, seq, row0);   // the table ends with a page, so all 16 rows are in it or none
         if (page < 0) continue;
-        const int64_t from = lvr_row_at(b, page, head, row0);
-        const int64_t to = (bh * n + row0) * ROW;
+        const int64_t from = lvr_row_at(b, page, head, row0) + at;
+        const int64_t to = (bh * n + row0) * ROW + at;
         const int last = (int)(end - row0 < 16 ? end - row0 : 16) - 1;
-        lvr_raw8<KT> k[4], v[4];
+        u32x4 k[N], v[N];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = i * 4 + sub < last ? i * 4 + sub : last;   // past the end: the last row once more
-            load_raw8(k_pages + from + r * b.row_stride, li * 8, k[i]);
-            load_raw8(v_pages + from + r * b.row_stride, li * 8, v[i]);
+        for (int i = 0; i < N; ++i) {
+            const int r = i * ROWS + r0 < last ? i * ROWS + r0 : last;   // past the end: the last row once more
+            k[i] = load_piece(k_pages + from + r * b.row_stride);
+            v[i] = load_piece(v_pages + from + r * b.row_stride);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i * 4 + sub <= last) {
-                store_raw8(K + to + (i * 4 + sub) * ROW, li * 8, k[i]);
-                store_raw8(V + to + (i * 4 + sub) * ROW, li * 8, v[i]);
+        for (int i = 0; i < N; ++i)
+            if (i * ROWS + r0 <= last) {
+                store_piece<STREAM>(K + to + (i * ROWS + r0) * ROW, k[i]);
+                store_piece<STREAM>(V + to + (i * ROWS + r0) * ROW, v[i]);
             }
     }
 }
@@ -350,20 +376,29 @@ int lvr_paged_append(lvr_paged *pc, void *k_pages, void *v_pages, const void *k_
     a.axis = pc->axis;
     a.n_kv = c.n_kv_heads;
     a.n_rows = 2 * c.n_kv_heads + (q ? c.n_q_heads : 0);
-    a.chunks = (a.n_rows + 7) / 8;
     a.rot = c.rot_dim;
     a.axes = c.rot_axes;
-    const dim3 grid((unsigned)((n_tokens * a.chunks + 3) / 4));
+    // Where there are tokens enough to fill the device a wave takes up to 24 rows, for which it makes sines and cosines once
+    const int rows = c.kv_dtype == LVR_BF16 ? 8 : 4;   // a wave's at a time
+    const bool many = n_tokens * a.n_rows >= APPEND_MANY;
+    const int per_wave = many ? 24 : rows;
+    a.groups = (a.n_rows + per_wave - 1) / per_wave;
+    const dim3 grid((unsigned)((n_tokens * a.groups + 3) / 4));
     hipStream_t st = static_cast<hipStream_t>(stream);
-#define LVR_APPEND(KT, N) hipLaunchKernelGGL((paged_append_kernel<KT, N>), grid, dim3(256), 0, st, a, b)
-    if (c.kv_dtype == LVR_BF16) {
-        if (c.rot_pairs == LVR_ROT_NEIGHBOURS) LVR_APPEND(lvr_bf16_t, true);
-        else LVR_APPEND(lvr_bf16_t, false);
-    } else {
-        if (c.rot_pairs == LVR_ROT_NEIGHBOURS) LVR_APPEND(lvr_f32_t, true);
-        else LVR_APPEND(lvr_f32_t, false);
-    }
+#define LVR_APPEND_PER(KT, N, PER)                                                                                \
+    do {                                                                                                          \
+        if (many) hipLaunchKernelGGL((paged_append_kernel<KT, N, PER, true>), grid, dim3(256), 0, st, a, b);      \
+        else hipLaunchKernelGGL((paged_append_kernel<KT, N, 1, false>), grid, dim3(256), 0, st, a, b);            \
+    } while (0)
+#define LVR_APPEND(KT, PER)                                                       \
+    do {                                                                          \
+        if (c.rot_pairs == LVR_ROT_NEIGHBOURS) LVR_APPEND_PER(KT, true, PER);     \
+        else LVR_APPEND_PER(KT, false, PER);                                      \
+    } while (0)
+    if (c.kv_dtype == LVR_BF16) LVR_APPEND(lvr_bf16_t, 3);
+    else LVR_APPEND(lvr_f32_t, 6);
 #undef LVR_APPEND
+#undef LVR_APPEND_PER
     LVR_HIP(hipGetLastError());
     return LVR_OK;
 }
@@ -396,12 +431,18 @@ int lvr_paged_gather(lvr_paged *pc, const void *k_pages, const void *v_pages, co
     const int64_t total = (n + 15) / 16 * n_kv * n_seqs;
     const int64_t wgs = (total + 3) / 4 < 65536 ? (total + 3) / 4 : 65536;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (pc->cfg.kv_dtype == LVR_BF16)
-        hipLaunchKernelGGL(paged_gather_kernel<lvr_bf16_t>, dim3((unsigned)wgs), dim3(256), 0, st, static_cast<const char *>(k_pages),
-                           static_cast<const char *>(v_pages), static_cast<char *>(K_out), static_cast<char *>(V_out), n, n_kv, b);
-    else
-        hipLaunchKernelGGL(paged_gather_kernel<lvr_f32_t>, dim3((unsigned)wgs), dim3(256), 0, st, static_cast<const char *>(k_pages),
-                           static_cast<const char *>(v_pages), static_cast<char *>(K_out), static_cast<char *>(V_out), n, n_kv, b);
+    const bool stream_out = n * n_kv * n_seqs * LVR_D * (pc->cfg.kv_dtype == LVR_BF16 ? 2 : 4) >= GATHER_STREAM;
+#define LVR_GATHER(KT, S)                                                                                                             \
+    hipLaunchKernelGGL((paged_gather_kernel<KT, S>), dim3((unsigned)wgs), dim3(256), 0, st, static_cast<const char *>(k_pages),       \
+                       static_cast<const char *>(v_pages), static_cast<char *>(K_out), static_cast<char *>(V_out), n, n_kv, b)
+    if (pc->cfg.kv_dtype == LVR_BF16) {
+        if (stream_out) LVR_GATHER(lvr_bf16_t, true);
+        else LVR_GATHER(lvr_bf16_t, false);
+    } else {
+        if (stream_out) LVR_GATHER(lvr_f32_t, true);
+        else LVR_GATHER(lvr_f32_t, false);
+    }
+#undef LVR_GATHER
     LVR_HIP(hipGetLastError());
     return LVR_OK;
 }
