@@ -19,8 +19,14 @@ namespace {
     } while (0)
 
 constexpr int PAIRS = LVR_D / 2;
-constexpr int64_t APPEND_MANY = 32768;        // rows of a call
-constexpr int64_t GATHER_STREAM = 4 << 20;   // bytes of each of K and V
+// Rows of a call (of K, V and q) from which a wave takes up to 24 of them and stores past the caches: it makes its sines and cosines
+// once, and the rows are more than the caches would keep.  us with eight rows a wave through the caches / so: 12288 rows 5.2 / 5.1,
+// with the attention behind it 21.4 / 23.0; 24576 rows 6.7 / 5.6; 98304 16.3 / 10.9; 393216 48.2 / 37.4 (4.2 / 5.4 TB/s).
+constexpr int64_t APPEND_MANY = 16384;
+// Bytes of K (and as many of V) from which gathered rows go past the caches.  Below that they wait in the memory-side cache for whoever
+// reads them next.  us with lvr_build behind, through / past: 32 MiB 49.8 / 54.3, 128 MiB 189 / 200, 256 MiB 389 / 393; alone 256 MiB
+// 202 / 191 (5.3 / 5.6 TB/s).
+constexpr int64_t GATHER_STREAM = (int64_t)192 << 20;
 
 // sin and cos of a fraction of a turn, given in units of 2^-32.  The nearest quarter turn is split off exactly (integers), the
 // rest lies within an eighth of a turn, where the Taylor series to x^9 and x^10 are off by less than 2^-28.

@@ -17,7 +17,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
 // Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.
 constexpr int ROWS16_PIECES = 512, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 512;
-constexpr int MIN_RUN = 256, MAX_RUNS = 512;
+constexpr int MIN_RUN = 256;
 // Rows of a sequence up to which it is taken in tiles of 16.  A wave of a 128-row tile works on 32 of them however many there are, and on
 // fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 57 in a tile of 128 / 46 in four of 16,
 // eight such sequences of 4096 keys 41 / 58; fp32 171 / 98).
@@ -94,7 +94,7 @@ __device__ __forceinline__ int token_of(const AttnArgs &a, int row) { return (in
 // up to a.narrow rows are taken in tiles of 16, others in tiles of 128; else all in tiles of 16.
 //
 // A sequence's tiles are cut into runs of keys of one length, as many as make about `target` pieces of the batch (but none under
-// MIN_RUN keys, and no more than MAX_RUNS of a tile; target 0: no cuts).  L is the keys of all tiles over target, where a tile
+// MIN_RUN keys; target 0: no cuts).  L is the keys of all tiles over target, where a tile
 // sees half of the sequence's own new keys.  Tiles of 128 rows are cut into span / L runs, rounded, so that equal ones fill whole
 // rounds of workgroups; beside them tiles of 16 rows, whose partial results are small, into runs of a quarter of that.  Without
 // tiles of 128 rows the number is rounded up.  There is room for the partial results of 2 * target pieces of cut 128-row tiles and
@@ -129,10 +129,6 @@ struct Division {
     __device__ __forceinline__ bool is_wide() const { return wide((s1 - s0) * G); }
     __device__ __forceinline__ void cut() {
         int L1 = L;
-        if (span > MAX_RUNS * (MIN_RUN / 2)) {
-            const int least = (span / MAX_RUNS + 64) & ~63;
-            if (L1 < least) L1 = least;
-        }
         if (MIXED && any_wide && !is_wide()) L1 = L1 > 4 * MIN_RUN ? L1 >> 2 : (L1 < MIN_RUN ? L1 : MIN_RUN);
         if (MIXED) {
             runs = about(span + (is_wide() ? L1 >> 1 : L1 - 1), L1);

@@ -150,6 +150,8 @@ LENS = {
     "beside_decodes": [(200, 333), (1, 90), (1, 1), (1, 513)],
     "many": [(1 + (i * 7) % 3, 3 + (i * 37) % 90) for i in range(70)] + [(0, 12)] * 70 + [(40, 300), (1, 600)],
     "many_single_tokens": [(1, 1 + (i * 53) % 400) for i in range(131)],
+    "cut_both_ways": [(40, 3000), (1, 4000), (2, 2500), (5, 700)],
+    "cut_chunk": [(300, 2600)],
     "tokens_before_the_cache": [(5, 3), (1, 0), (4, 0), (2, 40)],
 }
 
@@ -159,6 +161,27 @@ LENS = {
 def test_attention_over_lengths(lens, dtype):
     with Cache(LENS[lens], dtype=dtype, seed=3) as c:
         check_attention(c)
+
+
+@pytest.mark.parametrize("dtype, hq, hkv, lens, window", [
+    ("bf16", 8, 1, [(1, 20000)], 0),               # more runs than are merged at once
+    ("f32", 16, 1, [(1, 20000)], 0),
+    ("bf16", 4, 1, [(1, 9000), (1, 12000)], 7000),
+    ("bf16", 2, 1, [(1, 140000)], 0),
+    ("bf16", 8, 1, [(17, 9000)], 0),               # several tiles of 16 rows or one of 128, cut
+    ("f32", 4, 1, [(30, 5000), (1, 5000)], 0),
+])
+def test_attention_cut_into_many_runs(dtype, hq, hkv, lens, window):
+    with Cache(lens, dtype=dtype, hq=hq, hkv=hkv, page=64, seed=50) as c:
+        out = check_attention(c, window=window)
+        q = torch.Generator().manual_seed(3)
+        q = torch.randn(c.T, hq, D, generator=q).to(c.dt).cuda()
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        pools, batch = c.pools(), c.batch()
+        for o in (a, b):
+            L.lvr_paged_attention(c.h, *pools, q, *batch, o, window=window)
+        assert torch.equal(a, b), "the order of the runs shows in the result"
+        assert out.shape[0] == c.T
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -176,7 +199,7 @@ def test_attention_over_pages(page, layout):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("window", [1, 7, 33, 64, 300, 100000])
+@pytest.mark.parametrize("window", [1, 7, 33, 64, 300, 100000, 2 ** 31 - 1])
 def test_attention_with_a_window(window, dtype):
     with Cache([(1, 400), (90, 333), (5, 5), (1, 30)], dtype=dtype, seed=6) as c:
         check_attention(c, window=window)
@@ -481,3 +504,232 @@ def test_empty_batches():
         L.lvr_paged_append(c.h, *c.pools(), z(0, c.hkv, D), z(0, c.hkv, D), *c.batch())
         L.lvr_paged_gather(c.h, *c.pools(), *c.batch()[1:], z(0, c.hkv, 4, D), z(0, c.hkv, 4, D))
         torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------------------------------ as they are used
+def test_pools_of_more_than_4_gib():
+    """Pages past 2^32 bytes hold the same rows as a small pool and give the same bits."""
+    lens, hq, hkv, page = [(3, 200), (1, 77), (40, 90)], 16, 8, 64
+    big = 40000                                      # pages of 128 KiB
+    with Cache(lens, hq=hq, hkv=hkv, page=page, rot_dim=128, inv_freq=freqs(128), seed=60) as c:
+        used = [int(p) for p in c.table.flatten() if p >= 0]
+        far = {p: big - 1 - 37 * i for i, p in enumerate(used)}
+        cfg = L.make_paged_config(n_q_heads=hq, n_kv_heads=hkv, page_size=page, n_pages=big, rot_dim=128)
+        h = L.lvr_paged_create(cfg, inv_freq=freqs(128))
+        try:
+            K, V = (torch.empty(big, hkv, page, D, dtype=c.dt, device="cuda") for _ in range(2))
+            kp, vp = c.pools()
+            for p, f in far.items():
+                K[f], V[f] = kp[p], vp[p]
+            table = torch.tensor([[far.get(int(p), -1) for p in row] for row in c.table], dtype=torch.int32, device="cuda")
+            start, length, small_table = c.batch()
+            k, q = c.randn(c.T, hkv, D).cuda(), c.randn(c.T, hq, D).cuda()
+            got = []
+            for handle, pools, tab in ((c.h, (kp, vp), small_table), (h, (K, V), table)):
+                qo, out = torch.empty_like(q), torch.empty_like(q)
+                rows = [torch.zeros(3, hkv, 200, D, dtype=c.dt, device="cuda") for _ in range(2)]
+                L.lvr_paged_append(handle, *pools, k, k, start, length, tab, q=q, q_out=qo)
+                L.lvr_paged_attention(handle, *pools, qo, start, length, tab, out)
+                L.lvr_paged_gather(handle, *pools, length, tab, *rows)
+                got.append([qo, out, *rows])
+            assert all(torch.equal(x, y) for x, y in zip(*got))
+            for p, f in far.items():
+                assert torch.equal(K[f], kp[p]) and torch.equal(V[f], vp[p])
+        finally:
+            L.lvr_paged_destroy(h)
+
+
+def _prompt_in_chunks(c, k, v, q, sizes, stream=None):
+    """Appends and attends the tokens of one sequence piece by piece; returns pools and outputs."""
+    kp, vp = c.pools()
+    outs, at = [], 0
+    table = c.table.cuda()
+    for m in sizes:
+        start = torch.tensor([0, m], dtype=torch.int32, device="cuda")
+        length = torch.tensor([at + m], dtype=torch.int32, device="cuda")
+        qo, out = torch.empty_like(q[at:at + m]), torch.empty_like(q[at:at + m])
+        L.lvr_paged_append(c.h, kp, vp, k[at:at + m], v[at:at + m], start, length, table, q=q[at:at + m], q_out=qo, stream=stream)
+        L.lvr_paged_attention(c.h, kp, vp, qo, start, length, table, out, stream=stream)
+        outs.append(out)
+        at += m
+    return kp, vp, torch.cat(outs)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_from_the_prompt_to_the_index(dtype):
+    """A prompt comes in pieces of odd sizes through append and attention, its pages become rows, the rows an index, and the next token
+    is decoded from the index and from the pages: the same keys, the same attention."""
+    n, hq, hkv, f = 700, 8, 2, freqs(128)
+    with Cache([(n, n + 1)], dtype=dtype, hq=hq, hkv=hkv, rot_dim=128, inv_freq=f, seed=61) as c:
+        fused = c.randn(n + 1, (hq + 2 * hkv) * D)
+        q, k, v = (x.unflatten(1, (-1, D)) for x in fused.split([hq * D, hkv * D, hkv * D], dim=1))
+        dq, dk, dv = (x.unflatten(1, (-1, D)) for x in fused.cuda().split([hq * D, hkv * D, hkv * D], dim=1))
+        kp, vp, out = _prompt_in_chunks(c, dk[:n], dv[:n], dq[:n], [1, 130, 17, 300, 252])
+        # the whole prompt in 64 bits, from the rotated rows as the pages hold them
+        pos = torch.arange(n + 1)[:, None]
+        Kr = rotated(k, pos, f, [0] * 64, 128, L.LVR_ROT_HALVES)[0].to(c.dt)
+        Qr = rotated(q, pos, f, [0] * 64, 128, L.LVR_ROT_HALVES)[0].to(c.dt)
+        ref = torch.empty(n, hq, D, dtype=torch.float64)
+        for h in range(hq):
+            s = Qr[:n, h].double() @ Kr[:n, h // 4].double().T / math.sqrt(D)
+            s = torch.where(torch.ones(n, n, dtype=torch.bool).tril(), s, torch.tensor(-math.inf, dtype=torch.float64))
+            ref[:, h] = torch.softmax(s, dim=1) @ v[:n, h // 4].double()
+        # A key or query component may be rounded the other way than the reference's (its value lies next to a border: one step, 2 * HALF_STEP of
+        # it); a score of 128 such products of size S moves by at most 4 * HALF_STEP * S and a weight by twice that, on top of what
+        # test_attention_over_lengths counts.  S is at most about 30 here; the outputs are means of values of size 1.
+        step = HALF_STEP[dtype]
+        S = max(float((Qr[:n, h].double().abs() @ Kr[:n, h // 4].double().abs().T / math.sqrt(D)).max()) for h in range(hq))
+        tol = (8 * step * S + 4 * step) * 4
+        assert (out.cpu().double() - ref).abs().max() <= tol
+        rows = [torch.zeros(1, hkv, n, D, dtype=c.dt, device="cuda") for _ in range(2)]
+        length = torch.tensor([n], dtype=torch.int32, device="cuda")
+        L.lvr_paged_gather(c.h, kp, vp, length, c.table.cuda(), *rows)
+        assert torch.equal(rows[1][0].cpu(), v[:n].transpose(0, 1))
+        cfg = L.make_config(batch=1, n_q_heads=hq, n_kv_heads=hkv, kv_dtype=L.LVR_BF16 if dtype == "bf16" else L.LVR_F32, capacity=n + 1,
+                            group_size=1 if dtype == "bf16" else 4)
+        ix = L.lvr_create(cfg)
+        try:
+            L.lvr_build(ix, *rows)
+            start = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+            length = torch.tensor([n + 1], dtype=torch.int32, device="cuda")
+            qo, paged = (torch.empty(1, hq, D, dtype=c.dt, device="cuda") for _ in range(2))
+            L.lvr_paged_append(c.h, kp, vp, dk[n:], dv[n:], start, length, c.table.cuda(), q=dq[n:], q_out=qo)
+            L.lvr_paged_attention(c.h, kp, vp, qo, start, length, c.table.cuda(), paged)
+            new = [torch.zeros(1, hkv, n + 1, D, dtype=c.dt, device="cuda") for _ in range(2)]
+            L.lvr_paged_gather(c.h, kp, vp, length, c.table.cuda(), *new)
+            tau = torch.full((1, hq), -math.inf, device="cuda")
+            idx = torch.zeros(1, hq, n + 1, dtype=torch.int32, device="cuda")
+            cnt, dense = torch.zeros(1, hq, dtype=torch.int32, device="cuda"), torch.empty(1, hq, D, device="cuda")
+            L.lvr_append_decode_step(ix, new[0][:, :, n:].contiguous(), new[1][:, :, n:].contiguous(), qo.float(), tau, dense, idx, cnt)
+            torch.cuda.synchronize()
+            assert (cnt == n + 1).all()
+            got, want = paged.double().cpu(), dense.double().cpu()
+            # the index keeps its weights in fp32; the pages' attention rounds them to the cache's type, and its output
+            err = (got - want).abs().amax() / want.abs().amax()
+            assert err <= (4 * step if dtype == "bf16" else 2e-5), float(err)
+        finally:
+            L.lvr_destroy(ix)
+
+
+def test_calls_on_a_stream_of_their_own_and_two_handles_at_once():
+    f = freqs(128)
+    a = Cache([(130, 400), (1, 900)], rot_dim=128, inv_freq=f, seed=62)
+    b = Cache([(1, 3000), (3, 50)], rot_dim=128, inv_freq=f, seed=63)
+    with a, b:
+        args = []
+        for c in (a, b):
+            k, q = c.randn(c.T, c.hkv, D).cuda(), c.randn(c.T, c.hq, D).cuda()
+            args.append((c, c.pools(), k, q, c.batch(), torch.empty_like(q), torch.empty_like(q)))
+        def work(x, stream):
+            c, pools, k, q, batch, qo, out = x
+            L.lvr_paged_append(c.h, *pools, k, k, *batch, q=q, q_out=qo, stream=stream)
+            L.lvr_paged_attention(c.h, *pools, qo, *batch, out, stream=stream)
+        for x in args:
+            work(x, None)
+        torch.cuda.synchronize()
+        want = [x[6].clone() for x in args]
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        for _ in range(5):
+            for x in args:
+                x[6].fill_(7)
+            torch.cuda.synchronize()
+            for x, st in zip(args, streams):
+                work(x, st)
+            torch.cuda.synchronize()
+            assert all(torch.equal(x[6], w) for x, w in zip(args, want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_steps_follow_the_arrays(dtype):
+    """A decode step and a step with a prompt in it, recorded once each on one handle and replayed in turn while lengths, tables and inputs
+    change: every replay gives the eager call's bits.  Rows behind the last sequence (a padded batch) stay as they were."""
+    f = freqs(128)
+    with Cache([(1, 900), (1, 40), (1, 2000), (0, 0)], dtype=dtype, rot_dim=128, inv_freq=f, seed=64, behind=0) as c:
+        kp, vp = c.pools()
+        table = c.table.cuda()
+        steps = []
+        for T in (4, 160):
+            s = dict(start=torch.zeros(5, dtype=torch.int32, device="cuda"), length=torch.zeros(4, dtype=torch.int32, device="cuda"))
+            for name, heads in (("k", c.hkv), ("q", c.hq), ("qo", c.hq), ("out", c.hq)):
+                s[name] = torch.zeros(T, heads, D, dtype=c.dt, device="cuda")
+            steps.append(s)
+
+        def work(s):
+            L.lvr_paged_append(c.h, kp, vp, s["k"], s["k"], s["start"], s["length"], table, q=s["q"], q_out=s["qo"])
+            L.lvr_paged_attention(c.h, kp, vp, s["qo"], s["start"], s["length"], table, s["out"])
+
+        graphs = []
+        for s in steps:
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                work(s)
+            torch.cuda.current_stream().wait_stream(side)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                work(s)
+            graphs.append(g)
+        for turn, lens in enumerate([([1, 1, 1, 0], [900, 40, 2000, 0]), ([1, 0, 1, 0], [700, 0, 5, 0]), ([90, 1, 1, 0], [880, 33, 1999, 0]), ([1, 1, 1, 0], [64, 16, 17, 0])]):
+            for s, g in zip(steps, graphs):
+                if sum(lens[0]) > s["q"].shape[0]:
+                    continue
+                starts = np.concatenate([[0], np.cumsum(lens[0])])
+                s["start"].copy_(torch.tensor(starts, dtype=torch.int32))
+                s["length"].copy_(torch.tensor(lens[1], dtype=torch.int32))
+                for name in ("k", "q"):
+                    s[name].copy_(c.randn(*s[name].shape))
+                results = []
+                for replay in (False, True, True):
+                    s["out"].fill_(7)
+                    s["qo"].fill_(7)
+                    torch.cuda.synchronize()
+                    g.replay() if replay else work(s)
+                    torch.cuda.synchronize()
+                    results.append((s["out"].clone(), s["qo"].clone(), kp.clone(), vp.clone()))
+                for other in results[1:]:
+                    assert all(torch.equal(x, y) for x, y in zip(results[0], other)), turn
+                assert (results[0][0][int(starts[-1]):] == 7).all() and (results[0][1][int(starts[-1]):] == 7).all()
+                assert torch.isfinite(results[0][0].float()).all()
+
+
+def test_a_batch_of_many_pieces():
+    """4096 sequences of nine tiles each: more pieces than a launch has workgroups in one of its dimensions.  The same bits as from two halves."""
+    seqs, t, hq = 4096, 33, 32
+    cfg = L.make_paged_config(n_q_heads=hq, n_kv_heads=1, page_size=64, n_pages=seqs)
+    h = L.lvr_paged_create(cfg)
+    try:
+        g = torch.Generator(device="cuda").manual_seed(5)
+        K, V = (torch.randn(seqs, 1, 64, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+        q = torch.randn(seqs * t, hq, D, generator=g, device="cuda").to(torch.bfloat16)
+        start = torch.arange(0, seqs * t + 1, t, dtype=torch.int32, device="cuda")
+        length = torch.randint(t, 65, (seqs,), generator=g, device="cuda").to(torch.int32)
+        table = torch.randperm(seqs, generator=g, device="cuda").to(torch.int32)[:, None].contiguous()
+        whole, halves = torch.empty_like(q), torch.empty_like(q)
+        L.lvr_paged_attention(h, K, V, q, start, length, table, whole)
+        for a, b in ((0, seqs // 2), (seqs // 2, seqs)):
+            L.lvr_paged_attention(h, K, V, q[a * t:b * t], start[a:b + 1] - a * t, length[a:b], table[a:b], halves[a * t:b * t])
+        assert torch.equal(whole, halves) and torch.isfinite(whole.float()).all()
+    finally:
+        L.lvr_paged_destroy(h)
+
+
+def test_sequences_in_no_order_leave_the_handle_usable():
+    """seq_start that is not ascending is a mistake of the caller's: nothing is promised for that call's outputs, later calls are as before."""
+    with Cache([(1, 3000), (1, 400), (2, 90)], seed=65) as c:
+        q = c.randn(c.T, c.hq, D).cuda()
+        start, length, table = c.batch()
+        pools = c.pools()
+        want, out = torch.empty_like(q), torch.empty_like(q)
+        L.lvr_paged_attention(c.h, *pools, q, start, length, table, want)
+        for bad in ([4, 0, 4, 0], [0, 4, 0, 4], [-5, 100, 2, -7], [2 ** 31 - 1, 0, 1, -2 ** 31], [3, 3, 1, 4]):
+            L.lvr_paged_attention(c.h, *pools, q, torch.tensor(bad, dtype=torch.int32, device="cuda"), length, table, out)
+            L.lvr_paged_append(c.h, *[p.clone() for p in pools], q[:, :c.hkv].contiguous(), q[:, :c.hkv].contiguous(),
+                               torch.tensor(bad, dtype=torch.int32, device="cuda"), length, table)
+            torch.cuda.synchronize()
+            L.lvr_paged_attention(c.h, *pools, q, start, length, table, out)
+            assert torch.equal(out, want)
+        odd = torch.tensor([2 ** 31 - 1, -2 ** 31, 5], dtype=torch.int32, device="cuda")      # lengths beyond the table, below zero
+        L.lvr_paged_attention(c.h, *pools, q, start, odd, table, out)
+        L.lvr_paged_attention(c.h, *pools, q, start, length, table, out)
+        assert torch.equal(out, want)
