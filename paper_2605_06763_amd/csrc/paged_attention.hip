@@ -24,7 +24,7 @@ constexpr int MIN_RUN = 256;
 constexpr int NARROW_BF16 = 32, NARROW_F32 = 64;
 constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);
 constexpr int MERGE_WGS = 1024;
-constexpr int FAN = 8;        // partial results of 16-row tiles that a wave merges at a time
+constexpr int FAN_BITS = 3, FAN = 1 << FAN_BITS;   // partial results of 16-row tiles that a wave merges at a time
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -107,7 +107,9 @@ struct Division {
     int G, window, narrow, L;
     int n_wide;                              // pieces of 128-row tiles, which come first
     bool any_wide;
-    int s0, s1, n, tiles, span, run, runs;   // this lane's sequence
+    static constexpr int NO_CUTS = 1 << 30;   // an L
+    int s0, s1, n, tiles, span;              // this lane's sequence
+    int run = 0, runs = 1;
 
     __device__ __forceinline__ bool wide(int rows) const { return MIXED && rows > narrow; }
     __device__ __forceinline__ void look(int i) {
@@ -123,11 +125,14 @@ struct Division {
             tiles = wide(rows) ? (rows + 127) / 128 : (rows + 15) / 16;
             const int reach = window ? window + 128 : n;   // keys a tile can see, at most
             span = n < reach ? n : reach;
+            if (span > b.table_width << b.page_shift) span = b.table_width << b.page_shift;
             if (span < 1) span = 1;
         }
     }
     __device__ __forceinline__ bool is_wide() const { return wide((s1 - s0) * G); }
     __device__ __forceinline__ void cut() {
+        runs = 1;
+        if (L == NO_CUTS) return;
         int L1 = L;
         if (MIXED && any_wide && !is_wide()) L1 = L1 > 4 * MIN_RUN ? L1 >> 2 : (L1 < MIN_RUN ? L1 : MIN_RUN);
         if (MIXED) {
@@ -157,17 +162,17 @@ struct Division {
         } else {
             keys = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(keys)));
         }
-        L = 1 << 30;
+        L = NO_CUTS;
         if (target > 0) {
             const float want = keys * 1.001f / (float)target;   // (more than what the sum was rounded by)
-            L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? 1 << 30 : ((int)want + 63) & ~63);
+            L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? NO_CUTS : ((int)want + 63) & ~63);
         }
         if (!MIXED) {   // at most target pieces more than tiles, and at most 2 * target of cut tiles, since L is all keys over target
             n_wide = 0;
             if (b.n_seqs <= 64) cut();
             return true;
         }
-        for (;; L = L < 1 << 28 ? (L + L / 2) & ~63 : 1 << 30) {
+        for (;; L = L < 1 << 28 ? (L + L / 2) & ~63 : NO_CUTS) {
             int cut_wide = 0, cut_narrow = 0;
             n_wide = 0;
             for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
@@ -178,7 +183,7 @@ struct Division {
                 cut_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? cut_here : 0), 63);
                 cut_narrow += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? 0 : cut_here), 63);
             }
-            if ((cut_wide <= 2 * target && cut_wide + cut_narrow <= 3 * target) || L == 1 << 30) break;
+            if (cut_wide <= 2 * target && cut_wide + cut_narrow <= 3 * target) break;   // as it is at the latest without cuts
         }
         return true;
     }
@@ -571,8 +576,8 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
         // more the waves share the partials out; each takes up to FAN of them with all their loads in flight.  Partials cross
         // from one die to another: they are stored and read with accesses of device scope, and a workgroup waits for its own stores
         // before it takes a ticket, which wraps at the number of those who take it and so is zero again afterwards.
-        const int rows = t.rows - t.row0, sharers = rows <= 4 ? 4 : (rows <= 8 ? 2 : 1), fan = FAN * sharers;
-        const int slot0 = t.slot - t.split, fans = (t.splits + fan - 1) / fan, mine = t.split / fan;
+        const int rows = t.rows - t.row0, sharer_bits = rows <= 4 ? 2 : (rows <= 8 ? 1 : 0), sharers = 1 << sharer_bits, fan = FAN * sharers;
+        const int slot0 = t.slot - t.split, fans = (t.splits + fan - 1) >> (FAN_BITS + sharer_bits), mine = t.split >> (FAN_BITS + sharer_bits);
         const int in_mine = mine + 1 < fans ? fan : t.splits - mine * fan;
         float *first_part = partial<16>(a.part, slot0, a.n_kv, kvh);
         const int64_t step = (int64_t)a.n_kv * (16 * (LVR_D + 2));
@@ -590,7 +595,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
             return lds.arrived == (unsigned)n - 1u;
         };
         auto merge = [&](const float *p, int64_t apart, int n) {
-            const int share = wave * sharers / 4, mr = (wave & (4 / sharers - 1)) * 4 + (lane >> 4);   // whose turn, which row
+            const int share = wave >> (2 - sharer_bits), mr = (wave & ((4 >> sharer_bits) - 1)) * 4 + (lane >> 4);   // whose turn, which row
             x.clear();
             for (int p0 = share; p0 < n; p0 += fan) {
                 float2 ml[FAN], v[FAN][4];

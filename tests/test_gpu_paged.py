@@ -714,6 +714,32 @@ def test_a_batch_of_many_pieces():
         L.lvr_paged_destroy(h)
 
 
+@pytest.mark.parametrize("tokens", [1, 4, 40])
+def test_lengths_far_beyond_the_table(tokens):
+    """Sequences that claim 2^30 keys with a table of two pages: the division of such a batch stays within the work space of the fewest pieces
+    per KV head, and every token attends the keys there are."""
+    seqs, heads = 16, 256
+    cfg = L.make_paged_config(n_q_heads=heads, n_kv_heads=heads, page_size=16, n_pages=2 * seqs)
+    h = L.lvr_paged_create(cfg)
+    try:
+        g = torch.Generator(device="cuda").manual_seed(6)
+        K, V = (torch.randn(2 * seqs, heads, 16, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+        q = torch.randn(seqs * tokens, heads, D, generator=g, device="cuda").to(torch.bfloat16)
+        start = torch.arange(0, seqs * tokens + 1, tokens, dtype=torch.int32, device="cuda")
+        table = torch.arange(2 * seqs, dtype=torch.int32, device="cuda").view(seqs, 2)
+        outs = []
+        for n in (32 + tokens, 2 ** 30, 2 ** 31 - 1):
+            length, out = torch.full((seqs,), n, dtype=torch.int32, device="cuda"), torch.empty_like(q)
+            L.lvr_paged_attention(h, K, V, q, start, length, table, out)
+            outs.append(out)
+        s = torch.einsum("thd,hnd->thn", q[:tokens].float(), K[:2].permute(1, 0, 2, 3).reshape(heads, 32, D).float()) / math.sqrt(D)
+        ref = torch.einsum("thn,hnd->thd", torch.softmax(s, dim=2), V[:2].permute(1, 0, 2, 3).reshape(heads, 32, D).float())
+        assert (outs[0][:tokens].float() - ref).abs().max() <= 3 * 2.0 ** -8 * 5      # values below 5, each rounding half a step of them
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    finally:
+        L.lvr_paged_destroy(h)
+
+
 def test_sequences_in_no_order_leave_the_handle_usable():
     """seq_start that is not ascending is a mistake of the caller's: nothing is promised for that call's outputs, later calls are as before."""
     with Cache([(1, 3000), (1, 400), (2, 90)], seed=65) as c:
