@@ -456,6 +456,7 @@ class PagedHandle(C.c_void_p):
     """What lvr_paged_create returns: the C handle, with what the calls check tensors against."""
     cfg: lvr_paged_config
     cfg_at: int          # its address, for the compiled calls
+    device: int          # index of the GPU it was made on
     dtype: torch.dtype
 
 
@@ -489,6 +490,7 @@ def lvr_paged_create(cfg: lvr_paged_config, inv_freq=None, axis=None) -> PagedHa
     _check(lib().lvr_paged_create(C.byref(cfg), freq, ax, C.byref(h)), "lvr_paged_create")
     h.cfg = lvr_paged_config.from_buffer_copy(cfg)
     h.cfg_at = C.addressof(h.cfg)
+    h.device = torch.cuda.current_device()
     h.dtype = torch.bfloat16 if cfg.kv_dtype == LVR_BF16 else torch.float32
     return h
 
@@ -497,17 +499,19 @@ def lvr_paged_destroy(h) -> None:
     _check(lib().lvr_paged_destroy(h), "lvr_paged_destroy")
 
 
-def _tensor(t, name: str) -> torch.Tensor:
+def _tensor(h, t, name: str) -> torch.Tensor:
     if type(t) is DeviceArg:
         t = t.tensor
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    if t.get_device() != h.device:
+        raise ValueError(f"{name} must be on cuda:{h.device}, as the handle, not on {t.device}")
     return t
 
 
 def _pool(h, t, name: str):
     """A pool of pages: [page][head][token][head_dim] or [page][token][head][head_dim] with the strides of the configuration."""
-    c, t = h.cfg, _tensor(t, name)
+    c, t = h.cfg, _tensor(h, t, name)
     if t.dtype != h.dtype:
         raise ValueError(f"{name} must be {h.dtype}, got {t.dtype}")
     want, shape = tuple(c.page_strides), tuple(t.shape)
@@ -523,7 +527,7 @@ def _pool(h, t, name: str):
 
 def _tokens(h, t, heads: int, n, name: str):
     """Rows of new tokens [n_tokens][heads][head_dim], the heads of a token contiguous.  Returns pointer, token stride and n_tokens."""
-    c, t = h.cfg, _tensor(t, name)
+    c, t = h.cfg, _tensor(h, t, name)
     if t.dtype != h.dtype:
         raise ValueError(f"{name} must be {h.dtype}, got {t.dtype}")
     if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != c.head_dim or (n is not None and t.shape[0] != n):
@@ -536,8 +540,8 @@ def _tokens(h, t, heads: int, n, name: str):
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * c.head_dim, t.shape[0]
 
 
-def _whole(t, dtype, shape, name: str):
-    t = _tensor(t, name)
+def _whole(h, t, dtype, shape, name: str):
+    t = _tensor(h, t, name)
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if tuple(t.shape) != shape or not t.is_contiguous():
@@ -545,20 +549,20 @@ def _whole(t, dtype, shape, name: str):
     return t.data_ptr()
 
 
-def _batch(seq_start, seq_len, table):
-    table = _tensor(table, "table")
+def _batch(h, seq_start, seq_len, table):
+    table = _tensor(h, table, "table")
     if table.dim() != 2:
         raise ValueError("table must be [n_seqs][table_width]")
     n, width = table.shape
-    start = None if seq_start is None else _whole(seq_start, torch.int32, (n + 1,), "seq_start")
-    return start, _whole(seq_len, torch.int32, (n,), "seq_len"), _whole(table, torch.int32, (n, width), "table"), width, n
+    start = None if seq_start is None else _whole(h, seq_start, torch.int32, (n + 1,), "seq_start")
+    return start, _whole(h, seq_len, torch.int32, (n,), "seq_len"), _whole(h, table, torch.int32, (n, width), "table"), width, n
 
 
 def lvr_paged_append(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q=None, q_out=None, positions=None, stream=None) -> None:
     """k_new, v_new [n_tokens][n_kv_heads][128], q and q_out [n_tokens][n_q_heads][128] (q_out contiguous, or q itself);
     positions [n_tokens][rot_axes] int32, None: the token's position in its sequence; seq_start, seq_len, table: int32."""
     st = _early_stream(stream)
-    code = _call.paged_append(h, h.cfg_at, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, st) if st is not None else None
+    code = _call.paged_append(h, h.cfg_at, h.device, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, st) if st is not None else None
     if code is None:   # not all plain tensors of the right kind, or the first call
         kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
         k, ks, n = _tokens(h, k_new, h.cfg.n_kv_heads, None, "k_new")
@@ -569,9 +573,9 @@ def lvr_paged_append(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, tabl
         qs = 0
         if q is not None:
             qp, qs, _ = _tokens(h, q, h.cfg.n_q_heads, n, "q")
-            qo = _whole(q_out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "q_out")
-        pos = None if positions is None else _whole(positions, torch.int32, (n, max(h.cfg.rot_axes, 1)), "positions")
-        start, length, tab, width, seqs = _batch(seq_start, seq_len, table)
+            qo = _whole(h, q_out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "q_out")
+        pos = None if positions is None else _whole(h, positions, torch.int32, (n, max(h.cfg.rot_axes, 1)), "positions")
+        start, length, tab, width, seqs = _batch(h, seq_start, seq_len, table)
         code = lib().lvr_paged_append(h, kp, vp, k, v, qp, qo, (C.c_int64 * 3)(ks, vs, qs), pos, start, length, tab, width, seqs, n,
                                       _stream(stream))
     if code != LVR_OK:
@@ -581,12 +585,12 @@ def lvr_paged_append(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, tabl
 def lvr_paged_attention(h, k_pages, v_pages, q, seq_start, seq_len, table, out, window=0, stream=None) -> None:
     """q [n_tokens][n_q_heads][128], out the same and contiguous; seq_start, seq_len, table: int32."""
     st = _early_stream(stream)
-    code = _call.paged_attention(h, h.cfg_at, k_pages, v_pages, q, seq_start, seq_len, table, out, window, st) if st is not None else None
+    code = _call.paged_attention(h, h.cfg_at, h.device, k_pages, v_pages, q, seq_start, seq_len, table, out, window, st) if st is not None else None
     if code is None:   # not all plain tensors of the right kind, or the first call
         kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
         qp, qs, n = _tokens(h, q, h.cfg.n_q_heads, None, "q")
-        o = _whole(out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "out")
-        start, length, tab, width, seqs = _batch(seq_start, seq_len, table)
+        o = _whole(h, out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "out")
+        start, length, tab, width, seqs = _batch(h, seq_start, seq_len, table)
         if not 0 <= int(window) < 1 << 31:
             raise ValueError("window must be 0 (all keys) or a number of keys below 2^31")
         code = lib().lvr_paged_attention(h, kp, vp, qp, qs, start, length, tab, width, seqs, n, int(window), o, _stream(stream))
@@ -597,16 +601,16 @@ def lvr_paged_attention(h, k_pages, v_pages, q, seq_start, seq_len, table, out, 
 def lvr_paged_gather(h, k_pages, v_pages, seq_len, table, K_out, V_out, stream=None) -> None:
     """K_out, V_out: contiguous device tensors [n_seqs][n_kv_heads][n][128]; rows past a sequence's end stay as they are."""
     st = _early_stream(stream)
-    code = _call.paged_gather(h, h.cfg_at, k_pages, v_pages, seq_len, table, K_out, V_out, st) if st is not None else None
+    code = _call.paged_gather(h, h.cfg_at, h.device, k_pages, v_pages, seq_len, table, K_out, V_out, st) if st is not None else None
     if code is None:   # not all plain tensors of the right kind, or the first call
         kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
-        _, length, tab, width, seqs = _batch(None, seq_len, table)
-        K = _tensor(K_out, "K_out")
+        _, length, tab, width, seqs = _batch(h, None, seq_len, table)
+        K = _tensor(h, K_out, "K_out")
         if K.dim() != 4:
             raise ValueError("K_out must be [n_seqs][n_kv_heads][n][head_dim]")
         n = K.shape[2]
         shape = (seqs, h.cfg.n_kv_heads, n, h.cfg.head_dim)
-        ko, vo = _whole(K, h.dtype, shape, "K_out"), _whole(V_out, h.dtype, shape, "V_out")
+        ko, vo = _whole(h, K, h.dtype, shape, "K_out"), _whole(h, V_out, h.dtype, shape, "V_out")
         code = lib().lvr_paged_gather(h, kp, vp, length, tab, width, seqs, n, ko, vo, _stream(stream))
     if code != LVR_OK:
         raise LouverError(code, "lvr_paged_gather")

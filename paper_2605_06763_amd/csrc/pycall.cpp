@@ -195,23 +195,23 @@ PyObject *sparse_attention_static(PyObject *, PyObject *const *a, Py_ssize_t n) 
 
 // ---- the paged cache.  What binding.py checks, with the same outcome: anything else goes there and is refused.
 
-const at::Tensor *device_tensor(PyObject *o, int type) {
+const at::Tensor *device_tensor(PyObject *o, int type, int device) {
     if (PyObject_TypeCheck(o, &ArgType)) o = reinterpret_cast<Arg *>(o)->tensor;
     if (!o || !THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
-    return t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && (int)t.scalar_type() == type ? &t : nullptr;
+    return t.is_cuda() && t.get_device() == device && t.layout() == at::kStrided && t.has_storage() && (int)t.scalar_type() == type ? &t : nullptr;
 }
 
 struct Paged {
     lvr_paged *h;
     const lvr_paged_config *c;
     void *stream;
-    int type;
+    int type, device;
     void *k_pages, *v_pages, *start, *len, *table;
     int64_t width, seqs;
 
     bool pool(PyObject *o, void *&p) const {   // [page][head][token][head_dim], or token before head
-        const at::Tensor *t = device_tensor(o, type);
+        const at::Tensor *t = device_tensor(o, type, device);
         if (!t || t->dim() != 4 || t->stride(3) != 1 || t->size(0) != c->n_pages || t->size(3) != c->head_dim || t->stride(0) != c->page_strides[0])
             return false;
         const bool heads_first = t->size(1) == c->n_kv_heads && t->size(2) == c->page_size && t->stride(1) == c->page_strides[1] && t->stride(2) == c->page_strides[2];
@@ -221,7 +221,7 @@ struct Paged {
     }
     // rows of new tokens, a token's heads contiguous; n < 0: as many as there are
     bool tokens(PyObject *o, int64_t heads, int64_t &n, void *&p, int64_t &stride) const {
-        const at::Tensor *t = device_tensor(o, type);
+        const at::Tensor *t = device_tensor(o, type, device);
         if (!t || t->dim() != 3 || t->size(1) != heads || t->size(2) != c->head_dim || (n >= 0 && t->size(0) != n)) return false;
         n = t->size(0);
         if (n > 0 && (t->stride(2) != 1 || (heads > 1 && t->stride(1) != c->head_dim))) return false;
@@ -230,13 +230,13 @@ struct Paged {
         return true;
     }
     bool whole(PyObject *o, int want, c10::IntArrayRef shape, void *&p) const {
-        const at::Tensor *t = device_tensor(o, want);
+        const at::Tensor *t = device_tensor(o, want, device);
         if (!t || t->sizes() != shape || !t->is_contiguous()) return false;
         p = t->data_ptr();
         return true;
     }
     bool batch(PyObject *o_start, PyObject *o_len, PyObject *o_table) {
-        const at::Tensor *t = device_tensor(o_table, (int)at::kInt);
+        const at::Tensor *t = device_tensor(o_table, (int)at::kInt, device);
         if (!t || t->dim() != 2 || !t->is_contiguous()) return false;
         seqs = t->size(0);
         width = t->size(1);
@@ -244,10 +244,11 @@ struct Paged {
         start = nullptr;
         return whole(o_len, (int)at::kInt, {seqs}, len) && (!o_start || whole(o_start, (int)at::kInt, {seqs + 1}, start));
     }
-    // (h, address of its configuration, ..., stream)
-    bool begin(PyObject *o_h, PyObject *o_cfg, PyObject *o_stream) {
+    // (h, address of its configuration, its device, ..., stream)
+    bool begin(PyObject *o_h, PyObject *o_cfg, PyObject *o_device, PyObject *o_stream) {
         void *hp;
-        if (!address(o_h, hp) || !PyLong_CheckExact(o_cfg) || !address(o_stream, stream)) return false;
+        if (!address(o_h, hp) || !PyLong_CheckExact(o_cfg) || !PyLong_CheckExact(o_device) || !address(o_stream, stream)) return false;
+        device = (int)PyLong_AsLong(o_device);
         h = static_cast<lvr_paged *>(hp);
         c = static_cast<const lvr_paged_config *>(PyLong_AsVoidPtr(o_cfg));
         if (!c || PyErr_Occurred()) {
@@ -259,36 +260,36 @@ struct Paged {
     }
 };
 
-// (h, cfg, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, stream)
+// (h, cfg, device, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, stream)
 PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Paged p;
     void *k, *v, *q = nullptr, *q_out = nullptr, *pos = nullptr;
     int64_t tokens = -1, strides[3] = {0, 0, 0};
     LVR_PLAIN(
-        LVR_NOT_PLAIN(n == 13 && lib.paged_append && p.begin(a[0], a[1], a[12]) && p.pool(a[2], p.k_pages) && p.pool(a[3], p.v_pages) &&
-                      p.tokens(a[4], p.c->n_kv_heads, tokens, k, strides[0]) && p.tokens(a[5], p.c->n_kv_heads, tokens, v, strides[1]) &&
-                      p.batch(a[6], a[7], a[8]) && (a[9] == Py_None) == (a[10] == Py_None));
-        if (a[9] != Py_None)
-            LVR_NOT_PLAIN(p.tokens(a[9], p.c->n_q_heads, tokens, q, strides[2]) &&
-                          p.whole(a[10], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, q_out));
-        if (a[11] != Py_None) LVR_NOT_PLAIN(p.whole(a[11], I32, {tokens, (int64_t)(p.c->rot_axes > 1 ? p.c->rot_axes : 1)}, pos));)
+        LVR_NOT_PLAIN(n == 14 && lib.paged_append && p.begin(a[0], a[1], a[2], a[13]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
+                      p.tokens(a[5], p.c->n_kv_heads, tokens, k, strides[0]) && p.tokens(a[6], p.c->n_kv_heads, tokens, v, strides[1]) &&
+                      p.batch(a[7], a[8], a[9]) && (a[10] == Py_None) == (a[11] == Py_None));
+        if (a[10] != Py_None)
+            LVR_NOT_PLAIN(p.tokens(a[10], p.c->n_q_heads, tokens, q, strides[2]) &&
+                          p.whole(a[11], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, q_out));
+        if (a[12] != Py_None) LVR_NOT_PLAIN(p.whole(a[12], I32, {tokens, (int64_t)(p.c->rot_axes > 1 ? p.c->rot_axes : 1)}, pos));)
     return result_of([&] {
         return lib.paged_append(p.h, p.k_pages, p.v_pages, k, v, q, q_out, strides, (const int32_t *)pos, (const int32_t *)p.start,
                                 (const int32_t *)p.len, (const int32_t *)p.table, p.width, p.seqs, tokens, p.stream);
     });
 }
 
-// (h, cfg, k_pages, v_pages, q, seq_start, seq_len, table, out, window, stream)
+// (h, cfg, device, k_pages, v_pages, q, seq_start, seq_len, table, out, window, stream)
 PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Paged p;
     void *q, *out;
     int64_t tokens = -1, stride;
     long window = 0;
     LVR_PLAIN(
-        LVR_NOT_PLAIN(n == 11 && lib.paged_attention && p.begin(a[0], a[1], a[10]) && p.pool(a[2], p.k_pages) && p.pool(a[3], p.v_pages) &&
-                      p.tokens(a[4], p.c->n_q_heads, tokens, q, stride) && p.batch(a[5], a[6], a[7]) &&
-                      p.whole(a[8], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, out) && PyLong_CheckExact(a[9]));
-        window = PyLong_AsLong(a[9]);
+        LVR_NOT_PLAIN(n == 12 && lib.paged_attention && p.begin(a[0], a[1], a[2], a[11]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
+                      p.tokens(a[5], p.c->n_q_heads, tokens, q, stride) && p.batch(a[6], a[7], a[8]) &&
+                      p.whole(a[9], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, out) && PyLong_CheckExact(a[10]));
+        window = PyLong_AsLong(a[10]);
         if (PyErr_Occurred()) PyErr_Clear(), window = -1;
         LVR_NOT_PLAIN(window >= 0 && window <= INT32_MAX);)
     return result_of([&] {
@@ -297,19 +298,19 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// (h, cfg, k_pages, v_pages, seq_len, table, K_out, V_out, stream)
+// (h, cfg, device, k_pages, v_pages, seq_len, table, K_out, V_out, stream)
 PyObject *paged_gather(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Paged p;
     void *K, *V;
     int64_t rows = 0;
     LVR_PLAIN(
-        LVR_NOT_PLAIN(n == 9 && lib.paged_gather && p.begin(a[0], a[1], a[8]) && p.pool(a[2], p.k_pages) && p.pool(a[3], p.v_pages) &&
-                      p.batch(nullptr, a[4], a[5]));
-        const at::Tensor *t = device_tensor(a[6], p.type);
+        LVR_NOT_PLAIN(n == 10 && lib.paged_gather && p.begin(a[0], a[1], a[2], a[9]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
+                      p.batch(nullptr, a[5], a[6]));
+        const at::Tensor *t = device_tensor(a[7], p.type, p.device);
         LVR_NOT_PLAIN(t && t->dim() == 4);
         rows = t->size(2);
         const int64_t shape[4] = {p.seqs, p.c->n_kv_heads, rows, p.c->head_dim};
-        LVR_NOT_PLAIN(p.whole(a[6], p.type, shape, K) && p.whole(a[7], p.type, shape, V));)
+        LVR_NOT_PLAIN(p.whole(a[7], p.type, shape, K) && p.whole(a[8], p.type, shape, V));)
     return result_of([&] {
         return lib.paged_gather(p.h, p.k_pages, p.v_pages, (const int32_t *)p.len, (const int32_t *)p.table, p.width, p.seqs, rows, K, V, p.stream);
     });

@@ -84,7 +84,7 @@ def test_calls_without_a_handle_are_refused(L):
 def test_host_tensors_are_refused(L):
     h = L.PagedHandle()
     h.cfg, h.dtype = L.make_paged_config(**OK), torch.bfloat16
-    h.cfg_at = C.addressof(h.cfg)
+    h.cfg_at, h.device = C.addressof(h.cfg), 0
     pool, kv = torch.zeros(100, 8, 16, 128, dtype=torch.bfloat16), torch.zeros(3, 8, 128, dtype=torch.bfloat16)
     q, i = torch.zeros(3, 32, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
     table = torch.zeros(1, 4, dtype=torch.int32)
