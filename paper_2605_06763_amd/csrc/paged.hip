@@ -92,6 +92,9 @@ struct AppendArgs {
 // copied.  The lanes of a row touch neighbouring pieces in every access.  A lane needs the sines and cosines of E pairs, for all
 // of its rows.  The angle is position times turns per position modulo one turn, which in 64-bit integers is one product with the
 // overflow dropped: no far position loses anything.
+//
+// Bound by HBM where there are tokens enough: 8192 tokens (48 rows each, bf16) 37 us on one axis and 41 on three, 5.4 and 4.9 TB/s read and written;
+// 1885 fp32 tokens of 80 rows 25 us, 6.2 TB/s.  One token: 4.2 us, the launch and three dependent trips (rows and lengths, table, store).
 template <typename KT, bool NEIGHBOURS, int PER, bool STREAM>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_paged_batch b) {
     constexpr int ELT = sizeof(KT) == 4 ? 4 : 2, E = 16 / ELT, LANES = PAIRS / E, ROWS = 64 / LANES;
@@ -173,7 +176,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
 }
 
 // A wave takes 16 rows of one head, which lie in one page: one table entry, then 64 pieces of 16 bytes to an access, one behind the other
-// where the rows are.
+// where the rows are.  131072 keys of 8 heads 191 us, 5.6 TB/s read and written.
 template <typename KT, bool STREAM>
 __global__ void __launch_bounds__(256) paged_gather_kernel(const char *k_pages, const char *v_pages, char *K, char *V, int64_t n,
                                                            int32_t n_kv, lvr_paged_batch b) {

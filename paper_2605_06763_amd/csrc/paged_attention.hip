@@ -15,14 +15,20 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
-// Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.
+// Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.  A piece costs a
+// workgroup's start and, where its tile is cut, a partial result to be written and read; too few leave compute units idle at the end.  us with 256 / 512 /
+// 1024 pieces: tiles of 16 rows: one sequence of 32768 keys 30 / 32 / 36, four ragged ones (32 tiles) 33 / 36 / 41, eight 50 / 45 / 48, 48
+// of them 354 / 300 / 300; tiles of 128: 32 tokens over 131072 keys 169 / 138 / 180, 512 of 8192 121 / 87 / 99, 1000 of 12000 334 / 212 / 219,
+// 1000 of 12000 beside 31 single tokens 418 / 292 / 308, fp32 prompt of 2048 398 / 355 / 342.
 constexpr int ROWS16_PIECES = 512, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 512;
+constexpr int FEW_TILES = 32;   // sequences times KV heads up to which a batch of single tokens makes few pieces
+// Keys of the shortest run.  us with 128 / 256 / 512: one token over 1024 keys 10.9 / 10.2 / 11.9, over 2048 12.1 / 10.9 / 12.3.
 constexpr int MIN_RUN = 256;
 // Rows of a sequence up to which it is taken in tiles of 16.  A wave of a 128-row tile works on 32 of them however many there are, and on
 // fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 57 in a tile of 128 / 46 in four of 16,
 // eight such sequences of 4096 keys 41 / 58; fp32 171 / 98).
 constexpr int NARROW_BF16 = 32, NARROW_F32 = 64;
-constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);
+constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);   // partial results
 constexpr int MERGE_WGS = 1024;
 constexpr int FAN_BITS = 3, FAN = 1 << FAN_BITS;   // partial results of 16-row tiles that a wave merges at a time
 
@@ -94,12 +100,11 @@ __device__ __forceinline__ int token_of(const AttnArgs &a, int row) { return (in
 // up to a.narrow rows are taken in tiles of 16, others in tiles of 128; else all in tiles of 16.
 //
 // A sequence's tiles are cut into runs of keys of one length, as many as make about `target` pieces of the batch (but none under
-// MIN_RUN keys; target 0: no cuts).  L is the keys of all tiles over target, where a tile
-// sees half of the sequence's own new keys.  Tiles of 128 rows are cut into span / L runs, rounded, so that equal ones fill whole
-// rounds of workgroups; beside them tiles of 16 rows, whose partial results are small, into runs of a quarter of that.  Without
-// tiles of 128 rows the number is rounded up.  There is room for the partial results of 2 * target pieces of cut 128-row tiles and
-// for 3 * target pieces of cut tiles altogether, and the launch has as many workgroups beside one for each tile: should there
-// be more, L grows until there are not.
+// MIN_RUN keys; target 0: no cuts).  L is the keys of all tiles over target, where a tile sees half of the sequence's own new keys.
+// Tiles of 128 rows are cut into span / L runs, rounded, so that equal ones fill whole rounds of workgroups; beside them tiles of 16 rows,
+// whose partial results are small, into runs of a quarter of that.  Without tiles of 128 rows the number is rounded up.  There is
+// room for the partial results of 2 * target pieces of cut 128-row tiles and for 3 * target pieces of cut tiles altogether, and the
+// launch has as many workgroups beside one for each tile: should there be more, L grows until there are not.
 template <bool MIXED>
 struct Division {
     const AttnArgs &a;
@@ -339,6 +344,11 @@ __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, i
 // contribute, so key r of the tile is held as V row 4 b + j by the lanes that load it: a row is read whole by 16 lanes, eight
 // coordinates each, and which coordinates share a result tile is free as well (tile u: coordinates 8 i + u).
 // bf16: two score tiles make one operand of 32 keys; a pair of V rows is woven into it by byte permutes.
+//
+// Bound by the read of K and V: 131072 keys of one sequence 99 us, 48 ragged sequences of up to 32768 keys 362 us (1.97 GB), both 5.4 TB/s
+// where a read-only kernel reaches 6.1.  Short contexts are bound by dependent trips: 2048 keys 11 us, of which the launch is 2.4, lengths, table,
+// rows and the products of two turns 5.2, partial results 3.  Rows asked for a turn ahead: no gain (with three workgroups to a compute unit others
+// fill the wait), and fp32 spills; eight waves to a workgroup: 12.1 us at 2048 keys.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <typename KT>
 struct Rows16;
@@ -650,7 +660,15 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 // read transposed (four keys of one coordinate per lane and read).
 // fp32 (tiles of 32 keys): register r is the operand for the keys 8 i + 4 h + j themselves, and a lane's 16-byte read of V holds
 // the coordinates 4 n .. 4 n + 3, one for each of four result tiles.
-// 16-byte pieces of a row are stored at their number xor something of the row's, so that rows do not meet in the same banks.
+// 16-byte pieces of a row are stored at their number xor something of the row's, so that rows do not meet in the same banks (no bank
+// conflicts counted).
+//
+// 32 rows to a wave and two workgroups to a compute unit: 128 KiB of LDS and up to 256 registers a lane, so that one workgroup's matrix
+// instructions meet the other's exponentials.  A prompt of 16384 tokens (32 heads on 8, 2.2 TFLOP): 2.1 to 2.25 ms on different cards, 980 to
+// 1050 TFLOP/s; matrix units busy 46 % and vector units 42 % of the time at 2.2 GHz, where the library's product of 8192 x 8192 matrices reaches
+// 1148 TFLOP/s.  fp32, 8192 tokens: 134 TFLOP/s of the 154 the library reaches.  Tried without gain: the scores of the next tile made
+// between the exponentials of this one (-2 %), wave priorities around the products, tiles through registers (653 TFLOP/s: the loads were
+// waited for at once).
 // ---------------------------------------------------------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -958,7 +976,9 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
     else rows16_piece<KT>(a, bt, t, kvh, lds.narrow);
 }
 
-// Merges the runs of cut 128-row tiles.  16 rows of a tile at a time, 16 lanes to a row; the workgroups share them out.
+// Merges the runs of cut 128-row tiles.  16 rows of a tile at a time, 16 lanes to a row; the workgroups share them out.  A launch of its own, unlike
+// for tiles of 16 rows: a partial result of 128 rows is 66 KiB, and the last workgroup of a tile would read all of them alone.  Bound by that read:
+// 512 partial results (34 MB) 10 us.
 template <typename KT>
 __global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, lvr_paged_batch bt) {
     Division<true> d(a, bt);
@@ -1015,7 +1035,7 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     const int64_t rows = (int64_t)b.n_tokens * a.G;
     a.narrow = bf16 ? NARROW_BF16 : NARROW_F32;
     if (b.n_tokens <= b.n_seqs || rows <= a.narrow) {
-        a.target = (b.n_seqs * a.n_kv <= 32 ? ROWS16_PIECES_FEW : ROWS16_PIECES) / a.n_kv;   // n_kv is at most 256
+        a.target = (b.n_seqs * a.n_kv <= FEW_TILES ? ROWS16_PIECES_FEW : ROWS16_PIECES) / a.n_kv;   // n_kv is at most 256
         const dim3 grid = grid_of(a.n_kv, rows / 16 + b.n_seqs + a.target);
         if (bf16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
         else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
