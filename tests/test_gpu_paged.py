@@ -386,6 +386,21 @@ def test_appends_to_missing_pages_are_dropped():
         check_append(c, f, [0] * 64, 128, L.LVR_ROT_HALVES, None)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs", [L.LVR_ROT_HALVES, L.LVR_ROT_NEIGHBOURS])
+@pytest.mark.parametrize("rot", [64, 128])
+@pytest.mark.parametrize("hq, hkv, lens", [(66, 2, [(150, 200), (0, 7), (1, 90), (89, 89)]), (3, 3, [(1801, 1900), (20, 64)])])
+def test_append_of_many_rows(hq, hkv, lens, rot, pairs, dtype):
+    """At least 16384 rows, from which on a wave takes several and stores around the caches; 70 and 9 rows to a token, no multiple of a wave's."""
+    f = freqs(rot)
+    axis = [i % 3 for i in range(rot // 2)]
+    with Cache(lens, dtype=dtype, hq=hq, hkv=hkv, rot_dim=rot, rot_axes=3, pairs=pairs, inv_freq=f, axis=axis, seed=27, behind=3, gap=2) as c:
+        assert c.T * (hq + 2 * hkv) >= 16384
+        c.table[0, 2], c.table[3 if len(lens) > 2 else 1, 1] = -1, c.n_pages
+        pos = torch.randint(-50, 5000, (c.T, 3), generator=c.g).to(torch.int32)
+        check_append(c, f, axis, rot, pairs, pos)
+
+
 def test_query_is_rotated_in_place():
     f = freqs(128)
     with Cache([(7, 30)], rot_dim=128, inv_freq=f, seed=26) as c:
@@ -414,6 +429,39 @@ def test_gather(page, layout, dtype):
                     want = torch.full((c.hkv, n, D), 7.0, dtype=torch.float64)
                     want[:, :min(held, n)][:, has] = ref[:, has]
                     assert torch.equal(got[b].cpu().double(), want)
+
+
+@pytest.mark.parametrize("dtype, heads", [("bf16", 8), ("f32", 4)])
+@pytest.mark.parametrize("layout", ["head", "token"])
+def test_gather_of_more_than_the_caches_hold(dtype, heads, layout):
+    """3 sequences of up to 32773 rows: past 192 MiB of keys, where the rows are stored around the caches."""
+    n, lens, page = 32773, [32773, 20001, 0], 64
+    dt, g = DTYPES[dtype], torch.Generator(device="cuda").manual_seed(31)
+    used = [-(-x // page) for x in lens]
+    n_pages, width = sum(used) + 1, max(used)
+    assert n * heads * len(lens) * D * dt.itemsize >= 192 << 20
+    say(f"gather n={n} {dtype} heads={heads} {layout}")
+    shape = (n_pages, heads, page, D) if layout == "head" else (n_pages, page, heads, D)
+    kp, vp = (torch.randn(shape, generator=g, device="cuda").to(dt) for _ in range(2))
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(32)).tolist()
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    for b, u in enumerate(used):
+        table[b, :u] = torch.tensor([order.pop() for _ in range(u)], dtype=torch.int32)
+    table[0, 7] = -1
+    h = L.lvr_paged_create(L.make_paged_config(n_q_heads=heads, n_kv_heads=heads, kv_dtype=L.LVR_BF16 if dtype == "bf16" else L.LVR_F32, page_size=page,
+                                               n_pages=n_pages, layout=layout))
+    try:
+        K, V = (torch.full((len(lens), heads, n, D), 7.0, dtype=dt, device="cuda") for _ in range(2))
+        L.lvr_paged_gather(h, kp, vp, torch.tensor(lens, dtype=torch.int32, device="cuda"), table.cuda(), K, V)
+        for got, pool in ((K, kp), (V, vp)):
+            by_head = pool if layout == "head" else pool.transpose(1, 2)
+            for b, x in enumerate(lens):
+                rows = by_head[table[b, :used[b]].long().clamp(min=0).cuda()].transpose(0, 1).reshape(heads, -1, D)[:, :x].clone()
+                if b == 0:
+                    rows[:, 7 * page:8 * page] = 7
+                assert torch.equal(got[b, :, :x], rows) and (got[b, :, x:] == 7).all()
+    finally:
+        L.lvr_paged_destroy(h)
 
 
 # ------------------------------------------------------------------------------------------------ refusals
