@@ -93,7 +93,7 @@ struct AppendArgs {
 // of its rows.  The angle is position times turns per position modulo one turn, which in 64-bit integers is one product with the
 // overflow dropped: no far position loses anything.
 //
-// Bound by HBM where there are tokens enough: 8192 tokens (48 rows each, bf16) 37 us on one axis and 41 on three, 5.4 and 4.9 TB/s read and written;
+// Bound by HBM where there are tokens enough: 8192 tokens (48 rows each, bf16) 37 us on one axis and 41 to 44 on three, 5.4 and 4.6 to 4.9 TB/s read and written;
 // 1885 fp32 tokens of 80 rows 25 us, 6.2 TB/s.  One token: 4.2 us, the launch and three dependent trips (rows and lengths, table, store).
 template <typename KT, bool NEIGHBOURS, int PER, bool STREAM>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_paged_batch b) {

@@ -16,14 +16,15 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
 // Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.  A piece costs a
-// workgroup's start and, where its tile is cut, a partial result to be written and read; too few leave compute units idle at the end.  us with 256 / 512 /
-// 1024 pieces: tiles of 16 rows: one sequence of 32768 keys 30 / 32 / 36, four ragged ones (32 tiles) 33 / 36 / 41, eight 50 / 45 / 48, 48
-// of them 354 / 300 / 300; tiles of 128: 32 tokens over 131072 keys 169 / 138 / 180, 512 of 8192 121 / 87 / 99, 1000 of 12000 334 / 212 / 219,
-// 1000 of 12000 beside 31 single tokens 418 / 292 / 308, fp32 prompt of 2048 398 / 355 / 342.
+// workgroup's start and, where its tile is cut, a partial result to be written and read; too few leave compute units idle at the end.
+// us with 256 / 512 / 1024 pieces (8 KV heads) tiles of 16 rows: one sequence of 32768 keys 28 / 32 / 34, four ragged ones (32 tiles)
+// 32 / 35 / 38, eight 44 / 43 / 42, 48 of them 314 / 296 / 295; tiles of 128: 32 tokens over 131072 keys 165 / 137 / 179, 512 of 8192
+// 120 / 86 / 100, 1000 of 12000 327 / 218 / 225, 1000 of 12000 beside 31 single tokens 419 / 291 / 310, fp32 prompt of 2048 399 / 356 / 341.
 constexpr int ROWS16_PIECES = 512, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 512;
 constexpr int FEW_TILES = 32;   // sequences times KV heads up to which a batch of single tokens makes few pieces
-// Keys of the shortest run.  us with 128 / 256 / 512: one token over 1024 keys 10.9 / 10.2 / 11.9, over 2048 12.1 / 10.9 / 12.3.
-constexpr int MIN_RUN = 256;
+// Keys of the shortest run.  us with 64 / 128 / 256 / 512: one token over 1024 keys 9.3 / 9.9 / 10.9 / 12.2, over 2048 10.0 / 10.3 / 11.3 /
+// 13.3, over 8192 13.2 / 13.2 / 13.2 / 15.0; four prompts of 1024 73.3 / 73.5 / 72.2.
+constexpr int MIN_RUN = 64;
 // Rows of a sequence up to which it is taken in tiles of 16.  A wave of a 128-row tile works on 32 of them however many there are, and on
 // fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 57 in a tile of 128 / 46 in four of 16,
 // eight such sequences of 4096 keys 41 / 58; fp32 171 / 98).
@@ -345,10 +346,9 @@ __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, i
 // coordinates each, and which coordinates share a result tile is free as well (tile u: coordinates 8 i + u).
 // bf16: two score tiles make one operand of 32 keys; a pair of V rows is woven into it by byte permutes.
 //
-// Bound by the read of K and V: 131072 keys of one sequence 99 us, 48 ragged sequences of up to 32768 keys 362 us (1.97 GB), both 5.4 TB/s
-// where a read-only kernel reaches 6.1.  Short contexts are bound by dependent trips: 2048 keys 11 us, of which the launch is 2.4, lengths, table,
-// rows and the products of two turns 5.2, partial results 3.  Rows asked for a turn ahead: no gain (with three workgroups to a compute unit others
-// fill the wait), and fp32 spills; eight waves to a workgroup: 12.1 us at 2048 keys.
+// Bound by the read of K and V: 131072 keys of one sequence 99 us, 48 ragged sequences of up to 32768 keys 362 us (1.97 GB), both 5.4 TB/s.
+// Short contexts are bound by dependent trips (lengths, table, rows, products, partial results): 2048 keys 10 us.  Rows asked for a turn ahead: no
+// gain, and fp32 spills; eight waves to a workgroup: 12.1 us at 2048 keys where four took 11.3.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <typename KT>
 struct Rows16;
@@ -665,7 +665,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 //
 // 32 rows to a wave and two workgroups to a compute unit: 128 KiB of LDS and up to 256 registers a lane, so that one workgroup's matrix
 // instructions meet the other's exponentials.  A prompt of 16384 tokens (32 heads on 8, 2.2 TFLOP): 2.1 to 2.25 ms on different cards, 980 to
-// 1050 TFLOP/s; matrix units busy 46 % and vector units 42 % of the time at 2.2 GHz, where the library's product of 8192 x 8192 matrices reaches
+// 1050 TFLOP/s; matrix units busy 46 % and vector units 42 % of the clocks, where the library's product of 8192 x 8192 matrices reaches
 // 1148 TFLOP/s.  fp32, 8192 tokens: 134 TFLOP/s of the 154 the library reaches.  Tried without gain: the scores of the next tile made
 // between the exponentials of this one (-2 %), wave priorities around the products, tiles through registers (653 TFLOP/s: the loads were
 // waited for at once).
