@@ -9,27 +9,12 @@
 // Softmax in one pass, base 2 (the logit is score * sigma * log2 e in one fused multiply-add with the running maximum).  The
 // maximum is raised, and what was summed so far rescaled, only when a score passes it by more than RAISE: until then
 // weights grow up to 2^RAISE, which costs nothing in fp32 sums, and no lane has to ask another one for a maximum.
-#include "paged.h"
+#include "paged_division.h"
 
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
-// Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.  A piece costs a
-// workgroup's start and, where its tile is cut, a partial result to be written and read; too few leave compute units idle at the end.
-// us with 256 / 512 / 1024 pieces (8 KV heads) tiles of 16 rows: one sequence of 32768 keys 28 / 32 / 34, four ragged ones (32 tiles)
-// 32 / 35 / 38, eight 44 / 43 / 42, 48 of them 314 / 296 / 295; tiles of 128: 32 tokens over 131072 keys 165 / 137 / 179, 512 of 8192
-// 120 / 86 / 100, 1000 of 12000 327 / 218 / 225, 1000 of 12000 beside 31 single tokens 419 / 291 / 310, fp32 prompt of 2048 399 / 356 / 341.
-constexpr int ROWS16_PIECES = 512, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 512;
-constexpr int FEW_TILES = 32;   // sequences times KV heads up to which a batch of single tokens makes few pieces
-// Keys of the shortest run.  us with 64 / 128 / 256 / 512: one token over 1024 keys 9.3 / 9.9 / 10.9 / 12.2, over 2048 10.0 / 10.3 / 11.3 /
-// 13.3, over 8192 13.2 / 13.2 / 13.2 / 15.0; four prompts of 1024 73.3 / 73.5 / 72.2.
-constexpr int MIN_RUN = 64;
-// Rows of a sequence up to which it is taken in tiles of 16.  A wave of a 128-row tile works on 32 of them however many there are, and on
-// fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 57 in a tile of 128 / 46 in four of 16,
-// eight such sequences of 4096 keys 41 / 58; fp32 171 / 98).
-constexpr int NARROW_BF16 = 32, NARROW_F32 = 64;
-constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);   // partial results
 constexpr int MERGE_WGS = 1024;
 constexpr int FAN_BITS = 3, FAN = 1 << FAN_BITS;   // partial results of 16-row tiles that a wave merges at a time
 
@@ -41,32 +26,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const bf16x2 v = {(__bf16)lo, (__bf16)hi};   // rounds to nearest even, NaN stays NaN
     return __builtin_bit_cast(uint32_t, v);
 }
-
-struct AttnArgs {
-    const char *k_pages, *v_pages, *q;
-    char *out;
-    int64_t q_stride;    // bytes per token
-    int32_t n_kv, G, window;
-    uint32_t g_mul;      // row / G = row * g_mul >> g_shift
-    int32_t g_shift;
-    float unit;          // sigma * log2 e
-    int32_t narrow;      // rows of a sequence up to which it is taken in tiles of 16
-    int32_t target;      // pieces of work to make of the batch per KV head; 0: tiles are not cut
-    float *part;
-    uint32_t *ticket;    // a line for each slot of a cut tile
-};
-
-// A piece of work: a tile of TM packed rows of one sequence against a run of the keys they see.
-struct Tile {
-    int height;                // TM: 16 or 128
-    int seq, row0, rows;       // first packed row within the sequence; rows of the sequence
-    int first_token;           // of the sequence, in the packed arrays
-    int pos0;                  // position of the sequence's first new token
-    int lo, hi;                // keys that any row of the tile sees: lo .. hi - 1
-    int begin, end;            // the run
-    int split, splits;         // which run of how many
-    int slot;                  // where its partial result goes, if there is more than one run
-};
 
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp_or_zero(float v) {
@@ -82,171 +41,17 @@ __device__ __forceinline__ float wave_sum(float v) {   // as lvr_wave_inclusive_
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// The division of the batch stands before everything else a workgroup does, in code that is fetched anew by every launch: it is
-// kept short.  a / b is a handful of instructions less where it may be off by one,
-__device__ __forceinline__ int about(int a, int b) { return (int)((float)a * __builtin_amdgcn_rcpf((float)b)); }
-// for quotients below 2^21 one comparison either way puts that right,
-__device__ __forceinline__ int divide_small(int a, int b) {
-    int q = about(a, b);
-    const int r = a - q * b;
-    q += r >= b;
-    q -= r < 0;
-    return q;
-}
-// and for the query heads of a KV head the host has the reciprocal (rows are fewer than 2^28).
-__device__ __forceinline__ int token_of(const AttnArgs &a, int row) { return (int)((uint64_t)(uint32_t)row * a.g_mul >> a.g_shift); }
-
-// How a batch is divided into pieces, for one KV head.  The host knows neither how many tokens a sequence brings nor how many keys it
-// holds, so every workgroup works it out for itself, each wave on its own, a lane to a sequence (64 at a time).  MIXED: sequences of
-// up to a.narrow rows are taken in tiles of 16, others in tiles of 128; else all in tiles of 16.
-//
-// A sequence's tiles are cut into runs of keys of one length, as many as make about `target` pieces of the batch (but none under
-// MIN_RUN keys; target 0: no cuts).  L is the keys of all tiles over target, where a tile sees half of the sequence's own new keys.
-// Tiles of 128 rows are cut into span / L runs, rounded, so that equal ones fill whole rounds of workgroups; beside them tiles of 16 rows,
-// whose partial results are small, into runs of a quarter of that.  Without tiles of 128 rows the number is rounded up.  There is
-// room for the partial results of 2 * target pieces of cut 128-row tiles and for 3 * target pieces of cut tiles altogether, and the
-// launch has as many workgroups beside one for each tile: should there be more, L grows until there are not.
-template <bool MIXED>
-struct Division {
-    const AttnArgs &a;
-    const lvr_paged_batch &b;
-    int G, window, narrow, L;
-    int n_wide;                              // pieces of 128-row tiles, which come first
-    bool any_wide;
-    static constexpr int NO_CUTS = 1 << 30;   // an L
-    int s0, s1, n, tiles, span;              // this lane's sequence
-    int run = 0, runs = 1;
-
-    __device__ __forceinline__ bool wide(int rows) const { return MIXED && rows > narrow; }
-    __device__ __forceinline__ void look(int i) {
-        s0 = s1 = n = tiles = span = 0;
-        if (i < b.n_seqs) {   // whatever the arrays hold, rows stay within the packed arrays and the table
-            s0 = b.seq_start[i];
-            s1 = b.seq_start[i + 1];
-            n = b.seq_len[i];
-            s0 = s0 < 0 ? 0 : (s0 > b.n_tokens ? b.n_tokens : s0);
-            s1 = s1 < s0 ? s0 : (s1 > b.n_tokens ? b.n_tokens : s1);
-            n = n < 0 ? 0 : (n > 1 << 30 ? 1 << 30 : n);
-            const int rows = (s1 - s0) * G;
-            tiles = wide(rows) ? (rows + 127) / 128 : (rows + 15) / 16;
-            const int reach = window ? window + 128 : n;   // keys a tile can see, at most
-            span = n < reach ? n : reach;
-            if (span > b.table_width << b.page_shift) span = b.table_width << b.page_shift;
-            if (span < 1) span = 1;
-        }
-    }
-    __device__ __forceinline__ bool is_wide() const { return wide((s1 - s0) * G); }
-    __device__ __forceinline__ void cut() {
-        runs = 1;
-        if (L == NO_CUTS) return;
-        int L1 = L;
-        if (MIXED && any_wide && !is_wide()) L1 = L1 > 4 * MIN_RUN ? L1 >> 2 : (L1 < MIN_RUN ? L1 : MIN_RUN);
-        if (MIXED) {
-            runs = about(span + (is_wide() ? L1 >> 1 : L1 - 1), L1);
-            if (runs < 1) runs = 1;
-        } else {   // rounded up, and never more than that
-            runs = about(span - 1, L1) + 1;
-            runs -= (runs - 1) * L1 >= span;
-        }
-        run = (about(span, runs) + 64) & ~63;   // the last run takes what is left, whatever was rounded
-    }
-    __device__ __forceinline__ Division(const AttnArgs &args, const lvr_paged_batch &bt) : a(args), b(bt), G(a.G), window(a.window), narrow(a.narrow) {}
-    // false: seq_start is not ascending, no piece is where another expects it
-    __device__ __forceinline__ bool divide(int target) {
-        float keys = 0.f, tokens = 0.f;
-        any_wide = false;
-        for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
-            look(i0 + lvr_lane());
-            const int own = (s1 - s0 < n ? s1 - s0 : n) / 2;
-            tokens += (float)(s1 - s0);
-            any_wide |= __any(is_wide());
-            keys += (float)tiles * (float)(window || !MIXED ? span : span - own);
-        }
-        if (b.n_seqs > 1) {
-            if (wave_sum(tokens) > (float)b.n_tokens) return false;   // whole numbers below 2^24 where it matters
-            keys = wave_sum(keys);
-        } else {
-            keys = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(keys)));
-        }
-        L = NO_CUTS;
-        if (target > 0) {
-            const float want = keys * 1.001f / (float)target;   // (more than what the sum was rounded by)
-            L = want < (float)MIN_RUN ? MIN_RUN : (want > 1e9f ? NO_CUTS : ((int)want + 63) & ~63);
-        }
-        if (!MIXED) {   // at most target pieces more than tiles, and at most 2 * target of cut tiles, since L is all keys over target
-            n_wide = 0;
-            if (b.n_seqs <= 64) cut();
-            return true;
-        }
-        for (;; L = L < 1 << 28 ? (L + L / 2) & ~63 : NO_CUTS) {
-            int cut_wide = 0, cut_narrow = 0;
-            n_wide = 0;
-            for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
-                if (b.n_seqs > 64) look(i0 + lvr_lane());
-                cut();
-                const int cut_here = runs > 1 ? tiles * runs : 0;
-                n_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? tiles * runs : 0), 63);
-                cut_wide += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? cut_here : 0), 63);
-                cut_narrow += __builtin_amdgcn_readlane(lvr_wave_inclusive_sum(is_wide() ? 0 : cut_here), 63);
-            }
-            if (cut_wide <= 2 * target && cut_wide + cut_narrow <= 3 * target) break;   // as it is at the latest without cuts
-        }
-        return true;
-    }
-    // Piece x, or for CUT tile x of the 128-row tiles that are cut (its first run).  Long pieces come first: those of 128-row tiles, of a
-    // sequence's tiles the last ones, and the first runs of all of them before the second ones: a tile's last run is short, and
-    // workgroups that go to one compute unit lie a fixed number apart (fp32 prompt of 2048 tokens, tile by tile 464 us).
-    template <bool CUT>
-    __device__ __forceinline__ bool locate(int x, Tile &t) {
-        int before = 0, cut_before = 0;
-        const bool in_wide = CUT || x < n_wide;
-        if (!in_wide) x -= n_wide;
-        for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
-            if (b.n_seqs > 64) {
-                look(i0 + lvr_lane());
-                cut();
-            }
-            const int pieces = is_wide() == in_wide ? tiles * runs : 0, of_cut = runs > 1 ? pieces : 0;
-            const int count = CUT ? (of_cut ? tiles : 0) : pieces;
-            const int upto = before + lvr_wave_inclusive_sum(count);
-            const int cut_upto = cut_before + lvr_wave_inclusive_sum(of_cut);
-            const uint64_t past = __ballot(upto > x);
-            if (past) {
-                const int at = __builtin_ctzll(past);
-                auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-                const int seq_runs = of(runs), seq_run = of(run);
-                const int seq_tiles = of(tiles), k = x - of(upto - count);   // which of the sequence's pieces, run by run
-                t.split = CUT || seq_runs == 1 ? 0 : divide_small(k, seq_tiles);
-                const int from_last = k - t.split * seq_tiles;
-                t.slot = of(cut_upto - of_cut) + from_last * seq_runs + t.split;
-                t.seq = i0 + at;
-                const int first = of(s0), tokens = of(s1) - first;
-                t.first_token = first;
-                t.rows = tokens * G;
-                t.height = wide(t.rows) ? 128 : 16;
-                t.row0 = (seq_tiles - 1 - from_last) * t.height;
-                t.pos0 = of(n) - tokens;
-                const int last_row = (t.row0 + t.height < t.rows ? t.row0 + t.height : t.rows) - 1;
-                t.hi = t.pos0 + token_of(a, last_row) + 1;
-                if (t.hi > b.table_width << b.page_shift) t.hi = b.table_width << b.page_shift;
-                t.lo = window ? t.pos0 + token_of(a, t.row0) - window + 1 : 0;
-                if (t.lo < 0) t.lo = 0;
-                const int from = t.lo & ~63;
-                t.splits = 1;
-                if (seq_runs > 1 && t.hi > from) {
-                    t.splits = about(t.hi - from - 1, seq_run) + 1;   // the same for all pieces of the tile
-                    if (t.splits > seq_runs) t.splits = seq_runs;
-                }
-                if (t.split >= t.splits) return false;   // a run past what this tile sees
-                t.begin = from + t.split * seq_run;
-                t.end = t.split + 1 < t.splits ? t.begin + seq_run : t.hi;
-                return true;
-            }
-            before = __builtin_amdgcn_readlane(upto, 63);
-            cut_before = __builtin_amdgcn_readlane(cut_upto, 63);
-        }
-        return false;
-    }
+// What the division asks of a wave.
+struct Wave {
+    static constexpr int LANES = 64;
+    static __device__ __forceinline__ int lane() { return lvr_lane(); }
+    static __device__ __forceinline__ bool any(bool v) { return __any(v); }
+    static __device__ __forceinline__ uint64_t ballot(bool v) { return __ballot(v); }
+    static __device__ __forceinline__ float sum(float v) { return wave_sum(v); }
+    static __device__ __forceinline__ int inclusive_sum(int v) { return lvr_wave_inclusive_sum(v); }
+    static __device__ __forceinline__ int of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+    static __device__ __forceinline__ float of_first(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+    static __device__ __forceinline__ float reciprocal(float v) { return __builtin_amdgcn_rcpf(v); }
 };
 
 // Partial results of pieces of cut tiles of HEIGHT rows: per slot and KV head HEIGHT rows of 128 sums, then HEIGHT pairs of maximum
@@ -960,7 +765,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_rows16_kernel(AttnArgs
     __shared__ Rows16Lds lds;
     const int kvh = blockIdx.x;
     Tile t;
-    Division<false> d(a, bt);
+    Division<false, Wave> d(a, bt);
     if (d.divide(a.target) && d.template locate<false>(piece_of_block(), t)) rows16_piece<KT>(a, bt, t, kvh, lds);
 }
 
@@ -970,7 +775,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
     __shared__ union { Rows16Lds narrow; Rows128Lds<KT> wide; } lds;
     const int kvh = blockIdx.x;
     Tile t;
-    Division<true> d(a, bt);
+    Division<true, Wave> d(a, bt);
     if (!d.divide(a.target) || !d.template locate<false>(piece_of_block(), t)) return;
     if (t.height == 128) rows128_piece<KT>(a, bt, t, kvh, lds.wide);
     else rows16_piece<KT>(a, bt, t, kvh, lds.narrow);
@@ -981,7 +786,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
 // 512 partial results (34 MB) 10 us.
 template <typename KT>
 __global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, lvr_paged_batch bt) {
-    Division<true> d(a, bt);
+    Division<true, Wave> d(a, bt);
     if (!d.divide(a.target)) return;
     const int c0 = (threadIdx.x & 15) * 8;
     const int64_t step = (int64_t)a.n_kv * (128 * (LVR_D + 2));
@@ -1022,30 +827,18 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.q = static_cast<const char *>(q);
     a.out = static_cast<char *>(out);
     a.q_stride = q_stride_bytes;
-    a.n_kv = pc->cfg.n_kv_heads;
-    a.G = pc->cfg.n_q_heads / pc->cfg.n_kv_heads;
     a.window = window < 1 << 30 ? window : 0;   // no sequence is longer
-    a.g_shift = 28;
-    while (1 << (a.g_shift - 28) < a.G) ++a.g_shift;
-    a.g_mul = (uint32_t)((((uint64_t)1 << a.g_shift) + a.G - 1) / a.G);
     a.unit = pc->sigma * LOG2E;
     a.part = pc->part;
     a.ticket = pc->ticket;
     const bool bf16 = pc->cfg.kv_dtype == LVR_BF16;
-    const int64_t rows = (int64_t)b.n_tokens * a.G;
-    a.narrow = bf16 ? NARROW_BF16 : NARROW_F32;
-    if (b.n_tokens <= b.n_seqs || rows <= a.narrow) {
-        a.target = (b.n_seqs * a.n_kv <= FEW_TILES ? ROWS16_PIECES_FEW : ROWS16_PIECES) / a.n_kv;   // n_kv is at most 256
-        const dim3 grid = grid_of(a.n_kv, rows / 16 + b.n_seqs + a.target);
+    const PagedLaunch launch = paged_launch(a, b, pc->cfg.n_q_heads, pc->cfg.n_kv_heads, bf16);
+    const dim3 grid = grid_of(a.n_kv, launch.pieces);
+    if (!launch.mixed) {
         if (bf16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
         else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
         return hipGetLastError();
     }
-    a.target = MIXED_PIECES / a.n_kv;
-    // tiles enough to fill the device without cuts, or none longer than the shortest run
-    if (rows / 128 * a.n_kv >= 8 * MIXED_PIECES || b.table_width <= MIN_RUN >> b.page_shift) a.target = 0;
-    // tiles: a sequence's rows over 128 and one more, or at most narrow / 16
-    const dim3 grid = grid_of(a.n_kv, rows / 128 + (int64_t)(a.narrow / 16) * b.n_seqs + 3 * a.target);
     if (bf16) hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
     else hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
     if (a.target > 0) {

@@ -807,3 +807,16 @@ def test_sequences_in_no_order_leave_the_handle_usable():
         L.lvr_paged_attention(c.h, *pools, q, start, odd, table, out)
         L.lvr_paged_attention(c.h, *pools, q, start, length, table, out)
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq, hkv, lens", [
+    (64, 8, [(356, 356)]),
+    (32, 8, [(165, 165)] * 8),
+    (28, 4, [(546, 546)]),
+    (32, 8, [(96, 96), (1, 4000), (338, 352), (400, 400), (130, 131), (1, 1), (200, 900)]),
+])
+def test_prompts_whose_runs_are_made_longer(hq, hkv, lens, dtype):
+    """The shortest runs make more partial results of these than the work space holds (test_paged_division.py has the division itself)."""
+    with Cache(lens, dtype=dtype, hq=hq, hkv=hkv, seed=70) as c:
+        check_attention(c)
