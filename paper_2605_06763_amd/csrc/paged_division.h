@@ -126,7 +126,7 @@ struct Division {
         any_wide = false;
         for (int i0 = 0; i0 < b.n_seqs; i0 += LANES) {
             look(i0 + WAVE::lane());
-            const int own = (s1 - s0 < n ? s1 - s0 : n) / 2;
+            const int own = (s1 - s0 < span ? s1 - s0 : span) / 2;   // (new tokens past the table bring no keys)
             tokens += (float)(s1 - s0);
             any_wide |= WAVE::any(is_wide());
             keys += (float)tiles * (float)(window || !MIXED ? span : span - own);

@@ -820,3 +820,12 @@ def test_prompts_whose_runs_are_made_longer(hq, hkv, lens, dtype):
     """The shortest runs make more partial results of these than the work space holds (test_paged_division.py has the division itself)."""
     with Cache(lens, dtype=dtype, hq=hq, hkv=hkv, seed=70) as c:
         check_attention(c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [0, 100])
+def test_a_chunk_longer_than_twice_its_table(window, dtype):
+    with Cache([(600, 200), (1, 190), (9, 160)], dtype=dtype, seed=71, extra_width=0) as c:
+        c.lens = [(600, 600), (1, 190), (9, 160)]
+        c.len = torch.tensor([600, 190, 160], dtype=torch.int32)
+        check_attention(c, window=window)

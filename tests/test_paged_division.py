@@ -253,3 +253,12 @@ def test_batches_of_every_kind(divide):
         width = rng.choice([pages, pages, pages + 3, max(1, pages // 2), 1, 0])
         batches.append(batch(heads, lens, rng.choice(["bf16", "f32"]), page, rng.choice([0, 0, 1, 50, 3000]), width))
     divide(batches)
+
+
+def test_chunks_longer_than_their_table(divide):
+    """Every sequence counts for the keys it can see: a chunk of more than twice the tokens its table has room for is divided as fast as others, and
+    so are the sequences beside it."""
+    batches = [batch((1, 1), [(5000, 5000)], width=125), batch((1, 1), [(100000, 100000)], width=2500), batch((8, 8), [(30000, 30000), (90, 9000)], width=500),
+               batch((1, 1), [(20000, 20000)] + [(5, 4000)] * 40, width=250), batch((8, 2), [(9000, 2 ** 30)], "f32", width=100)]
+    cases, _, most = divide(batches)
+    assert cases == len(batches) and most <= 2
