@@ -516,11 +516,12 @@ def _pool(h, t, name: str):
         raise ValueError(f"{name} must be {h.dtype}, got {t.dtype}")
     want, shape = tuple(c.page_strides), tuple(t.shape)
     if t.dim() == 4 and t.stride(3) == 1:
-        s = t.stride()
-        if shape == (c.n_pages, c.n_kv_heads, c.page_size, c.head_dim) and s[:3] == want:
-            return t.data_ptr()
-        if shape == (c.n_pages, c.page_size, c.n_kv_heads, c.head_dim) and (s[0], s[2], s[1]) == want:
-            return t.data_ptr()
+        for order in ((0, 1, 2), (0, 2, 1)):   # where the page, the head and the token stand
+            sizes = tuple(shape[i] for i in order)
+            # (the stride of a single page or head says nothing)
+            if sizes + shape[3:] == (c.n_pages, c.n_kv_heads, c.page_size, c.head_dim) and all(
+                    n == 1 or t.stride(i) == s for i, n, s in zip(order, sizes, want)):
+                return t.data_ptr()
     raise ValueError(f"{name} must be {c.n_pages} pages of {c.page_size} tokens and {c.n_kv_heads} heads of {c.head_dim} with strides "
                      f"{want} (page, head, token), got {shape} with strides {tuple(t.stride())}")
 

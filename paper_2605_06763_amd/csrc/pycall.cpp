@@ -212,10 +212,12 @@ struct Paged {
 
     bool pool(PyObject *o, void *&p) const {   // [page][head][token][head_dim], or token before head
         const at::Tensor *t = device_tensor(o, type, device);
-        if (!t || t->dim() != 4 || t->stride(3) != 1 || t->size(0) != c->n_pages || t->size(3) != c->head_dim || t->stride(0) != c->page_strides[0])
-            return false;
-        const bool heads_first = t->size(1) == c->n_kv_heads && t->size(2) == c->page_size && t->stride(1) == c->page_strides[1] && t->stride(2) == c->page_strides[2];
-        const bool tokens_first = t->size(2) == c->n_kv_heads && t->size(1) == c->page_size && t->stride(2) == c->page_strides[1] && t->stride(1) == c->page_strides[2];
+        if (!t || t->dim() != 4 || t->stride(3) != 1 || t->size(3) != c->head_dim) return false;
+        auto is = [&](int dim, int64_t n, int64_t stride) { return t->size(dim) == n && (n == 1 || t->stride(dim) == stride); };   // (that of a single one says nothing)
+        auto in_order = [&](int head, int token) {
+            return is(0, c->n_pages, c->page_strides[0]) && is(head, c->n_kv_heads, c->page_strides[1]) && is(token, c->page_size, c->page_strides[2]);
+        };
+        const bool heads_first = in_order(1, 2), tokens_first = in_order(2, 1);
         p = t->data_ptr();
         return heads_first || tokens_first;
     }

@@ -829,3 +829,22 @@ def test_a_chunk_longer_than_twice_its_table(window, dtype):
         c.lens = [(600, 600), (1, 190), (9, 160)]
         c.len = torch.tensor([600, 190, 160], dtype=torch.int32)
         check_attention(c, window=window)
+
+
+@pytest.mark.parametrize("compiled", [True, False])
+def test_pools_of_one_head_in_any_shape(compiled, monkeypatch):
+    if not compiled:
+        monkeypatch.setattr(L.binding, "_call", None)
+    for layout in ("head", "token"):
+        with Cache([(5, 40), (1, 20)], hq=4, hkv=1, layout=layout, seed=72) as c:
+            q = c.randn(c.T, c.hq, D).cuda()
+            outs = []
+            for shape in ("as it is", "other order", "other stride"):
+                kp, vp = c.K.cuda(), c.V.cuda()      # with one head the memory is the same in both layouts
+                if shape == "other order":
+                    kp, vp = kp.transpose(1, 2), vp.transpose(1, 2)
+                elif shape == "other stride":
+                    kp, vp = (x.as_strided(x.shape, (x.stride(0), 8, D, 1)) for x in (kp, vp))
+                outs.append(torch.empty_like(q))
+                L.lvr_paged_attention(c.h, kp, vp, q, *c.batch(), outs[-1])
+            assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])

@@ -141,3 +141,20 @@ int main() {
                        capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     assert subprocess.run([str(exe)]).returncode == 0
+
+
+def test_the_stride_of_a_single_head_or_page_says_nothing(L, monkeypatch):
+    """A pool of one KV head (or one page) is the same memory whatever stride its only head has: torch's contiguous() leaves it as it is."""
+    monkeypatch.setattr(L.binding, "_tensor", lambda h, t, name: t)
+    h = L.PagedHandle()
+    h.dtype = torch.bfloat16
+    for layout, heads, pages in (("head", 1, 9), ("token", 1, 9), ("token", 1, 1), ("head", 4, 1)):
+        h.cfg = L.make_paged_config(n_q_heads=4, n_kv_heads=heads, page_size=16, n_pages=pages, layout=layout)
+        p = torch.zeros(pages, heads, 16, 128, dtype=torch.bfloat16)
+        views = [p, p.as_strided(p.shape, (p.stride(0) if pages > 1 else 8, p.stride(1) if heads > 1 else 24, 128, 1))]
+        if heads == 1:
+            views += [v.transpose(1, 2).contiguous() for v in views]
+        for v in views:
+            assert L.binding._pool(h, v, "k_pages") == p.data_ptr()
+        with pytest.raises(ValueError):
+            L.binding._pool(h, p.repeat(1, 1, 2, 1)[:, :, ::2], "k_pages")
