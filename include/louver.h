@@ -436,7 +436,7 @@ size_t lvr_paged_bytes(const lvr_paged_config *cfg_host);
 /* Stores the new tokens' K and V in their pages.  K is rotated on the way, and q, if there is one (q_dev
  * and q_out_dev NULL: none), into q_out_dev [n_tokens][n_q_heads][head_dim], contiguous: pair (x, y) of a
  * head becomes (x cos a - y sin a, x sin a + y cos a), a = position[axis] * inv_freq, in fp32 with the
- * angle exact to 2^-32 of a turn, rounded once to the cache's type.  positions_dev [n_tokens][rot_axes] int32, any values; NULL:
+ * angle good to 2^-31 of a turn at any position and frequency, rounded once to the cache's type.  positions_dev [n_tokens][rot_axes] int32, any values; NULL:
  * the token's position in its sequence, on every axis.  token_strides_host = {k, v, q}.  q_out_dev may be
  * q_dev itself where q is contiguous; other overlaps of inputs and outputs are not allowed.  Two tokens of one
  * call must not share a row of a page. */

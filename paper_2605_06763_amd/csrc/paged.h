@@ -1,5 +1,7 @@
 // The paged cache's handle and what its kernels share: where a token, a page and a row lie.
 #pragma once
+#include <math.h>
+
 #include "lvr_internal.h"
 
 #define LVR_PAGED_MAX_SEQS 4096
@@ -28,6 +30,28 @@ size_t lvr_paged_partial_bytes();
 size_t lvr_paged_ticket_bytes();
 hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
                                       int64_t q_stride_bytes, int32_t window, void *out, hipStream_t st);
+
+// A frequency's turns per position, frequency / 2 pi without the whole turns, in units of 2^-64 turn; off by less than one.  With the
+// frequency m * 2^e (m a whole number of 53 bits), bits of 1 / 2 pi above 2^-e make whole turns alone and those 128 further down none that
+// count, so that m times the 128 between them is all there is to it (M. Payne and R. Hanek, "Radian reduction for trigonometric functions", 1983).
+inline uint64_t lvr_turns_of(double inv_freq) {
+    // 1 / 2 pi, 1152 bits behind the point; the largest double needs 971 + 128 of them
+    static const uint64_t per_radian[18] = {
+        0x28be60db9391054a, 0x7f09d5f47d4d3770, 0x36d8a5664f10e410, 0x7f9458eaf7aef158, 0x6dc91b8e909374b8, 0x01924bba82746487,
+        0x3f877ac72c4a69cf, 0xba208d7d4baed121, 0x3a671c09ad17df90, 0x4e64758e60d4ce7d, 0x272117e2ef7e4a0e, 0xc7fe25fff7816603,
+        0xfbcbc462d6829b47, 0xdb4d9fb3c9f2c26d, 0xd3d18fd9a797fa8b, 0x5d49eeb1faf97c5e, 0xcf41ce7de294a4ba, 0x9afed7ec47e35742};
+    typedef unsigned __int128 u128;
+    int e;
+    const uint64_t m = (uint64_t)ldexp(frexp(fabs(inv_freq), &e), 53);
+    e -= 53;
+    const int word = e > 0 ? e / 64 : 0, shift = e > 0 ? e % 64 : 0;
+    auto bits = [&](int i) { return shift ? per_radian[i] << shift | per_radian[i + 1] >> (64 - shift) : per_radian[i]; };
+    const u128 low = (u128)m * bits(word + 1), high = (u128)m * bits(word) + (low >> 64);
+    uint64_t turns;
+    if (e >= 0) turns = (uint64_t)high + ((uint64_t)low >> 63);
+    else turns = e > -128 ? (uint64_t)((high + ((u128)1 << (-e - 1))) >> -e) : 0;
+    return inv_freq < 0 ? 0 - turns : turns;
+}
 
 #ifdef __HIPCC__
 // The page that holds a position of a sequence, or -1: a position outside the table, or an entry outside the pool.

@@ -311,11 +311,7 @@ int lvr_paged_create(const lvr_paged_config *cfg, const double *inv_freq, const 
             if (!isfinite(inv_freq[c])) return LVR_E_INVALID;
             if (axis && (axis[c] < 0 || axis[c] >= cfg->rot_axes)) return LVR_E_INVALID;
             axes[c] = axis ? axis[c] : 0;
-            // turns per position without the whole ones, as a fraction of 2^64 (80-bit arithmetic: off by a unit or two)
-            long double f = (long double)inv_freq[c] / 6.283185307179586476925286766559L;
-            f -= floorl(f);
-            f = ldexpl(f, 64);
-            turns[c] = f >= 18446744073709551615.0L ? 0 : (uint64_t)f;
+            turns[c] = lvr_turns_of(inv_freq[c]);
         }
     }
     lvr_paged *pc = new (std::nothrow) lvr_paged();

@@ -848,3 +848,31 @@ def test_pools_of_one_head_in_any_shape(compiled, monkeypatch):
                 outs.append(torch.empty_like(q))
                 L.lvr_paged_attention(c.h, kp, vp, q, *c.batch(), outs[-1])
             assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_frequencies_of_many_turns_per_position(dtype):
+    """Frequencies up to 1e300 radians per position at the farthest positions; angles reduced in whole numbers for the reference."""
+    from fractions import Fraction
+    bits, term, two_pi, k = 1400, 0, 0, 0
+    for n, c in ((5, 16), (239, -4)):            # pi = 16 atan(1/5) - 4 atan(1/239)
+        term, k = (c << bits) // n, 0
+        while term not in (0, -1):
+            two_pi += 2 * (-(term // (2 * k + 1)) if k % 2 else term // (2 * k + 1))
+            term, k = term // (n * n), k + 1
+    f = [10.0 ** (i / 4) * (-1) ** i for i in range(48)] + [1e6, 1e17, 2.0 ** 80, 3e300] * 4
+    positions = [0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 2, 10 ** 9 + 7, 12345]
+    turns = [[float(Fraction(p * Fraction(x).numerator << bits, Fraction(x).denominator * two_pi) % 1) for x in f] for p in positions]
+    angle = torch.tensor(turns, dtype=torch.float64)[:, None] * (2 * math.pi)
+    with Cache([(8, 8)], dtype=dtype, rot_dim=128, inv_freq=f, seed=73) as c:
+        k, q = c.randn(c.T, c.hkv, D), c.randn(c.T, c.hq, D)
+        kp, vp = c.pools()
+        qo = torch.empty_like(q).cuda()
+        L.lvr_paged_append(c.h, kp, vp, k.cuda(), k.cuda(), *c.batch(), q=q.cuda(), q_out=qo, positions=torch.tensor(positions, dtype=torch.int32, device="cuda")[:, None])
+        kr = c.from_pool(kp)[int(c.table[0, 0]), :, :8].transpose(0, 1)
+        for x, got in ((k, kr), (q, qo.cpu())):
+            u, w = x.double().split(64, dim=2)
+            want = torch.cat([u * angle.cos() - w * angle.sin(), u * angle.sin() + w * angle.cos()], dim=2)
+            size = (u.abs() + w.abs()).repeat(1, 1, 2)
+            # as in check_append; the angle's 2^-31 of a turn are 0.05 of a step of 2^-24 radians
+            assert ((got.double() - want).abs() <= HALF_STEP[dtype] * want.abs() + 12.05 * 2.0 ** -24 * size).all()

@@ -158,3 +158,43 @@ def test_the_stride_of_a_single_head_or_page_says_nothing(L, monkeypatch):
             assert L.binding._pool(h, v, "k_pages") == p.data_ptr()
         with pytest.raises(ValueError):
             L.binding._pool(h, p.repeat(1, 1, 2, 1)[:, :, ::2], "k_pages")
+
+
+def _two_pi(bits):
+    """2 pi * 2^bits: pi = 20 atan(1/7) + 8 atan(3/79), summed in integers."""
+    b = bits + 64
+
+    def atan(p, q):
+        term, k, total = (p << b) // q, 1, 0
+        while term:
+            total += -(term // k) if k % 4 == 3 else term // k
+            term, k = term * p * p // (q * q), k + 2
+        return total
+
+    return (2 * (20 * atan(1, 7) + 8 * atan(3, 79))) >> 64
+
+
+def test_turns_per_position_of_any_frequency(L, tmp_path):
+    """Frequencies become turns per position without the whole ones, to a unit of 2^-64, however many whole ones there are."""
+    import random
+    from fractions import Fraction
+    rng = random.Random(3)
+    freqs = [0.0, 1.0, -1.0, 0.75, 9.5, -9.5, 1e6, 1e17, 1.7976931348623157e308, -1.7976931348623157e308, 5e-324, -5e-324, 1e-300, 2.0 ** 63, 2.0 ** 64 - 2048,
+             6.283185307179586, 6.283185307179587, -6.283185307179586, 10000.0 ** (-1 / 64), 2.0 ** -60, 2.0 ** -64, 2.0 ** 971, 2.0 ** 970 * 1.5]
+    freqs += [rng.choice([1, -1]) * rng.uniform(1, 2) * 2.0 ** rng.uniform(-70, 70) for _ in range(3000)]
+    freqs += [rng.choice([1, -1]) * rng.uniform(1, 2) * 2.0 ** rng.uniform(-1070, 1022) for _ in range(3000)]
+    src, exe = tmp_path / "turns.hip", tmp_path / "turns"
+    src.write_text('#include <cstdio>\n#include "paged.h"\nint main() {\n    double f;\n    while (scanf("%la", &f) == 1) printf("%llu\\n", (unsigned long long)lvr_turns_of(f));\n}\n')
+    from paper_2605_06763_amd.build import CSRC
+    r = subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), "--offload-arch=gfx950", "-O1", "-std=c++17", "-I", CSRC, str(src), "-o", str(exe)],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    got = subprocess.run([str(exe)], input="\n".join(f.hex() for f in freqs), capture_output=True, text=True).stdout.split()
+    assert len(got) == len(freqs)
+    bits = 1300
+    two_pi = _two_pi(bits)
+    for f, g in zip(freqs, got):
+        x = Fraction(f)
+        want = ((x.numerator << (bits + 64)) // (x.denominator * two_pi)) % (1 << 64)
+        off = (int(g) - want) % (1 << 64)
+        assert min(off, (1 << 64) - off) <= 1, (f, int(g), want)
