@@ -876,3 +876,36 @@ def test_frequencies_of_many_turns_per_position(dtype):
             size = (u.abs() + w.abs()).repeat(1, 1, 2)
             # as in check_append; the angle's 2^-31 of a turn are 0.05 of a step of 2^-24 radians
             assert ((got.double() - want).abs() <= HALF_STEP[dtype] * want.abs() + 12.05 * 2.0 ** -24 * size).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_prompt_in_chunks_token_by_token(dtype):
+    """Every chunk's outputs against 64 bits over the rows that append left in the pages, each value within what its own row allows: zeros, a
+    mean of the values and attention without the causal mask are all farther off."""
+    n, hq, hkv, f = 700, 8, 2, freqs(128)
+    with Cache([(n, n)], dtype=dtype, hq=hq, hkv=hkv, rot_dim=128, inv_freq=f, seed=74) as c:
+        k, q = c.randn(n, hkv, D), c.randn(n, hq, D)
+        v = (c.randn(n, hkv, D).float() + 0.5).to(c.dt)
+        kp, vp = c.pools()
+        table, at, got, rotated_q = c.table.cuda(), 0, [], []
+        for m in (1, 130, 17, 300, 252):
+            start = torch.tensor([0, m], dtype=torch.int32, device="cuda")
+            length = torch.tensor([at + m], dtype=torch.int32, device="cuda")
+            qo, out = (torch.empty(m, hq, D, dtype=c.dt, device="cuda") for _ in range(2))
+            L.lvr_paged_append(c.h, kp, vp, k[at:at + m].cuda(), v[at:at + m].cuda(), start, length, table, q=q[at:at + m].cuda(), q_out=qo)
+            L.lvr_paged_attention(c.h, kp, vp, qo, start, length, table, out)
+            got.append(out.cpu().double())
+            rotated_q.append(qo.cpu())
+            at += m
+        got, rotated_q = torch.cat(got), torch.cat(rotated_q)
+        c.K, c.V = c.from_pool(kp), c.from_pool(vp)
+        ref, tol = c.attention(rotated_q, 0)
+        assert ((got - ref).abs() <= tol).all(), float(((got - ref).abs() - tol).max())
+        # the bound tells wrong outputs apart in every row where they differ: the last rows see nearly all keys, the first row one
+        Kc, Vc, _ = c.rows(0, n)
+        Kc, Vc = Kc.repeat_interleave(hq // hkv, dim=0), Vc.repeat_interleave(hq // hkv, dim=0)
+        s = torch.matmul(rotated_q.transpose(0, 1).double(), Kc.transpose(1, 2)) / math.sqrt(D)
+        unmasked = torch.matmul(torch.softmax(s, dim=2), Vc).transpose(0, 1)
+        mean = (Vc.cumsum(dim=1) / torch.arange(1, n + 1)[:, None]).transpose(0, 1)
+        for wrong, rows in ((torch.zeros_like(ref), slice(0, n)), (unmasked, slice(0, n - 50)), (mean, slice(1, n))):
+            assert ((wrong - ref).abs() > tol).any(dim=2)[rows].all()
