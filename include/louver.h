@@ -448,7 +448,7 @@ int lvr_paged_append(lvr_paged *pc, void *k_pages_dev, void *v_pages_dev, const 
 /* Attention of the new tokens over the pages (Sec. 2 "Attention", causal): the token at position p attends the
  * keys at positions 0 .. p of its sequence, or with window > 0 the last `window` of them (window = 0: all;
  * negative: LVR_E_INVALID).  Softmax over those keys of sigma <q, k>; a token with no key to attend gives
- * zeros.  K and V of keys that no token sees may hold anything, infinities and NaN included; a value that is
+ * zeros, and so does one whose every score is minus infinity (in fp32).  K and V of keys that no token sees may hold anything, infinities and NaN included; a value that is
  * infinite or NaN reaches the tokens that see it and no others.
  *   q_dev    [n_tokens][n_q_heads][head_dim] of kv_dtype, q_token_stride elements between tokens
  *   out_dev  [n_tokens][n_q_heads][head_dim] of kv_dtype, contiguous, apart from q

@@ -909,3 +909,36 @@ def test_a_prompt_in_chunks_token_by_token(dtype):
         mean = (Vc.cumsum(dim=1) / torch.arange(1, n + 1)[:, None]).transpose(0, 1)
         for wrong, rows in ((torch.zeros_like(ref), slice(0, n)), (unmasked, slice(0, n - 50)), (mean, slice(1, n))):
             assert ((wrong - ref).abs() > tol).any(dim=2)[rows].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_of_minus_infinity(dtype):
+    """A key whose score is minus infinity has no weight; a token with no other key gives zeros (0 / 0 by the formula), single, in tiles and cut."""
+    lens = [(1, 40), (70, 90), (1, 3000), (130, 2000)]
+    with Cache(lens, dtype=dtype, seed=75) as c:
+        kp, vp = c.pools()
+        q = c.randn(c.T, c.hq, D).abs()
+        start, length, table = c.batch()
+        out = torch.full((c.T, c.hq, D), 7.0, dtype=c.dt, device="cuda")
+        L.lvr_paged_attention(c.h, torch.full_like(kp, -math.inf), vp, q.cuda(), start, length, table, out)
+        assert (out == 0).all()
+    with Cache(lens, dtype=dtype, seed=75) as c:
+        q = c.randn(c.T, c.hq, D).abs() + 0.1
+        c.K[:, :, 1::3, 5] = -math.inf                  # position 0 and others between are as they were
+        kp, vp = c.pools()
+        L.lvr_paged_attention(c.h, kp, vp, q.cuda(), *c.batch(), out)
+        got, t0 = out.cpu().double(), 0
+        for b, (t, n) in enumerate(lens):
+            K, V, _ = c.rows(b, n)
+            finite = torch.where(torch.isfinite(K), K, torch.zeros_like(K))
+            hidden = torch.arange(n)[None] > torch.arange(n - t, n)[:, None]
+            for h in range(c.hq):
+                g, qh = h // (c.hq // c.hkv), q[t0:t0 + t, h].double()
+                w = torch.softmax((qh @ K[g].T * c.scale).masked_fill(hidden, -math.inf), dim=1)
+                ref = w @ V[g]
+                # as in Cache.attention, the scores' size over all keys
+                S = (qh @ finite[g].abs().T * c.scale).amax()
+                weight = 2 * (136 * 2.0 ** -24 * S + 2.0 ** -21) + (1.02 * HALF_STEP[dtype] if dtype == "bf16" else 0)
+                tol = (weight + (n + 64) * 2.0 ** -24) * (w @ V[g].abs() + ref.abs()) + HALF_STEP[dtype] * ref.abs()
+                assert ((got[t0:t0 + t, h] - ref).abs() <= tol).all()
+            t0 += t
