@@ -152,8 +152,8 @@ __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, i
 // bf16: two score tiles make one operand of 32 keys; a pair of V rows is woven into it by byte permutes.
 //
 // Bound by the read of K and V: 131072 keys of one sequence 99 us, 48 ragged sequences of up to 32768 keys 362 us (1.97 GB), both 5.4 TB/s.
-// Short contexts are bound by dependent trips (lengths, table, rows, products, partial results): 2048 keys 10 us.  Rows asked for a turn ahead: no
-// gain, and fp32 spills; eight waves to a workgroup: 12.1 us at 2048 keys where four took 11.3.
+// Short contexts are bound by dependent trips (lengths, table, rows, products, partial results): 2048 keys 10 us, in runs of 64 keys, for which two of the
+// four waves have none.  Rows asked for a turn ahead: no gain, and fp32 spills; eight waves to a workgroup: 12.1 us at 2048 keys where four took 11.3.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <typename KT>
 struct Rows16;
@@ -189,7 +189,9 @@ struct Rows16<lvr_bf16_t> {
             s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[kk]), q[kk], s, 0, 0, 0);
         return s;
     }
-    // o[u] += V^T P^T over the 32 keys; l += the weights as rounded, which is what the second product sees
+    // o[u] += V^T P^T over the 32 keys.  The weights are rounded to bf16, as the matrix instruction takes them beside V (a weight off by up to 2^-8 of
+    // itself; with it outputs are off by 1.9e-3 to 2.4e-3 of their root mean square, 1.6e-3 with fp32 weights, most of both the last rounding); l sums
+    // them as rounded, which is what the second product sees.
     static __device__ __forceinline__ void add(const V &v, const float (&p)[2][4], f32x4 (&o)[8], float &l) {
         uint32_t pw[4] = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
 #pragma unroll
@@ -386,8 +388,8 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     };
     from_lds(4);
     if (t.splits > 1) {
-        // The last workgroup to end of every `fan` of a tile's runs merges those, and the last of these merges what they made: one
-        // compute unit reads some 30 GB/s, so nobody is left with all of them.  Four rows fill a wave, and where a tile has no
+        // The last workgroup to end of every `fan` of a tile's runs merges those, and the last of these merges what they made, so that nobody
+        // is left with all of them (one token over 8192 keys 13.1 us; all merged by one workgroup 15.2).  Four rows fill a wave, and where a tile has no
         // more the waves share the partials out; each takes up to FAN of them with all their loads in flight.  Partials cross
         // from one die to another: they are stored and read with accesses of device scope, and a workgroup waits for its own stores
         // before it takes a ticket, which wraps at the number of those who take it and so is zero again afterwards.
@@ -465,8 +467,8 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 // read transposed (four keys of one coordinate per lane and read).
 // fp32 (tiles of 32 keys): register r is the operand for the keys 8 i + 4 h + j themselves, and a lane's 16-byte read of V holds
 // the coordinates 4 n .. 4 n + 3, one for each of four result tiles.
-// 16-byte pieces of a row are stored at their number xor something of the row's, so that rows do not meet in the same banks (no bank
-// conflicts counted).
+// 16-byte pieces of a row are stored at their number xor something of the row's, so that rows do not meet in the same banks (bf16: no bank
+// conflicts counted; fp32, whose V rows lie as they are: conflicts in 13 % of the clocks that LDS works).
 //
 // 32 rows to a wave and two workgroups to a compute unit: 128 KiB of LDS and up to 256 registers a lane, so that one workgroup's matrix
 // instructions meet the other's exponentials.  A prompt of 16384 tokens (32 heads on 8, 2.2 TFLOP): 2.1 to 2.25 ms on different cards, 980 to
