@@ -166,8 +166,8 @@ def _to_codes(x):
     7 or below, values to the nearest code, ties to the even one.  In the type of x."""
     blocks = x.unflatten(-1, (4, 32))
     m, e = torch.frexp(blocks.abs().amax(dim=-1))
-    e = (e - 3 + (m > 0.875)).clamp(-125, 125)
-    e[m == 0] = -125
+    e = (e - 3 + (m > 0.875)).clamp(-120, 125)
+    e[m == 0] = -120
     t = blocks * _power_of_two(-e, x.dtype)[..., None]
     y = t.abs().clamp_max(6)
     half, one, two = (y * 2).round(), y.round(), (y / 2).round()
@@ -431,7 +431,7 @@ def _nearest(x):
     b = x.reshape(x.shape[:-1] + (4, 32))
     top = b.abs().amax(dim=-1, keepdim=True)
     e = torch.ceil(torch.log2(top.clamp_min(1e-300) / 7))
-    e = torch.where(top > 7 * 2.0 ** e, e + 1, torch.where(top <= 7 * 2.0 ** (e - 1), e - 1, e)).clamp(-125, 125)
+    e = torch.where(top > 7 * 2.0 ** e, e + 1, torch.where(top <= 7 * 2.0 ** (e - 1), e - 1, e)).clamp(-120, 125)
     t = b.abs() / 2.0 ** e
     even = (t > 0.25).int() + (t >= 0.75) + (t > 1.25) + (t >= 1.75) + (t > 2.5) + (t >= 3.5) + (t > 5)
     size = torch.tensor(LEVELS, dtype=torch.float64, device=x.device)[even.long()]
