@@ -36,7 +36,7 @@ extern "C" {
 
 typedef struct lvr_index lvr_index; /* opaque, owned by the library */
 
-enum lvr_dtype { LVR_BF16 = 0, LVR_F32 = 1 };
+enum lvr_dtype { LVR_BF16 = 0, LVR_F32 = 1, LVR_FP4 = 4 /* pages of a paged cache alone, see there */ };
 
 /* How keys are put into groups of r (Def. 2 of the appendix "Ablation on Index Design";
  * the query result does not depend on the choice, only the pruning power does).
@@ -402,7 +402,18 @@ int lvr_length(const lvr_index *ix, int64_t *n_host, int64_t *n_indexed_host);
  * hold then.  n_tokens is the number of rows of the packed arrays (n_tokens times n_q_heads, or 16 if
  * that is more, at most 2^27, LVR_E_CAPACITY beyond); rows are [n_tokens][heads][head_dim] with the stride between tokens (elements)
  * given, heads of a token contiguous, so that q, k and v may be slices of one projection's output.
- * Token strides and page strides are multiples of 16 bytes. */
+ * Token strides and page strides are multiples of 16 bytes.
+ *
+ * kv_dtype LVR_FP4: the pages hold 4 bits a coordinate; new K, V and q, outputs and gathered rows are bf16.  A row is four blocks of
+ * 32 coordinates, each with a scale 2^e: e is the least whole number with A <= 7 * 2^e, A the block's largest magnitude, held to
+ * -120 .. 125, and a coordinate becomes the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e with its sign (between two the one
+ * whose code is even): off by at most 2^e (2^e / 2 below 4 * 2^e, 2^e / 4 below 2 * 2^e).  The codes are those of the exact value: a
+ * row of K is normed and rotated in 64 bits before it is rounded, once.  A block with an infinity or a NaN reads as NaN.  A page is
+ *   codes   n_kv_heads * page_size rows of 64 bytes, [head][token] or [token][head]: coordinate 2 i of a row in the low half of its byte i, 2 i + 1 in
+ *           the high half; a code is the place in the list above, plus 8 for a sign
+ *   scales  behind them, in the same order, 4 bytes a row: the byte of a block is e + 127, 255 for no number
+ * page_strides are bytes then: {page, at least n_kv_heads * page_size * 68; head, token of the codes: 64 * page_size and 64, or 64 and
+ * 64 * n_kv_heads (LVR_E_UNSUPPORTED otherwise)}. */
 typedef struct lvr_paged lvr_paged; /* opaque, owned by the library */
 
 /* Which coordinates are rotated together: HALVES c and c + rot_dim / 2; NEIGHBOURS 2 c and 2 c + 1. */
@@ -412,13 +423,13 @@ typedef struct lvr_paged_config {
     int32_t n_q_heads;    /* H_q, at most 1024                                                       */
     int32_t n_kv_heads;   /* H_kv, divides H_q (any ratio), at most 256                              */
     int32_t head_dim;     /* this build supports 128                                                 */
-    int32_t kv_dtype;     /* lvr_dtype of the pages, of new K, V, q, and of the outputs               */
+    int32_t kv_dtype;     /* lvr_dtype of the pages, of new K, V, q, and of the outputs (LVR_FP4: bf16) */
     int32_t page_size;    /* tokens per page: a power of two, 16 .. 65536                            */
     int32_t rot_dim;      /* leading coordinates that are rotated, a multiple of 16 up to head_dim; 0: none */
     int32_t rot_axes;     /* axes a position has, 1 .. 4 (a text's has one; time, row, column: three)  */
     int32_t rot_pairs;    /* lvr_rot_pairs                                                           */
     int64_t n_pages;      /* pages in each pool, 1 .. 2^30                                           */
-    int64_t page_strides[3]; /* element strides of the pools: page, kv head, token (at most 2^24); head_dim is contiguous */
+    int64_t page_strides[3]; /* element strides of the pools (LVR_FP4: bytes): page, kv head, token (at most 2^24); head_dim is contiguous */
     float scale;          /* sigma; 0 means 1/sqrt(head_dim)                                         */
 } lvr_paged_config;
 
@@ -445,6 +456,16 @@ int lvr_paged_append(lvr_paged *pc, void *k_pages_dev, void *v_pages_dev, const 
                      const int32_t *positions_dev, const int32_t *seq_start_dev, const int32_t *seq_len_dev,
                      const int32_t *table_dev, int64_t table_width, int64_t n_seqs, int64_t n_tokens, void *stream);
 
+/* lvr_paged_append with a norm of every row of K and q in the same pass, before the rotation: x becomes
+ * x / sqrt(mean of x^2 over the head's coordinates + eps) * weight.  q_weight_dev, k_weight_dev: [head_dim] of the type of new rows, the same for
+ * all heads, 16-byte aligned; NULL: ones.  eps >= 0 and finite (LVR_E_INVALID otherwise).  Squares are summed in 64 bits, the rest
+ * is fp32 (64 bits for K on LVR_FP4 pages), rounded once at the end.  V is stored as it is. */
+int lvr_paged_norm_append(lvr_paged *pc, void *k_pages_dev, void *v_pages_dev, const void *k_new_dev, const void *v_new_dev,
+                          const void *q_dev, void *q_out_dev, const int64_t token_strides_host[3], const void *q_weight_dev,
+                          const void *k_weight_dev, float eps, const int32_t *positions_dev, const int32_t *seq_start_dev,
+                          const int32_t *seq_len_dev, const int32_t *table_dev, int64_t table_width, int64_t n_seqs,
+                          int64_t n_tokens, void *stream);
+
 /* Attention of the new tokens over the pages (Sec. 2 "Attention", causal): the token at position p attends the
  * keys at positions 0 .. p of its sequence, or with window > 0 the last `window` of them (window = 0: all;
  * negative: LVR_E_INVALID).  Softmax over those keys of sigma <q, k>; a token with no key to attend gives
@@ -460,6 +481,14 @@ int lvr_paged_attention(lvr_paged *pc, const void *k_pages_dev, const void *v_pa
                         int64_t q_token_stride, const int32_t *seq_start_dev, const int32_t *seq_len_dev,
                         const int32_t *table_dev, int64_t table_width, int64_t n_seqs, int64_t n_tokens, int32_t window,
                         void *out_dev, void *stream);
+
+/* lvr_paged_attention with a window beside which the first `sinks` positions of a sequence stay visible: the token at position p
+ * attends the keys j <= p with j > p - window or j < sinks (window = 0: all; negative window or sinks: LVR_E_INVALID).  Pages
+ * that neither the window nor the first positions reach may be gone from the table; the work does not grow with them. */
+int lvr_paged_sink_attention(lvr_paged *pc, const void *k_pages_dev, const void *v_pages_dev, const void *q_dev,
+                             int64_t q_token_stride, const int32_t *seq_start_dev, const int32_t *seq_len_dev,
+                             const int32_t *table_dev, int64_t table_width, int64_t n_seqs, int64_t n_tokens, int32_t window,
+                             int32_t sinks, void *out_dev, void *stream);
 
 /* The pages' rows as lvr_build reads them: row j of KV head h of sequence b goes to K_out_dev / V_out_dev
  * [n_seqs][n_kv_heads][n][head_dim] (contiguous) for j < min(seq_len[b], n); other rows, and those whose table

@@ -21,14 +21,14 @@ if os.path.exists(CALL_PATH):
         from . import _call
         if _call.TORCH_VERSION != re.match(r"[\d.]*\d", torch.__version__).group():
             raise ImportError(f"built for torch {_call.TORCH_VERSION}, this is {torch.__version__}")
-        if not hasattr(_call, "paged_gather"):
+        if not hasattr(_call, "paged_sink_attention"):
             raise ImportError("built from other sources")
     except ImportError as e:
         _call = None
         warnings.warn(f"{os.path.basename(CALL_PATH)} does not load, calls go through ctypes; build it again "
                       f"(python -m paper_2605_06763_amd.build): {e}")
 
-LVR_BF16, LVR_F32 = 0, 1
+LVR_BF16, LVR_F32, LVR_FP4 = 0, 1, 4
 LVR_GROUP_CONTIGUOUS, LVR_GROUP_TREE, LVR_GROUP_SUBSPACE_TREE = 0, 1, 2
 LVR_ENCLOSE_BALL, LVR_ENCLOSE_AABB = 0, 1
 LVR_ATTEND_BUFFER_DENSE = 1
@@ -86,6 +86,7 @@ EXPORTS = [
     "lvr_subspace_thresholds", "lvr_sparse_attention_static",
     "lvr_set_bound_test", "lvr_stream_read", "lvr_export_labels", "lvr_export_channel_scales",
     "lvr_paged_create", "lvr_paged_destroy", "lvr_paged_bytes", "lvr_paged_append", "lvr_paged_attention", "lvr_paged_gather",
+    "lvr_paged_norm_append", "lvr_paged_sink_attention",
 ]
 
 _lib = None
@@ -145,13 +146,16 @@ def lib():
     L.lvr_paged_bytes.restype = C.c_size_t
     L.lvr_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, C.POINTER(i64), vp, vp, vp, vp, i64, i64, i64, vp]
     L.lvr_paged_attention.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, C.c_int32, vp, vp]
+    L.lvr_paged_norm_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, C.POINTER(i64), vp, vp, C.c_float, vp, vp, vp, vp, i64, i64, i64, vp]
+    L.lvr_paged_sink_attention.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, C.c_int32, C.c_int32, vp, vp]
     L.lvr_paged_gather.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp]
     L.lvr_strerror.argtypes = [C.c_int]
     L.lvr_strerror.restype = C.c_char_p
     L.lvr_last_hip_error.restype = C.c_int
     if _call is not None:
         for name in ("lvr_decode_step", "lvr_append_decode_step", "lvr_query", "lvr_sparse_attention", "lvr_sparse_attention_static",
-                     "lvr_dense_attention", "lvr_paged_append", "lvr_paged_attention", "lvr_paged_gather"):
+                     "lvr_dense_attention", "lvr_paged_append", "lvr_paged_attention", "lvr_paged_gather", "lvr_paged_norm_append",
+                     "lvr_paged_sink_attention"):
             _call.bind(name, C.cast(getattr(L, name), vp).value)
     _lib = L
     return L
@@ -457,20 +461,27 @@ class PagedHandle(C.c_void_p):
     cfg: lvr_paged_config
     cfg_at: int          # its address, for the compiled calls
     device: int          # index of the GPU it was made on
-    dtype: torch.dtype
+    dtype: torch.dtype   # of new rows, queries and outputs
 
 
 def make_paged_config(*, n_q_heads, n_kv_heads, head_dim=128, kv_dtype=LVR_BF16, page_size, n_pages, layout="head", page_strides=None,
                       scale=0.0, rot_dim=0, rot_axes=1, rot_pairs=LVR_ROT_HALVES) -> lvr_paged_config:
     """layout: "head" for pools [page][head][token][head_dim], "token" for [page][token][head][head_dim], both contiguous; or
-    page_strides, the element strides {page, head, token} of pools laid out otherwise."""
+    page_strides, the element strides {page, head, token} of pools laid out otherwise.  kv_dtype LVR_FP4: pools are uint8 [page][bytes]
+    (paged_page_bytes of them), the codes of a page in either order, their scales behind them; page_strides are bytes."""
     if page_strides is None:
         if layout not in ("head", "token"):
             raise ValueError('layout must be "head" or "token"')
-        page = n_kv_heads * page_size * head_dim
-        page_strides = (page, page_size * head_dim, head_dim) if layout == "head" else (page, head_dim, n_kv_heads * head_dim)
+        row = head_dim // 2 if kv_dtype == LVR_FP4 else head_dim
+        page = n_kv_heads * page_size * (row + head_dim // 32 if kv_dtype == LVR_FP4 else row)
+        page_strides = (page, page_size * row, row) if layout == "head" else (page, row, n_kv_heads * row)
     return lvr_paged_config(n_q_heads, n_kv_heads, head_dim, kv_dtype, page_size, rot_dim, rot_axes, rot_pairs, n_pages,
                             (C.c_int64 * 3)(*page_strides), scale)
+
+
+def paged_page_bytes(cfg: lvr_paged_config) -> int:
+    """Bytes of a page of an LVR_FP4 pool: 64 of codes and 4 of scales a row."""
+    return cfg.n_kv_heads * cfg.page_size * (cfg.head_dim // 2 + cfg.head_dim // 32)
 
 
 def lvr_paged_bytes(cfg: lvr_paged_config) -> int:
@@ -491,7 +502,7 @@ def lvr_paged_create(cfg: lvr_paged_config, inv_freq=None, axis=None) -> PagedHa
     h.cfg = lvr_paged_config.from_buffer_copy(cfg)
     h.cfg_at = C.addressof(h.cfg)
     h.device = torch.cuda.current_device()
-    h.dtype = torch.bfloat16 if cfg.kv_dtype == LVR_BF16 else torch.float32
+    h.dtype = torch.float32 if cfg.kv_dtype == LVR_F32 else torch.bfloat16
     return h
 
 
@@ -510,8 +521,17 @@ def _tensor(h, t, name: str) -> torch.Tensor:
 
 
 def _pool(h, t, name: str):
-    """A pool of pages: [page][head][token][head_dim] or [page][token][head][head_dim] with the strides of the configuration."""
+    """A pool of pages: [page][head][token][head_dim] or [page][token][head][head_dim] with the strides of the configuration; of LVR_FP4
+    [page][bytes]."""
     c, t = h.cfg, _tensor(h, t, name)
+    if c.kv_dtype == LVR_FP4:
+        size = paged_page_bytes(c)
+        if t.dtype != torch.uint8:
+            raise ValueError(f"{name} must be {torch.uint8}, got {t.dtype}")
+        if tuple(t.shape) == (c.n_pages, size) and t.stride(1) == 1 and (c.n_pages == 1 or t.stride(0) == c.page_strides[0]):
+            return t.data_ptr()
+        raise ValueError(f"{name} must be {c.n_pages} pages of {size} bytes with a stride of {c.page_strides[0]}, got {tuple(t.shape)} "
+                         f"with strides {tuple(t.stride())}")
     if t.dtype != h.dtype:
         raise ValueError(f"{name} must be {h.dtype}, got {t.dtype}")
     want, shape = tuple(c.page_strides), tuple(t.shape)
@@ -559,28 +579,57 @@ def _batch(h, seq_start, seq_len, table):
     return start, _whole(h, seq_len, torch.int32, (n,), "seq_len"), _whole(h, table, torch.int32, (n, width), "table"), width, n
 
 
+def _append_arrays(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions):
+    kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
+    k, ks, n = _tokens(h, k_new, h.cfg.n_kv_heads, None, "k_new")
+    v, vs, _ = _tokens(h, v_new, h.cfg.n_kv_heads, n, "v_new")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    qp = qo = None
+    qs = 0
+    if q is not None:
+        qp, qs, _ = _tokens(h, q, h.cfg.n_q_heads, n, "q")
+        qo = _whole(h, q_out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "q_out")
+    pos = None if positions is None else _whole(h, positions, torch.int32, (n, max(h.cfg.rot_axes, 1)), "positions")
+    start, length, tab, width, seqs = _batch(h, seq_start, seq_len, table)
+    return (kp, vp, k, v, qp, qo, (C.c_int64 * 3)(ks, vs, qs)), (pos, start, length, tab, width, seqs, n)
+
+
 def lvr_paged_append(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q=None, q_out=None, positions=None, stream=None) -> None:
     """k_new, v_new [n_tokens][n_kv_heads][128], q and q_out [n_tokens][n_q_heads][128] (q_out contiguous, or q itself);
     positions [n_tokens][rot_axes] int32, None: the token's position in its sequence; seq_start, seq_len, table: int32."""
     st = _early_stream(stream)
     code = _call.paged_append(h, h.cfg_at, h.device, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, st) if st is not None else None
     if code is None:   # not all plain tensors of the right kind, or the first call
-        kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
-        k, ks, n = _tokens(h, k_new, h.cfg.n_kv_heads, None, "k_new")
-        v, vs, _ = _tokens(h, v_new, h.cfg.n_kv_heads, n, "v_new")
-        if (q is None) != (q_out is None):
-            raise ValueError("q and q_out go together")
-        qp = qo = None
-        qs = 0
-        if q is not None:
-            qp, qs, _ = _tokens(h, q, h.cfg.n_q_heads, n, "q")
-            qo = _whole(h, q_out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "q_out")
-        pos = None if positions is None else _whole(h, positions, torch.int32, (n, max(h.cfg.rot_axes, 1)), "positions")
-        start, length, tab, width, seqs = _batch(h, seq_start, seq_len, table)
-        code = lib().lvr_paged_append(h, kp, vp, k, v, qp, qo, (C.c_int64 * 3)(ks, vs, qs), pos, start, length, tab, width, seqs, n,
-                                      _stream(stream))
+        rows, batch = _append_arrays(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions)
+        code = lib().lvr_paged_append(h, *rows, *batch, _stream(stream))
     if code != LVR_OK:
         raise LouverError(code, "lvr_paged_append")
+
+
+def lvr_paged_norm_append(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q=None, q_out=None, q_weight=None, k_weight=None,
+                          eps=1e-6, positions=None, stream=None) -> None:
+    """lvr_paged_append with the rows of k_new and q divided by their root mean square first; q_weight, k_weight [128] of their type,
+    None: ones."""
+    st, eps = _early_stream(stream), float(eps)
+    code = _call.paged_norm_append(h, h.cfg_at, h.device, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, st, q_weight,
+                                   k_weight, eps) if st is not None else None
+    if code is None:   # not all plain tensors of the right kind, or the first call
+        rows, batch = _append_arrays(h, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions)
+        weights = [None if w is None else _whole(h, w, h.dtype, (h.cfg.head_dim,), name) for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"))]
+        code = lib().lvr_paged_norm_append(h, *rows, *weights, eps, *batch, _stream(stream))
+    if code != LVR_OK:
+        raise LouverError(code, "lvr_paged_norm_append")
+
+
+def _attention_arrays(h, k_pages, v_pages, q, seq_start, seq_len, table, out, window):
+    kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
+    qp, qs, n = _tokens(h, q, h.cfg.n_q_heads, None, "q")
+    o = _whole(h, out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "out")
+    start, length, tab, width, seqs = _batch(h, seq_start, seq_len, table)
+    if not 0 <= int(window) < 1 << 31:
+        raise ValueError("window must be 0 (all keys) or a number of keys below 2^31")
+    return (kp, vp, qp, qs, start, length, tab, width, seqs, n, int(window)), o
 
 
 def lvr_paged_attention(h, k_pages, v_pages, q, seq_start, seq_len, table, out, window=0, stream=None) -> None:
@@ -588,15 +637,23 @@ def lvr_paged_attention(h, k_pages, v_pages, q, seq_start, seq_len, table, out, 
     st = _early_stream(stream)
     code = _call.paged_attention(h, h.cfg_at, h.device, k_pages, v_pages, q, seq_start, seq_len, table, out, window, st) if st is not None else None
     if code is None:   # not all plain tensors of the right kind, or the first call
-        kp, vp = _pool(h, k_pages, "k_pages"), _pool(h, v_pages, "v_pages")
-        qp, qs, n = _tokens(h, q, h.cfg.n_q_heads, None, "q")
-        o = _whole(h, out, h.dtype, (n, h.cfg.n_q_heads, h.cfg.head_dim), "out")
-        start, length, tab, width, seqs = _batch(h, seq_start, seq_len, table)
-        if not 0 <= int(window) < 1 << 31:
-            raise ValueError("window must be 0 (all keys) or a number of keys below 2^31")
-        code = lib().lvr_paged_attention(h, kp, vp, qp, qs, start, length, tab, width, seqs, n, int(window), o, _stream(stream))
+        arrays, o = _attention_arrays(h, k_pages, v_pages, q, seq_start, seq_len, table, out, window)
+        code = lib().lvr_paged_attention(h, *arrays, o, _stream(stream))
     if code != LVR_OK:
         raise LouverError(code, "lvr_paged_attention")
+
+
+def lvr_paged_sink_attention(h, k_pages, v_pages, q, seq_start, seq_len, table, out, window, sinks, stream=None) -> None:
+    """lvr_paged_attention with a window beside which the first `sinks` positions of every sequence stay visible."""
+    st = _early_stream(stream)
+    code = _call.paged_sink_attention(h, h.cfg_at, h.device, k_pages, v_pages, q, seq_start, seq_len, table, out, window, st, sinks) if st is not None else None
+    if code is None:   # not all plain tensors of the right kind, or the first call
+        arrays, o = _attention_arrays(h, k_pages, v_pages, q, seq_start, seq_len, table, out, window)
+        if not 0 <= int(sinks) < 1 << 31:
+            raise ValueError("sinks must be a number of keys from 0 to below 2^31")
+        code = lib().lvr_paged_sink_attention(h, *arrays, int(sinks), o, _stream(stream))
+    if code != LVR_OK:
+        raise LouverError(code, "lvr_paged_sink_attention")
 
 
 def lvr_paged_gather(h, k_pages, v_pages, seq_len, table, K_out, V_out, stream=None) -> None:

@@ -23,13 +23,19 @@ struct lvr_paged_batch {
     int32_t page_shift;        // log2 of the page size
     int32_t n_pages;
     int64_t page_stride, head_stride, row_stride;   // bytes
+    int64_t scales;            // pages in 4 bits: bytes from a page's start to its scales
 };
+
+// A row in 4 bits: 64 bytes of codes (coordinate 2 i in the low half of byte i) and, elsewhere in its page, the scales of its four blocks of 32.
+#define LVR_FP4_CODES (LVR_D / 2)
+#define LVR_FP4_SCALES (LVR_D / 32)
+struct lvr_fp4_t {};   // the type of such pages, for kernels that are made for each
 
 // work space of the attention, whatever the batch
 size_t lvr_paged_partial_bytes();
 size_t lvr_paged_ticket_bytes();
 hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
-                                      int64_t q_stride_bytes, int32_t window, void *out, hipStream_t st);
+                                      int64_t q_stride_bytes, int32_t window, int32_t sinks, void *out, hipStream_t st);
 
 // A frequency's turns per position, frequency / 2 pi without the whole turns, in units of 2^-64 turn; off by less than one.  With the
 // frequency m * 2^e (m a whole number of 53 bits), bits of 1 / 2 pi above 2^-e make whole turns alone and those 128 further down none that
@@ -63,6 +69,21 @@ __host__ __device__ __forceinline__ int32_t lvr_page_of(const lvr_paged_batch &b
 // Bytes from the start of a pool to the row of a position in that page.
 __host__ __device__ __forceinline__ int64_t lvr_row_at(const lvr_paged_batch &b, int32_t page, int head, int64_t position) {
     return page * b.page_stride + head * b.head_stride + (position & (((int64_t)1 << b.page_shift) - 1)) * b.row_stride;
+}
+// Pages in 4 bits: from the start of a pool to that row's scales.  They lie as the codes do, 4 bytes for every 64.
+__host__ __device__ __forceinline__ int64_t lvr_scales_at(const lvr_paged_batch &b, int32_t page, int head, int64_t position) {
+    const int64_t in_page = head * b.head_stride + (position & (((int64_t)1 << b.page_shift) - 1)) * b.row_stride;
+    return page * b.page_stride + b.scales + in_page / (LVR_FP4_CODES / LVR_FP4_SCALES);
+}
+// What a scale byte stands for, 2^(s - 127); the conversions read the exponent alone, and take that of 255 for no number.
+__device__ __forceinline__ float lvr_fp4_scale(uint32_t s) { return __uint_as_float(s << 23); }
+// Eight codes as bf16, exactly (every product of a code and a scale that lvr_paged_append writes is a normal one).
+typedef __bf16 lvr_bf16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ lvr_bf16x8 lvr_fp4_values(uint32_t codes, float scale) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+    return lvr_bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 // The sequence a row of the packed arrays belongs to: the last one that starts at or before it (an empty one starts where its

@@ -104,16 +104,26 @@ __device__ __forceinline__ void store_row(const AttnArgs &a, const Tile &t, int 
     }
 }
 
-// One query row over the keys k0 .. k0 + run - 1, then `step` further on, and so on before `end`, on the vector units: two coordinates a lane.
+// One query row over the places k0 .. k0 + run - 1, then `step` further on, and so on before `end`, on the vector units: two coordinates a lane.
 // For rows whose neighbours in a tile do not see a value that is infinite or no number: in a matrix product it would reach them
 // with weight zero.
 struct RowSum {
     float m, l, o0, o1;
 };
-template <int ELT>
+// The key at a place, and whether a row that sees first .. last (and the first keys) sees it.
+__device__ __forceinline__ int key_at(const Tile &t, int place) { return place + (place >= t.fold ? t.shift : 0); }
+__device__ __forceinline__ bool hidden(const AttnArgs &a, int key, int first, int last) { return key > last || (key < first && key >= a.sinks); }
+// `size` keys from `key` on: all of them seen by rows that see at least first .. end - 1; one of them by none of the tile's rows.
+__device__ __forceinline__ bool all_seen(const AttnArgs &a, int key, int size, int first, int end) {
+    return key + size <= end && (key >= first || key + size <= a.sinks);
+}
+
+// KT: the type of the pages
+template <typename KT>
 __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, int kvh, int row, int k0, int run, int step) {
     const int lane = lvr_lane(), token = token_of(a, row), head = kvh * a.G + row - token * a.G;
     const int last = t.pos0 + token, first = a.window && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
+    constexpr int ELT = sizeof(KT) == 4 ? 4 : 2;
     auto pair = [&](const char *r) {
         if constexpr (ELT == 2) {
             const uint32_t w = *reinterpret_cast<const uint32_t *>(r + lane * 4);
@@ -125,11 +135,22 @@ __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, i
     const float2 q = pair(a.q + (int64_t)(t.first_token + token) * a.q_stride + (int64_t)head * LVR_D * ELT);
     RowSum s = {-INFINITY, 0.f, 0.f, 0.f};
     for (; k0 < t.end; k0 += step)
-        for (int key = k0; key < k0 + run && key < t.end; ++key) {
-            const int page = key < first || key > last ? -1 : lvr_page_of(bt, t.seq, key);
+        for (int place = k0; place < k0 + run && place < t.end; ++place) {
+            const int key = key_at(t, place);
+            const int page = hidden(a, key, first, last) ? -1 : lvr_page_of(bt, t.seq, key);
             if (page < 0) continue;
             const int64_t at = lvr_row_at(bt, page, kvh, key);
-            const float2 k = pair(a.k_pages + at), v = pair(a.v_pages + at);
+            float2 k, v;
+            if constexpr (__is_same(KT, lvr_fp4_t)) {
+                const int64_t sc = lvr_scales_at(bt, page, kvh, key) + lane / 16;
+                auto two = [&](const char *pages) {
+                    const auto x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint8_t)pages[at + lane], lvr_fp4_scale((uint8_t)pages[sc]), 0);
+                    return make_float2((float)x[0], (float)x[1]);
+                };
+                k = two(a.k_pages), v = two(a.v_pages);
+            } else {
+                k = pair(a.k_pages + at), v = pair(a.v_pages + at);
+            }
             const float x = wave_sum(q.x * k.x + q.y * k.y) * a.unit;
             const float raised = fmaxf(s.m, x);
             const float old = s.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.m - raised);
@@ -169,11 +190,11 @@ struct Rows16<lvr_bf16_t> {
         for (int kk = 0; kk < 4; ++kk)
             q[kk] = row ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(row + kk * 64 + b * 16)) : bf16x8{};
     }
-    static __device__ __forceinline__ void load_k(const char *row, int b, uint4 (&k)[4]) {
+    static __device__ __forceinline__ void load_k(const char *row, const char *, int b, uint4 (&k)[4]) {
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) k[kk] = *reinterpret_cast<const uint4 *>(row + kk * 64 + b * 16);
     }
-    static __device__ __forceinline__ void load_v(const char *row, int i, uint4 &v) { v = *reinterpret_cast<const uint4 *>(row + i * 16); }
+    static __device__ __forceinline__ void load_v(const char *row, const char *, int i, uint4 &v) { v = *reinterpret_cast<const uint4 *>(row + i * 16); }
     static __device__ __forceinline__ void zero_v(uint4 &v) { v = make_uint4(0, 0, 0, 0); }
     static __device__ __forceinline__ bool odd_v(const uint4 &v) {   // an infinity or a NaN among the eight
         bool bad = false;
@@ -224,11 +245,11 @@ struct Rows16<lvr_f32_t> {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) q[kk] = row ? *reinterpret_cast<const float4 *>(row + kk * 64 + b * 16) : make_float4(0, 0, 0, 0);
     }
-    static __device__ __forceinline__ void load_k(const char *row, int b, float4 (&k)[8]) {
+    static __device__ __forceinline__ void load_k(const char *row, const char *, int b, float4 (&k)[8]) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) k[kk] = *reinterpret_cast<const float4 *>(row + kk * 64 + b * 16);
     }
-    static __device__ __forceinline__ void load_v(const char *row, int i, Raw &v) {
+    static __device__ __forceinline__ void load_v(const char *row, const char *, int i, Raw &v) {
         v.a = *reinterpret_cast<const float4 *>(row + i * 16);
         v.b = *reinterpret_cast<const float4 *>(row + 256 + i * 16);
     }
@@ -267,6 +288,48 @@ struct Rows16<lvr_f32_t> {
     static __device__ __forceinline__ int coordinate(int r, int u) { return u < 4 ? 4 * r + u : 64 + 4 * r + u - 4; }
 };
 
+// Pages in 4 bits.  Lanes (i, b) hold block b of a key's row, 32 coordinates with one scale, and of V the eight coordinates that they hold in bf16; both
+// become bf16 in registers, exactly.
+template <>
+struct Rows16<lvr_fp4_t> {
+    static constexpr int ELT = 2;
+    struct Key { uint4 codes; uint32_t scale; };
+    struct Value { uint32_t codes, scale; };
+    typedef bf16x8 Q[4];
+    typedef Key K[2];
+    typedef Value V[2][4];
+    static __device__ __forceinline__ void load_q(const char *row, int b, Q &q) {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+            q[kk] = row ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(row + b * 64 + kk * 16)) : bf16x8{};
+    }
+    static __device__ __forceinline__ void load_k(const char *row, const char *scales, int b, Key &k) {
+        k.codes = *reinterpret_cast<const uint4 *>(row + b * 16);
+        k.scale = (uint8_t)scales[b];
+    }
+    static __device__ __forceinline__ void load_v(const char *row, const char *scales, int i, Value &v) {
+        v.codes = *reinterpret_cast<const uint32_t *>(row + i * 4);
+        v.scale = (uint8_t)scales[i >> 2];
+    }
+    static __device__ __forceinline__ void zero_v(Value &v) { v.codes = 0, v.scale = 127; }
+    static __device__ __forceinline__ bool odd_v(const Value &v) { return v.scale == 255; }
+    static __device__ __forceinline__ f32x4 score(const Key &k, const Q &q) {
+        const float scale = lvr_fp4_scale(k.scale);
+        const uint32_t w[4] = {k.codes.x, k.codes.y, k.codes.z, k.codes.w};
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lvr_fp4_values(w[kk], scale), q[kk], s, 0, 0, 0);
+        return s;
+    }
+    static __device__ __forceinline__ void add(const V &v, const float (&p)[2][4], f32x4 (&o)[8], float &l) {
+        Rows16<lvr_bf16_t>::V wide;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) wide[c >> 2][c & 3] = __builtin_bit_cast(uint4, lvr_fp4_values(v[c >> 2][c & 3].codes, lvr_fp4_scale(v[c >> 2][c & 3].scale)));
+        Rows16<lvr_bf16_t>::add(wide, p, o, l);
+    }
+    static __device__ __forceinline__ int coordinate(int r, int u) { return Rows16<lvr_bf16_t>::coordinate(r, u); }
+};
+
 struct Rows16Lds {
     float m[4][16], l[4][16];
     float o[4][16][LVR_D + 4];
@@ -296,7 +359,8 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 #pragma unroll
     for (int u = 0; u < 8; ++u) o[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    for (int k0 = t.begin + wave * 32; k0 < t.end; k0 += 128) {   // uniform over the wave
+    for (int place = t.begin + wave * 32; place < t.end; place += 128) {   // uniform over the wave
+        const int k0 = key_at(t, place);
         typename R::K k;
         typename R::V v;
         bool none[2];
@@ -307,11 +371,18 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
             none[h] = page < 0;
             const int64_t at = lvr_row_at(bt, none[h] ? 0 : page, kvh, none[h] ? 0 : kt);   // no page: some memory of the pool
             const char *kp = a.k_pages + at, *vp = a.v_pages + at;
-            R::load_k(kp + i * bt.row_stride, b, k[h]);
+            const char *ks = nullptr, *vs = nullptr;
+            int64_t scale_stride = 0;
+            if constexpr (__is_same(KT, lvr_fp4_t)) {
+                const int64_t sc = lvr_scales_at(bt, none[h] ? 0 : page, kvh, none[h] ? 0 : kt);
+                ks = a.k_pages + sc, vs = a.v_pages + sc;
+                scale_stride = bt.row_stride / (LVR_FP4_CODES / LVR_FP4_SCALES);
+            }
+            R::load_k(kp + i * bt.row_stride, ks + i * scale_stride, b, k[h]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) R::load_v(vp + (4 * b + j) * bt.row_stride, i, v[h][j]);
+            for (int j = 0; j < 4; ++j) R::load_v(vp + (4 * b + j) * bt.row_stride, vs + (4 * b + j) * scale_stride, i, v[h][j]);
         }
-        const bool partly = k0 < row_begin || k0 + 32 > row_end || none[0] || none[1];
+        const bool partly = !all_seen(a, k0, 32, row_begin, row_end) || none[0] || none[1];
         float p[2][4];
         bool poison = false;
 #pragma unroll
@@ -322,10 +393,10 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
                 p[h][j] = s[j];
                 if (partly) {
                     const int key = k0 + h * 16 + 4 * b + j;
-                    if (none[h] || key < first || key > last) p[h][j] = -INFINITY;
+                    if (none[h] || hidden(a, key, first, last)) p[h][j] = -INFINITY;
                     // a row of V that no query row sees is memory nobody has written; one that some see meets the others with
                     // weight zero, which an infinity or a NaN would survive
-                    if (none[h] || key < t.lo || key >= t.hi) R::zero_v(v[h][j]);
+                    if (none[h] || hidden(a, key, t.lo, t.hi - 1)) R::zero_v(v[h][j]);
                     else if (R::odd_v(v[h][j])) poison = true;
                 }
             }
@@ -356,7 +427,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     // the four waves' (m, l, o) become the rows' outputs
     if (__any(redo)) {
         for (int r = 0; r < 16 && t.row0 + r < t.rows; ++r) {
-            const RowSum s = one_row<R::ELT>(a, bt, t, kvh, t.row0 + r, t.begin + wave * 32, 32, 128);
+            const RowSum s = one_row<KT>(a, bt, t, kvh, t.row0 + r, t.begin + wave * 32, 32, 128);
             lds.m[wave][r] = s.m;
             lds.l[wave][r] = s.l;
             lds.o[wave][r][2 * lane] = s.o0;
@@ -584,6 +655,10 @@ struct Rows128<lvr_f32_t> {
     }
 };
 
+// Pages in 4 bits: a tile becomes bf16 on its way into LDS and is worked on as such.
+template <>
+struct Rows128<lvr_fp4_t> : Rows128<lvr_bf16_t> {};
+
 // 16 bytes per lane from global memory into LDS, the wave's 1 KiB in a row from `to` on.  vmcnt counts it.
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t offset, char *to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(from + offset),
@@ -630,19 +705,46 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
         k_off[i] = (uint32_t)(R::key_of_k_row(r) - group) * (uint32_t)bt.row_stride + R::k_piece(r, piece) * 16;
         v_off[i] = (uint32_t)(r - group) * (uint32_t)bt.row_stride + R::v_piece(r, piece) * 16;
     }
-    auto pages_of = [&](int k0) {
-        const int key = k0 + 16 * (lane % (TK / 16));
+    auto pages_of = [&](int place) {
+        const int key = key_at(t, place) + 16 * (lane % (TK / 16));
         return key < t.hi ? lvr_page_of(bt, t.seq, key) : -1;
     };
-    auto load = [&](int k0, int pages, int buf) {
+    constexpr bool FP4 = __is_same(KT, lvr_fp4_t);
+    struct { uint32_t k[4], v[4], ks[4], vs[4]; } raw;   // of FP4: a lane's codes (eight of four rows each) and their scales, on their way
+    const int dword = lane % 16, row_of = lane / 16;
+    auto load = [&](int place, int pages, int buf) {
+        const int k0 = key_at(t, place);
         const int page = __builtin_amdgcn_readlane(pages, group / 16);
         const int64_t at = page < 0 ? kvh * bt.head_stride : lvr_row_at(bt, page, kvh, k0 + group);   // no page: some memory of the pool
+        if constexpr (FP4) {
+            const int64_t sc = lvr_scales_at(bt, page < 0 ? 0 : page, kvh, page < 0 ? 0 : k0 + group);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t c = (uint32_t)(4 * i + row_of) * (uint32_t)bt.row_stride;
+                raw.k[i] = *reinterpret_cast<const uint32_t *>(a.k_pages + at + c + dword * 4);
+                raw.v[i] = *reinterpret_cast<const uint32_t *>(a.v_pages + at + c + dword * 4);
+                raw.ks[i] = (uint8_t)a.k_pages[sc + c / 16 + dword / 4];
+                raw.vs[i] = (uint8_t)a.v_pages[sc + c / 16 + dword / 4];
+            }
+            return (uint32_t)__ballot(pages < 0) & ((1u << TK / 16) - 1u);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             load_to_lds(a.k_pages + at, k_off[i], lds.k[buf] + (wave * 4 + i) * 1024);
             load_to_lds(a.v_pages + at, v_off[i], lds.v[buf] + (wave * 4 + i) * 1024);
         }
         return (uint32_t)__ballot(pages < 0) & ((1u << TK / 16) - 1u);   // groups without a page
+    };
+    // Of FP4: what was loaded for the tile at `place`, into LDS.  A row of V that no query row sees may be memory nobody has written.
+    auto unfold = [&](int place, uint32_t none, int buf) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int key = group + 4 * i + row_of, kr = R::key_of_k_row(key);   // (that permutation is its own inverse)
+            *reinterpret_cast<lvr_bf16x8 *>(lds.k[buf] + kr * R::ROWB + R::k_piece(kr, dword) * 16) = lvr_fp4_values(raw.k[i], lvr_fp4_scale(raw.ks[i]));
+            const bool unseen = (none >> (group >> 4) & 1) || hidden(a, key_at(t, place) + key, t.lo, t.hi - 1);
+            *reinterpret_cast<lvr_bf16x8 *>(lds.v[buf] + key * R::ROWB + R::v_piece(key, dword) * 16) =
+                lvr_fp4_values(unseen ? 0u : raw.v[i], unseen ? 1.f : lvr_fp4_scale(raw.vs[i]));
+        }
     };
     auto arrived = [] {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -654,25 +756,28 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
     uint32_t none = 0, next_none = 0;
     if (t.begin < t.end) none = load(t.begin, pages_of(t.begin), 0);
     int pages = pages_of(t.begin + TK);
+    if constexpr (FP4)
+        if (t.begin < t.end) unfold(t.begin, none, 0);
     arrived();
-    for (int k0 = t.begin; k0 < t.end; k0 += TK, buf ^= 1, none = next_none) {   // uniform over the workgroup
-        if (k0 + TK < t.end) {
-            next_none = load(k0 + TK, pages, buf ^ 1);
-            pages = pages_of(k0 + 2 * TK);
+    for (int place = t.begin; place < t.end; place += TK, buf ^= 1, none = next_none) {   // uniform over the workgroup
+        const int k0 = key_at(t, place);
+        if (place + TK < t.end) {
+            next_none = load(place + TK, pages, buf ^ 1);
+            pages = pages_of(place + 2 * TK);
         }
-        if (k0 < t.lo || k0 + TK > t.hi || none != 0) {   // a row of V that no query row sees may be memory nobody has written
+        if (!FP4 && (!all_seen(a, k0, TK, t.lo, t.hi) || none != 0)) {   // a row of V that no query row sees may be memory nobody has written
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int key = srow + i * RPI;
-                if (k0 + key < t.lo || k0 + key >= t.hi || (none >> (key >> 4) & 1))
+                if (hidden(a, k0 + key, t.lo, t.hi - 1) || (none >> (key >> 4) & 1))
                     *reinterpret_cast<uint4 *>(lds.v[buf] + key * R::ROWB + piece * 16) = make_uint4(0, 0, 0, 0);
             }
             arrived();
         }
-        if (k0 < whi && k0 + TK > wlo) {
+        if (k0 < whi && (k0 + TK > wlo || k0 < a.sinks)) {
             f32x16 p[R::NT];
             R::scores(lds.k[buf], q, n, h, p);
-            const bool partly = k0 < all_lo || k0 + TK > all_hi || none != 0;
+            const bool partly = !all_seen(a, k0, TK, all_lo, all_hi) || none != 0;
             if (partly) {
                 asm volatile("");   // a branch, not 32 selects in every tile
 #pragma unroll 1
@@ -682,7 +787,7 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int key = R::key_of(h, kt, r);
-                        if (k0 + key < first || k0 + key > last || (none >> (key >> 4) & 1)) p[kt][r] = -INFINITY;
+                        if (hidden(a, k0 + key, first, last) || (none >> (key >> 4) & 1)) p[kt][r] = -INFINITY;
                     }
             }
             float top = p[0][0];
@@ -706,12 +811,14 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
                 for (int r = 0; r < 16; ++r) p[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[kt][r], a.unit, -base));
             R::add(lds.v[buf], p, lane, o, l);
         }
+        if constexpr (FP4)
+            if (place + TK < t.end) unfold(place + TK, next_none, buf ^ 1);
         arrived();
     }
     l += __shfl_xor(l, 32, 64);
     if (__any(redo)) {
         for (int r = row0; r < row0 + 32 && r < t.rows; ++r) {
-            RowSum s = one_row<R::ELT>(a, bt, t, kvh, r, t.begin, 1 << 30, 1 << 30);
+            RowSum s = one_row<KT>(a, bt, t, kvh, r, t.begin, 1 << 30, 1 << 30);
             if (t.splits > 1) {
                 float *mine = partial<128>(a.part, t.slot, a.n_kv, kvh);
                 *reinterpret_cast<float2 *>(mine + (r - t.row0) * LVR_D + 2 * lane) = make_float2(s.o0, s.o1);
@@ -822,31 +929,37 @@ size_t lvr_paged_partial_bytes() { return ((size_t)WIDE_ROOM * 128 + (size_t)NAR
 size_t lvr_paged_ticket_bytes() { return (size_t)NARROW_ROOM * LVR_CNT_STRIDE * sizeof(uint32_t); }
 
 hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, const void *k_pages, const void *v_pages, const void *q,
-                                      int64_t q_stride_bytes, int32_t window, void *out, hipStream_t st) {
+                                      int64_t q_stride_bytes, int32_t window, int32_t sinks, void *out, hipStream_t st) {
     AttnArgs a;
     a.k_pages = static_cast<const char *>(k_pages);
     a.v_pages = static_cast<const char *>(v_pages);
     a.q = static_cast<const char *>(q);
     a.out = static_cast<char *>(out);
     a.q_stride = q_stride_bytes;
-    a.window = window < 1 << 30 ? window : 0;   // no sequence is longer
+    a.window = (int64_t)window + sinks < 1 << 30 ? window : 0;   // no sequence is longer
+    a.sinks = a.window ? sinks : 0;
     a.unit = pc->sigma * LOG2E;
     a.part = pc->part;
     a.ticket = pc->ticket;
-    const bool bf16 = pc->cfg.kv_dtype == LVR_BF16;
-    const PagedLaunch launch = paged_launch(a, b, pc->cfg.n_q_heads, pc->cfg.n_kv_heads, bf16);
+    const int type = pc->cfg.kv_dtype;
+    const PagedLaunch launch = paged_launch(a, b, pc->cfg.n_q_heads, pc->cfg.n_kv_heads, type != LVR_F32);
     const dim3 grid = grid_of(a.n_kv, launch.pieces);
+#define LVR_BY_TYPE(KERNEL, GRID)                                                                                       \
+    do {                                                                                                                \
+        if (type == LVR_BF16) hipLaunchKernelGGL(KERNEL<lvr_bf16_t>, GRID, dim3(256), 0, st, a, b);                     \
+        else if (type == LVR_F32) hipLaunchKernelGGL(KERNEL<lvr_f32_t>, GRID, dim3(256), 0, st, a, b);                  \
+        else hipLaunchKernelGGL(KERNEL<lvr_fp4_t>, GRID, dim3(256), 0, st, a, b);                                       \
+    } while (0)
     if (!launch.mixed) {
-        if (bf16) hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
-        else hipLaunchKernelGGL(paged_attention_rows16_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
+        LVR_BY_TYPE(paged_attention_rows16_kernel, grid);
         return hipGetLastError();
     }
-    if (bf16) hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_bf16_t>, grid, dim3(256), 0, st, a, b);
-    else hipLaunchKernelGGL(paged_attention_mixed_kernel<lvr_f32_t>, grid, dim3(256), 0, st, a, b);
-    if (a.target > 0) {
+    LVR_BY_TYPE(paged_attention_mixed_kernel, grid);
+#undef LVR_BY_TYPE
+    if (a.target > 0) {   // (what it merges is fp32, what it writes fp32 or bf16)
         const dim3 merge(MERGE_WGS);
-        if (bf16) hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_bf16_t>, merge, dim3(256), 0, st, a, b);
-        else hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_f32_t>, merge, dim3(256), 0, st, a, b);
+        if (type == LVR_F32) hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_f32_t>, merge, dim3(256), 0, st, a, b);
+        else hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_bf16_t>, merge, dim3(256), 0, st, a, b);
     }
     return hipGetLastError();
 }

@@ -26,6 +26,7 @@ struct AttnArgs {
     char *out;
     int64_t q_stride;    // bytes per token
     int32_t n_kv, G, window;
+    int32_t sinks;       // first keys that stay visible beside a window; 0 without one.  window + sinks is at most 2^30
     uint32_t g_mul;      // row / G = row * g_mul >> g_shift
     int32_t g_shift;
     float unit;          // sigma * log2 e
@@ -41,8 +42,9 @@ struct Tile {
     int seq, row0, rows;       // first packed row within the sequence; rows of the sequence
     int first_token;           // of the sequence, in the packed arrays
     int pos0;                  // position of the sequence's first new token
-    int lo, hi;                // keys that any row of the tile sees: lo .. hi - 1
-    int begin, end;            // the run
+    int lo, hi;                // keys that any row of the tile sees: lo .. hi - 1, and those before a.sinks
+    int begin, end;            // the run, of places: place x is key x, or x + shift from `fold` on
+    int fold, shift;           // (both multiples of 64: where the first keys and the window's lie apart, the places skip what is between)
     int split, splits;         // which run of how many
     int slot;                  // where its partial result goes, if there is more than one run
 };
@@ -102,7 +104,7 @@ struct Division {
             n = n < 0 ? 0 : (n > 1 << 30 ? 1 << 30 : n);
             const int rows = (s1 - s0) * G;
             tiles = wide(rows) ? (rows + 127) / 128 : (rows + 15) / 16;
-            const int reach = window ? window + 128 : n;   // keys a tile can see, at most
+            const int reach = window ? window + 128 + ((a.sinks + 63) & ~63) : n;   // keys a tile can see, at most
             span = n < reach ? n : reach;
             if (span > b.table_width << b.page_shift) span = b.table_width << b.page_shift;
             if (span < 1) span = 1;
@@ -204,15 +206,24 @@ struct Division {
                 if (t.hi > b.table_width << b.page_shift) t.hi = b.table_width << b.page_shift;
                 t.lo = window ? t.pos0 + token_of(a, t.row0) - window + 1 : 0;
                 if (t.lo < 0) t.lo = 0;
-                const int from = t.lo & ~63;
+                int from = t.lo & ~63, to = t.hi;
+                t.fold = t.shift = 0;
+                if (a.sinks) {
+                    t.fold = (a.sinks + 63) & ~63;
+                    if (from > t.fold) {
+                        t.shift = from - t.fold;
+                        to = to > from ? to - t.shift : (to < t.fold ? to : t.fold);
+                    }
+                    from = 0;
+                }
                 t.splits = 1;
-                if (seq_runs > 1 && t.hi > from) {
-                    t.splits = about<WAVE>(t.hi - from - 1, seq_run) + 1;   // the same for all pieces of the tile
+                if (seq_runs > 1 && to > from) {
+                    t.splits = about<WAVE>(to - from - 1, seq_run) + 1;   // the same for all pieces of the tile
                     if (t.splits > seq_runs) t.splits = seq_runs;
                 }
                 if (t.split >= t.splits) return false;   // a run past what this tile sees
                 t.begin = from + t.split * seq_run;
-                t.end = t.split + 1 < t.splits ? t.begin + seq_run : t.hi;
+                t.end = t.split + 1 < t.splits ? t.begin + seq_run : to;
                 return true;
             }
             before = WAVE::of(upto, LANES - 1);

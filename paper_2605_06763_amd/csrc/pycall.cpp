@@ -87,6 +87,8 @@ struct {
     decltype(&lvr_paged_append) paged_append;
     decltype(&lvr_paged_attention) paged_attention;
     decltype(&lvr_paged_gather) paged_gather;
+    decltype(&lvr_paged_norm_append) paged_norm_append;
+    decltype(&lvr_paged_sink_attention) paged_sink_attention;
 } lib;
 
 // Runs `call` (which returns an error code) without the GIL.
@@ -210,7 +212,15 @@ struct Paged {
     void *k_pages, *v_pages, *start, *len, *table;
     int64_t width, seqs;
 
-    bool pool(PyObject *o, void *&p) const {   // [page][head][token][head_dim], or token before head
+    bool pool(PyObject *o, void *&p) const {   // [page][head][token][head_dim], or token before head; of LVR_FP4 [page][bytes]
+        if (c->kv_dtype == LVR_FP4) {
+            const at::Tensor *t = device_tensor(o, (int)at::kByte, device);
+            if (!t || t->dim() != 2 || t->size(0) != c->n_pages || t->size(1) != (int64_t)c->n_kv_heads * c->page_size * (c->head_dim / 2 + c->head_dim / 32) ||
+                t->stride(1) != 1 || (c->n_pages > 1 && t->stride(0) != c->page_strides[0]))
+                return false;
+            p = t->data_ptr();
+            return true;
+        }
         const at::Tensor *t = device_tensor(o, type, device);
         if (!t || t->dim() != 4 || t->stride(3) != 1 || t->size(3) != c->head_dim) return false;
         auto is = [&](int dim, int64_t n, int64_t stride) { return t->size(dim) == n && (n == 1 || t->stride(dim) == stride); };   // (that of a single one says nothing)
@@ -257,46 +267,66 @@ struct Paged {
             PyErr_Clear();
             return false;
         }
-        type = (int)(c->kv_dtype == LVR_BF16 ? at::kBFloat16 : at::kFloat);
+        type = (int)(c->kv_dtype == LVR_F32 ? at::kFloat : at::kBFloat16);
         return true;
     }
 };
 
-// (h, cfg, device, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, stream)
+// (h, cfg, device, k_pages, v_pages, k_new, v_new, seq_start, seq_len, table, q, q_out, positions, stream), with NORM also q_weight, k_weight, eps
+template <bool NORM>
 PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Paged p;
-    void *k, *v, *q = nullptr, *q_out = nullptr, *pos = nullptr;
+    void *k, *v, *q = nullptr, *q_out = nullptr, *pos = nullptr, *qw = nullptr, *kw = nullptr;
     int64_t tokens = -1, strides[3] = {0, 0, 0};
     LVR_PLAIN(
-        LVR_NOT_PLAIN(n == 14 && lib.paged_append && p.begin(a[0], a[1], a[2], a[13]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
+        LVR_NOT_PLAIN(n == (NORM ? 17 : 14) && (NORM ? lib.paged_norm_append != nullptr : lib.paged_append != nullptr) && p.begin(a[0], a[1], a[2], a[13]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
                       p.tokens(a[5], p.c->n_kv_heads, tokens, k, strides[0]) && p.tokens(a[6], p.c->n_kv_heads, tokens, v, strides[1]) &&
                       p.batch(a[7], a[8], a[9]) && (a[10] == Py_None) == (a[11] == Py_None));
         if (a[10] != Py_None)
             LVR_NOT_PLAIN(p.tokens(a[10], p.c->n_q_heads, tokens, q, strides[2]) &&
                           p.whole(a[11], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, q_out));
+        if (NORM) {
+            LVR_NOT_PLAIN(PyFloat_CheckExact(a[16]));
+            if (a[14] != Py_None) LVR_NOT_PLAIN(p.whole(a[14], p.type, {(int64_t)p.c->head_dim}, qw));
+            if (a[15] != Py_None) LVR_NOT_PLAIN(p.whole(a[15], p.type, {(int64_t)p.c->head_dim}, kw));
+        }
         if (a[12] != Py_None) LVR_NOT_PLAIN(p.whole(a[12], I32, {tokens, (int64_t)(p.c->rot_axes > 1 ? p.c->rot_axes : 1)}, pos));)
+    const float eps = NORM ? (float)PyFloat_AS_DOUBLE(a[16]) : 0.f;
     return result_of([&] {
+        if (NORM)
+            return lib.paged_norm_append(p.h, p.k_pages, p.v_pages, k, v, q, q_out, strides, qw, kw, eps, (const int32_t *)pos, (const int32_t *)p.start,
+                                         (const int32_t *)p.len, (const int32_t *)p.table, p.width, p.seqs, tokens, p.stream);
         return lib.paged_append(p.h, p.k_pages, p.v_pages, k, v, q, q_out, strides, (const int32_t *)pos, (const int32_t *)p.start,
                                 (const int32_t *)p.len, (const int32_t *)p.table, p.width, p.seqs, tokens, p.stream);
     });
 }
 
-// (h, cfg, device, k_pages, v_pages, q, seq_start, seq_len, table, out, window, stream)
+// A number of keys, 0 .. 2^31 - 1.
+bool keys(PyObject *o, int32_t &n) {
+    if (!PyLong_CheckExact(o)) return false;
+    long v = PyLong_AsLong(o);
+    if (PyErr_Occurred()) PyErr_Clear(), v = -1;
+    n = (int32_t)v;
+    return v >= 0 && v <= INT32_MAX;
+}
+
+// (h, cfg, device, k_pages, v_pages, q, seq_start, seq_len, table, out, window, stream), with SINKS also sinks
+template <bool SINKS>
 PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Paged p;
     void *q, *out;
     int64_t tokens = -1, stride;
-    long window = 0;
+    int32_t window = 0, sinks = 0;
     LVR_PLAIN(
-        LVR_NOT_PLAIN(n == 12 && lib.paged_attention && p.begin(a[0], a[1], a[2], a[11]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
+        LVR_NOT_PLAIN(n == (SINKS ? 13 : 12) && (SINKS ? lib.paged_sink_attention != nullptr : lib.paged_attention != nullptr) && p.begin(a[0], a[1], a[2], a[11]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
                       p.tokens(a[5], p.c->n_q_heads, tokens, q, stride) && p.batch(a[6], a[7], a[8]) &&
-                      p.whole(a[9], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, out) && PyLong_CheckExact(a[10]));
-        window = PyLong_AsLong(a[10]);
-        if (PyErr_Occurred()) PyErr_Clear(), window = -1;
-        LVR_NOT_PLAIN(window >= 0 && window <= INT32_MAX);)
+                      p.whole(a[9], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, out) && keys(a[10], window) && (!SINKS || keys(a[12], sinks)));)
     return result_of([&] {
+        if (SINKS)
+            return lib.paged_sink_attention(p.h, p.k_pages, p.v_pages, q, stride, (const int32_t *)p.start, (const int32_t *)p.len, (const int32_t *)p.table,
+                                            p.width, p.seqs, tokens, window, sinks, out, p.stream);
         return lib.paged_attention(p.h, p.k_pages, p.v_pages, q, stride, (const int32_t *)p.start, (const int32_t *)p.len, (const int32_t *)p.table,
-                                   p.width, p.seqs, tokens, (int32_t)window, out, p.stream);
+                                   p.width, p.seqs, tokens, window, out, p.stream);
     });
 }
 
@@ -328,7 +358,8 @@ PyObject *bind(PyObject *, PyObject *args) {
         {"lvr_query", (void **)&lib.query}, {"lvr_sparse_attention", (void **)&lib.sparse_attention},
         {"lvr_sparse_attention_static", (void **)&lib.sparse_attention_static}, {"lvr_dense_attention", (void **)&lib.dense_attention},
         {"lvr_paged_append", (void **)&lib.paged_append}, {"lvr_paged_attention", (void **)&lib.paged_attention},
-        {"lvr_paged_gather", (void **)&lib.paged_gather}};
+        {"lvr_paged_gather", (void **)&lib.paged_gather}, {"lvr_paged_norm_append", (void **)&lib.paged_norm_append},
+        {"lvr_paged_sink_attention", (void **)&lib.paged_sink_attention}};
     for (auto &f : all)
         if (!strcmp(f.name, name)) {
             *f.slot = (void *)(uintptr_t)at;
@@ -410,8 +441,10 @@ PyMethodDef methods[] = {{"decode_step", (PyCFunction)(void (*)())decode_step, M
                          {"sparse_attention", (PyCFunction)(void (*)())sparse_attention, METH_FASTCALL, nullptr},
                          {"sparse_attention_static", (PyCFunction)(void (*)())sparse_attention_static, METH_FASTCALL, nullptr},
                          {"dense_attention", (PyCFunction)(void (*)())dense_attention, METH_FASTCALL, nullptr},
-                         {"paged_append", (PyCFunction)(void (*)())paged_append, METH_FASTCALL, nullptr},
-                         {"paged_attention", (PyCFunction)(void (*)())paged_attention, METH_FASTCALL, nullptr},
+                         {"paged_append", (PyCFunction)(void (*)())paged_append<false>, METH_FASTCALL, nullptr},
+                         {"paged_attention", (PyCFunction)(void (*)())paged_attention<false>, METH_FASTCALL, nullptr},
+                         {"paged_norm_append", (PyCFunction)(void (*)())paged_append<true>, METH_FASTCALL, nullptr},
+                         {"paged_sink_attention", (PyCFunction)(void (*)())paged_attention<true>, METH_FASTCALL, nullptr},
                          {"paged_gather", (PyCFunction)(void (*)())paged_gather, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
