@@ -18,11 +18,13 @@ constexpr float RAISE = 8.f;
 constexpr int MERGE_WGS = 1024;
 constexpr int FAN_BITS = 3, FAN = 1 << FAN_BITS;   // partial results of 16-row tiles that a wave merges at a time
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const bf16x2 v = {(__bf16)lo, (__bf16)hi};   // rounds to nearest even, NaN stays NaN
     return __builtin_bit_cast(uint32_t, v);
 }
@@ -54,13 +56,9 @@ struct Wave {
     static __device__ __forceinline__ float reciprocal(float v) { return __builtin_amdgcn_rcpf(v); }
 };
 
-// Partial results of pieces of cut tiles of HEIGHT rows: per slot and KV head HEIGHT rows of 128 sums, then HEIGHT pairs of maximum
-// and weight.  Those of 128-row tiles first.
-template <int HEIGHT>
-__device__ __forceinline__ float *partial(float *part, int slot, int n_kv, int kvh) {
-    if (HEIGHT == 16) part += (int64_t)WIDE_ROOM * 128 * (LVR_D + 2);
-    return part + ((int64_t)slot * n_kv + kvh) * (HEIGHT * (LVR_D + 2));
-}
+// Partial results of pieces of cut tiles: per slot and KV head 128 (or 16) rows of 128 sums, then as many pairs of maximum and weight.
+// Those of 128-row tiles first.
+__device__ __forceinline__ float *partial128(float *part, int slot, int n_kv, int kvh) { return part + ((int64_t)slot * n_kv + kvh) * (128 * (LVR_D + 2)); }
 
 // Sums over several sets of keys, brought to a common maximum.
 struct Merged {
@@ -80,13 +78,6 @@ struct Merged {
         for (int e = 0; e < 8; ++e) o[e] = o[e] * old + scale * v[e];
     }
 };
-__device__ __forceinline__ void store_shared(float *p, float2 v) {
-    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 load_shared(const float *p) {
-    return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-}
-
 // Where a packed row's output lies.
 template <int ELT>
 __device__ __forceinline__ char *output_row(const AttnArgs &a, const Tile &t, int kvh, int row) {
@@ -111,15 +102,19 @@ struct RowSum {
     float m, l, o0, o1;
 };
 // The key at a place, and whether a row that sees first .. last (and the first keys) sees it.
-__device__ __forceinline__ int key_at(const Tile &t, int place) { return place + (place >= t.fold ? t.shift : 0); }
-__device__ __forceinline__ bool hidden(const AttnArgs &a, int key, int first, int last) { return key > last || (key < first && key >= a.sinks); }
+// SINKS: there may be first keys that stay visible; the rest is the same without them, and less.
+template <bool SINKS>
+__device__ __forceinline__ int key_at(const Tile &t, int place) { return SINKS ? place + (place >= t.fold ? t.shift : 0) : place; }
+template <bool SINKS>
+__device__ __forceinline__ bool hidden(const AttnArgs &a, int key, int first, int last) { return key > last || (key < first && !(SINKS && key < a.sinks)); }
 // `size` keys from `key` on: all of them seen by rows that see at least first .. end - 1; one of them by none of the tile's rows.
+template <bool SINKS>
 __device__ __forceinline__ bool all_seen(const AttnArgs &a, int key, int size, int first, int end) {
-    return key + size <= end && (key >= first || key + size <= a.sinks);
+    return key + size <= end && (key >= first || (SINKS && key + size <= a.sinks));
 }
 
 // KT: the type of the pages
-template <typename KT>
+template <typename KT, bool SINKS>
 __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, int kvh, int row, int k0, int run, int step) {
     const int lane = lvr_lane(), token = token_of(a, row), head = kvh * a.G + row - token * a.G;
     const int last = t.pos0 + token, first = a.window && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
@@ -136,8 +131,8 @@ __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, i
     RowSum s = {-INFINITY, 0.f, 0.f, 0.f};
     for (; k0 < t.end; k0 += step)
         for (int place = k0; place < k0 + run && place < t.end; ++place) {
-            const int key = key_at(t, place);
-            const int page = hidden(a, key, first, last) ? -1 : lvr_page_of(bt, t.seq, key);
+            const int key = key_at<SINKS>(t, place);
+            const int page = hidden<SINKS>(a, key, first, last) ? -1 : lvr_page_of(bt, t.seq, key);
             if (page < 0) continue;
             const int64_t at = lvr_row_at(bt, page, kvh, key);
             float2 k, v;
@@ -190,11 +185,11 @@ struct Rows16<lvr_bf16_t> {
         for (int kk = 0; kk < 4; ++kk)
             q[kk] = row ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(row + kk * 64 + b * 16)) : bf16x8{};
     }
-    static __device__ __forceinline__ void load_k(const char *row, const char *, int b, uint4 (&k)[4]) {
+    static __device__ __forceinline__ void load_k(const char *row, int b, uint4 (&k)[4]) {
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) k[kk] = *reinterpret_cast<const uint4 *>(row + kk * 64 + b * 16);
     }
-    static __device__ __forceinline__ void load_v(const char *row, const char *, int i, uint4 &v) { v = *reinterpret_cast<const uint4 *>(row + i * 16); }
+    static __device__ __forceinline__ void load_v(const char *row, int i, uint4 &v) { v = *reinterpret_cast<const uint4 *>(row + i * 16); }
     static __device__ __forceinline__ void zero_v(uint4 &v) { v = make_uint4(0, 0, 0, 0); }
     static __device__ __forceinline__ bool odd_v(const uint4 &v) {   // an infinity or a NaN among the eight
         bool bad = false;
@@ -214,9 +209,12 @@ struct Rows16<lvr_bf16_t> {
     // itself; with it outputs are off by 1.9e-3 to 2.4e-3 of their root mean square, 1.6e-3 with fp32 weights, most of both the last rounding); l sums
     // them as rounded, which is what the second product sees.
     static __device__ __forceinline__ void add(const V &v, const float (&p)[2][4], f32x4 (&o)[8], float &l) {
-        uint32_t pw[4] = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
+        const uint32_t pw[4] = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
 #pragma unroll
         for (int c = 0; c < 4; ++c) l += lvr_bf16_lo(pw[c]) + lvr_bf16_hi(pw[c]);
+        add_rounded(v, pw, o);
+    }
+    static __device__ __forceinline__ void add_rounded(const V &v, const uint32_t (&pw)[4], f32x4 (&o)[8]) {
         const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -245,11 +243,11 @@ struct Rows16<lvr_f32_t> {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) q[kk] = row ? *reinterpret_cast<const float4 *>(row + kk * 64 + b * 16) : make_float4(0, 0, 0, 0);
     }
-    static __device__ __forceinline__ void load_k(const char *row, const char *, int b, float4 (&k)[8]) {
+    static __device__ __forceinline__ void load_k(const char *row, int b, float4 (&k)[8]) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) k[kk] = *reinterpret_cast<const float4 *>(row + kk * 64 + b * 16);
     }
-    static __device__ __forceinline__ void load_v(const char *row, const char *, int i, Raw &v) {
+    static __device__ __forceinline__ void load_v(const char *row, int i, Raw &v) {
         v.a = *reinterpret_cast<const float4 *>(row + i * 16);
         v.b = *reinterpret_cast<const float4 *>(row + 256 + i * 16);
     }
@@ -294,25 +292,15 @@ template <>
 struct Rows16<lvr_fp4_t> {
     static constexpr int ELT = 2;
     struct Key { uint4 codes; uint32_t scale; };
-    struct Value { uint32_t codes, scale; };
+    struct Values { uint32_t codes[4], scales; };   // eight coordinates of four keys; the scales of one of them
     typedef bf16x8 Q[4];
     typedef Key K[2];
-    typedef Value V[2][4];
+    typedef Values V[2];
     static __device__ __forceinline__ void load_q(const char *row, int b, Q &q) {
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
             q[kk] = row ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(row + b * 64 + kk * 16)) : bf16x8{};
     }
-    static __device__ __forceinline__ void load_k(const char *row, const char *scales, int b, Key &k) {
-        k.codes = *reinterpret_cast<const uint4 *>(row + b * 16);
-        k.scale = (uint8_t)scales[b];
-    }
-    static __device__ __forceinline__ void load_v(const char *row, const char *scales, int i, Value &v) {
-        v.codes = *reinterpret_cast<const uint32_t *>(row + i * 4);
-        v.scale = (uint8_t)scales[i >> 2];
-    }
-    static __device__ __forceinline__ void zero_v(Value &v) { v.codes = 0, v.scale = 127; }
-    static __device__ __forceinline__ bool odd_v(const Value &v) { return v.scale == 255; }
     static __device__ __forceinline__ f32x4 score(const Key &k, const Q &q) {
         const float scale = lvr_fp4_scale(k.scale);
         const uint32_t w[4] = {k.codes.x, k.codes.y, k.codes.z, k.codes.w};
@@ -321,11 +309,26 @@ struct Rows16<lvr_fp4_t> {
         for (int kk = 0; kk < 4; ++kk) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lvr_fp4_values(w[kk], scale), q[kk], s, 0, 0, 0);
         return s;
     }
+    // The four lanes of a quad, which hold coordinates of the same block, have the scales of a key each.
+    template <int J>
+    static __device__ __forceinline__ float scale_of(float own) {
+        return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(own), J * 0x55, 0xf, 0xf, true));
+    }
+    static __device__ __forceinline__ uint32_t own_scale(const Values &v) { return v.scales >> (threadIdx.x & 12) * 2 & 255; }
     static __device__ __forceinline__ void add(const V &v, const float (&p)[2][4], f32x4 (&o)[8], float &l) {
         Rows16<lvr_bf16_t>::V wide;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) wide[c >> 2][c & 3] = __builtin_bit_cast(uint4, lvr_fp4_values(v[c >> 2][c & 3].codes, lvr_fp4_scale(v[c >> 2][c & 3].scale)));
-        Rows16<lvr_bf16_t>::add(wide, p, o, l);
+        for (int h = 0; h < 2; ++h) {
+            const float own = lvr_fp4_scale(own_scale(v[h]));
+            wide[h][0] = __builtin_bit_cast(uint4, lvr_fp4_values(v[h].codes[0], scale_of<0>(own)));
+            wide[h][1] = __builtin_bit_cast(uint4, lvr_fp4_values(v[h].codes[1], scale_of<1>(own)));
+            wide[h][2] = __builtin_bit_cast(uint4, lvr_fp4_values(v[h].codes[2], scale_of<2>(own)));
+            wide[h][3] = __builtin_bit_cast(uint4, lvr_fp4_values(v[h].codes[3], scale_of<3>(own)));
+        }
+        const uint32_t pw[4] = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[c]), bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
+        Rows16<lvr_bf16_t>::add_rounded(wide, pw, o);
     }
     static __device__ __forceinline__ int coordinate(int r, int u) { return Rows16<lvr_bf16_t>::coordinate(r, u); }
 };
@@ -336,15 +339,15 @@ struct Rows16Lds {
     unsigned arrived;
 };
 
-template <typename KT>
+template <typename KT, bool SINKS>
 __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, Rows16Lds &lds) {
     typedef Rows16<KT> R;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = lvr_lane(), i = lane & 15, b = lane >> 4;
 
-    const int row = t.row0 + i;                      // this lane's query row (column i of the score tiles)
-    const int token = token_of(a, row), head = kvh * a.G + row - token * a.G;
-    const bool has_row = row < t.rows;
+    const int q_row = t.row0 + i;                    // this lane's query row (column i of the score tiles)
+    const int token = token_of(a, q_row), head = kvh * a.G + q_row - token * a.G;
+    const bool has_row = q_row < t.rows;
     typename R::Q q;
     R::load_q(has_row ? a.q + (int64_t)(t.first_token + token) * a.q_stride + (int64_t)head * LVR_D * R::ELT : nullptr, b, q);
     const int last = t.pos0 + token;                 // keys this row sees: first .. last
@@ -359,45 +362,102 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 #pragma unroll
     for (int u = 0; u < 8; ++u) o[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    for (int place = t.begin + wave * 32; place < t.end; place += 128) {   // uniform over the wave
-        const int k0 = key_at(t, place);
+    struct Keys {   // 32 of them on their way
         typename R::K k;
         typename R::V v;
         bool none[2];
+    };
+    constexpr bool FP4 = __is_same(KT, lvr_fp4_t);
+    static_assert(LVR_FP4_CODES / LVR_FP4_SCALES == 16, "");
+    const uint32_t row = (uint32_t)bt.row_stride;
+    uint32_t k_place = i * row + b * 16, k_scale = i * (row / 16) + b, v_place[4], v_scales = (4 * b + (i & 3)) * (row / 16);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {   // 16 keys: one page
-            const int kt = k0 + h * 16;
-            const int page = kt < t.hi ? __builtin_amdgcn_readfirstlane(lvr_page_of(bt, t.seq, kt)) : -1;
-            none[h] = page < 0;
-            const int64_t at = lvr_row_at(bt, none[h] ? 0 : page, kvh, none[h] ? 0 : kt);   // no page: some memory of the pool
-            const char *kp = a.k_pages + at, *vp = a.v_pages + at;
-            const char *ks = nullptr, *vs = nullptr;
-            int64_t scale_stride = 0;
-            if constexpr (__is_same(KT, lvr_fp4_t)) {
-                const int64_t sc = lvr_scales_at(bt, none[h] ? 0 : page, kvh, none[h] ? 0 : kt);
-                ks = a.k_pages + sc, vs = a.v_pages + sc;
-                scale_stride = bt.row_stride / (LVR_FP4_CODES / LVR_FP4_SCALES);
-            }
-            R::load_k(kp + i * bt.row_stride, ks + i * scale_stride, b, k[h]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) R::load_v(vp + (4 * b + j) * bt.row_stride, vs + (4 * b + j) * scale_stride, i, v[h][j]);
+    for (int j = 0; j < 4; ++j) v_place[j] = (4 * b + j) * row + i * 4;
+    const int first_place = t.begin + wave * 32, turns = first_place < t.end ? (t.end - first_place + 127) / 128 : 0;
+    auto key_of_turn = [&](int turn) { return key_at<SINKS>(t, first_place + turn * 128); };
+    // The pages of 32 turns are looked up at once, by one lane for each 16 keys, which lie in one page.  Where there is none, some memory of the pool.
+    struct {
+        int page;                   // or, of FP4, what is added to a pool's address for the codes (low, high), and to that for the scales
+        uint32_t low, high;
+        int32_t scales;
+    } place_of = {};
+    uint64_t without = 0;           // (FP4) which of them have no page
+    auto look_up = [&](int turn) {
+        const int place = first_place + (turn + (lane >> 1)) * 128;
+        const int key = place < t.end ? key_at<SINKS>(t, place) + (lane & 1) * 16 : t.hi;
+        place_of.page = key < t.hi ? lvr_page_of(bt, t.seq, key) : -1;
+        if constexpr (FP4) {        // a page is at most 2^30 bytes of codes
+            const uint32_t in_page = (uint32_t)kvh * (uint32_t)bt.head_stride + ((uint32_t)key & ((1u << bt.page_shift) - 1)) * row;
+            const bool none = place_of.page < 0;
+            const uint64_t at = none ? 0 : (uint64_t)(uint32_t)place_of.page * (uint64_t)bt.page_stride + in_page;
+            place_of.low = (uint32_t)at;
+            place_of.high = (uint32_t)(at >> 32);
+            place_of.scales = (int32_t)bt.scales + (none ? 0 : (int32_t)(in_page / 16) - (int32_t)in_page);
+            without = __ballot(none);
         }
-        const bool partly = !all_seen(a, k0, 32, row_begin, row_end) || none[0] || none[1];
+    };
+    auto ask = [&](int turn, Keys &x) {
+        if (FP4 && turn >= turns) turn = turns - 1;
+        if ((turn & 31) == 0) look_up(turn);
+        const int k0 = key_of_turn(turn);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int who = 2 * (turn & 31) + h;
+            if constexpr (FP4) {
+                // One address for the wave and a lane's 32-bit place behind it, in the load itself (the places are made opaque here, or they are widened
+                // before the loop and added up in registers that loads are on their way to).
+                x.none[h] = without >> who & 1;
+                const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place_of.high, who) << 32 | (uint32_t)__builtin_amdgcn_readlane(place_of.low, who);
+                const int32_t scales = __builtin_amdgcn_readlane(place_of.scales, who);
+                const char *kp = a.k_pages + at, *vp = a.v_pages + at, *ks = kp + scales, *vs = vp + scales;
+                asm volatile("" : "+v"(k_place), "+v"(k_scale), "+v"(v_scales));
+                x.k[h].codes = *reinterpret_cast<const uint4 *>(kp + k_place);
+                x.k[h].scale = (uint8_t)ks[k_scale];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    asm volatile("" : "+v"(v_place[j]));
+                    x.v[h].codes[j] = *reinterpret_cast<const uint32_t *>(vp + v_place[j]);
+                }
+                x.v[h].scales = *reinterpret_cast<const uint32_t *>(vs + v_scales);
+            } else {
+                const int page = __builtin_amdgcn_readlane(place_of.page, who);
+                x.none[h] = page < 0;
+                const int64_t at = lvr_row_at(bt, x.none[h] ? 0 : page, kvh, x.none[h] ? 0 : k0 + h * 16);
+                const char *kp = a.k_pages + at, *vp = a.v_pages + at;
+                R::load_k(kp + i * bt.row_stride, b, x.k[h]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) R::load_v(vp + (4 * b + j) * bt.row_stride, i, x.v[h][j]);
+            }
+        }
+    };
+    auto work = [&](int k0, Keys &x) {
+        const bool partly = !all_seen<SINKS>(a, k0, 32, row_begin, row_end) || x.none[0] || x.none[1];
         float p[2][4];
         bool poison = false;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const f32x4 s = R::score(k[h], q);
+            const f32x4 s = R::score(x.k[h], q);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                p[h][j] = s[j];
-                if (partly) {
+            for (int j = 0; j < 4; ++j) p[h][j] = s[j];
+        }
+        if (partly) {
+            if (FP4) asm volatile("");   // one branch
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
                     const int key = k0 + h * 16 + 4 * b + j;
-                    if (none[h] || hidden(a, key, first, last)) p[h][j] = -INFINITY;
+                    if (x.none[h] || hidden<SINKS>(a, key, first, last)) p[h][j] = -INFINITY;
                     // a row of V that no query row sees is memory nobody has written; one that some see meets the others with
                     // weight zero, which an infinity or a NaN would survive
-                    if (none[h] || hidden(a, key, t.lo, t.hi - 1)) R::zero_v(v[h][j]);
-                    else if (R::odd_v(v[h][j])) poison = true;
+                    const bool unseen = x.none[h] || hidden<SINKS>(a, key, t.lo, t.hi - 1);
+                    if constexpr (FP4) x.v[h].codes[j] = unseen ? 0 : x.v[h].codes[j];
+                    else if (unseen) R::zero_v(x.v[h][j]);
+                    else if (R::odd_v(x.v[h][j])) poison = true;
+                }
+                if constexpr (FP4) {   // the key whose scales this lane has
+                    if (x.none[h] || hidden<SINKS>(a, k0 + h * 16 + 4 * b + (i & 3), t.lo, t.hi - 1)) x.v[h].scales = 0x7f7f7f7f;
+                    else if (R::own_scale(x.v[h]) == 255) poison = true;
                 }
             }
         }
@@ -419,7 +479,31 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 #pragma unroll
         for (int c = 0; c < 8; ++c) p[c >> 2][c & 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[c >> 2][c & 3], a.unit, -base));
         redo |= poison;
-        R::add(v, p, o, l);
+        R::add(x.v, p, o, l);
+    };
+    if constexpr (!FP4) {
+        for (int turn = 0; turn < turns; ++turn) {   // uniform over the wave
+            Keys x;
+            ask(turn, x);
+            work(key_of_turn(turn), x);
+        }
+    } else if (turns > 0) {
+        // Rows are asked for two turns ahead.  The last turns ask for rows that are there already, so that there are always as many loads
+        // behind the ones that are waited for.
+        Keys x, y, z;
+        ask(0, x);
+        ask(1, y);
+        for (int turn = 0;;) {
+            ask(turn + 2, z);
+            work(key_of_turn(turn), x);
+            if (++turn >= turns) break;
+            ask(turn + 2, x);
+            work(key_of_turn(turn), y);
+            if (++turn >= turns) break;
+            ask(turn + 2, y);
+            work(key_of_turn(turn), z);
+            if (++turn >= turns) break;
+        }
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
@@ -427,7 +511,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     // the four waves' (m, l, o) become the rows' outputs
     if (__any(redo)) {
         for (int r = 0; r < 16 && t.row0 + r < t.rows; ++r) {
-            const RowSum s = one_row<KT>(a, bt, t, kvh, t.row0 + r, t.begin + wave * 32, 32, 128);
+            const RowSum s = one_row<KT, SINKS>(a, bt, t, kvh, t.row0 + r, t.begin + wave * 32, 32, 128);
             lds.m[wave][r] = s.m;
             lds.l[wave][r] = s.l;
             lds.o[wave][r][2 * lane] = s.o0;
@@ -444,81 +528,82 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
             for (int u = 0; u < 8; u += 4)
                 *reinterpret_cast<float4 *>(&lds.o[wave][i][R::coordinate(4 * b + c, u)]) = make_float4(o[u][c], o[u + 1][c], o[u + 2][c], o[u + 3][c]);
     }
-    __syncthreads();
     const int r = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 8;
     const bool writes = t.row0 + r < t.rows;
+    // The last workgroup to end of every `fan` of a tile's runs merges those, and the last of these merges what they made, so that nobody
+    // is left with all of them (one token over 8192 keys 13.1 us; all merged by one workgroup 15.2).  Four rows fill a wave, and where a tile has no
+    // more the waves share the partials out; each takes up to FAN of them with all their loads in flight.  Partials cross
+    // from one die to another: they are stored and read with accesses of device scope, and a workgroup waits for its own stores
+    // before it takes a ticket, which wraps at the number of those who take it and so is zero again afterwards.
+    // All of this is code that one workgroup in many runs, and fetches as it goes: it is kept short.
+    const int rows = t.rows - t.row0, sharer_bits = rows <= 4 ? 2 : (rows <= 8 ? 1 : 0), sharers = 1 << sharer_bits, fan = FAN * sharers;
+    const int slot0 = t.slot - t.split, fans = (t.splits + fan - 1) >> (FAN_BITS + sharer_bits), mine = t.split >> (FAN_BITS + sharer_bits);
+    const int levels = t.splits == 1 ? 0 : (fans == 1 ? 1 : 2);
+    int slot = t.slot, first_slot = slot0 + mine * fan, apart = 1, n = mine + 1 < fans ? fan : t.splits - mine * fan;
+    const uint32_t part_size = 16 * (LVR_D + 2) * sizeof(float);
+    const auto parts = __builtin_amdgcn_make_buffer_rsrc(a.part + (int64_t)WIDE_ROOM * 128 * (LVR_D + 2), 0, NARROW_ROOM * part_size, 0x00027000);
+    constexpr int DEVICE = 16;   // sc1
     Merged x;
-    auto from_lds = [&](int n) {   // the sums of n sets of keys
-        x.clear();
-        for (int w = 0; w < n; ++w) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = lds.o[w][r][c0 + e];
-            x.add(lds.m[w][r], lds.l[w][r], v);
-        }
-    };
-    from_lds(4);
-    if (t.splits > 1) {
-        // The last workgroup to end of every `fan` of a tile's runs merges those, and the last of these merges what they made, so that nobody
-        // is left with all of them (one token over 8192 keys 13.1 us; all merged by one workgroup 15.2).  Four rows fill a wave, and where a tile has no
-        // more the waves share the partials out; each takes up to FAN of them with all their loads in flight.  Partials cross
-        // from one die to another: they are stored and read with accesses of device scope, and a workgroup waits for its own stores
-        // before it takes a ticket, which wraps at the number of those who take it and so is zero again afterwards.
-        const int rows = t.rows - t.row0, sharer_bits = rows <= 4 ? 2 : (rows <= 8 ? 1 : 0), sharers = 1 << sharer_bits, fan = FAN * sharers;
-        const int slot0 = t.slot - t.split, fans = (t.splits + fan - 1) >> (FAN_BITS + sharer_bits), mine = t.split >> (FAN_BITS + sharer_bits);
-        const int in_mine = mine + 1 < fans ? fan : t.splits - mine * fan;
-        float *first_part = partial<16>(a.part, slot0, a.n_kv, kvh);
-        const int64_t step = (int64_t)a.n_kv * (16 * (LVR_D + 2));
-        auto put = [&](float *p) {
-            if (!writes) return;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) store_shared(p + r * LVR_D + c0 + e, make_float2(x.o[e], x.o[e + 1]));
-            if (c0 == 0) store_shared(p + 16 * LVR_D + r * 2, make_float2(x.m, x.l));
-        };
-        auto last_of = [&](int slot, int word, int n) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    int sets = 4;
+#pragma unroll 1
+    for (int level = 0;; ++level) {
+        if (level == 0 || sharers > 1) {   // the sums of the waves' sets of keys, or of their shares
             __syncthreads();
-            if (threadIdx.x == 0) lds.arrived = atomicInc(a.ticket + ((int64_t)slot * a.n_kv + kvh) * LVR_CNT_STRIDE + word, (unsigned)n - 1u);
-            __syncthreads();
-            return lds.arrived == (unsigned)n - 1u;
-        };
-        auto merge = [&](const float *p, int64_t apart, int n) {
-            const int share = wave >> (2 - sharer_bits), mr = (wave & ((4 >> sharer_bits) - 1)) * 4 + (lane >> 4);   // whose turn, which row
             x.clear();
-            for (int p0 = share; p0 < n; p0 += fan) {
-                float2 ml[FAN], v[FAN][4];
+            for (int w = 0; w < sets; ++w) {
+                float v[8];
 #pragma unroll
-                for (int k = 0; k < FAN; ++k) {   // past the last one the last once more
-                    const float *from = p + (p0 + k * sharers < n ? p0 + k * sharers : n - 1) * apart;
-                    ml[k] = load_shared(from + 16 * LVR_D + mr * 2);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[k][e] = load_shared(from + mr * LVR_D + c0 + 2 * e);
-                }
-#pragma unroll
-                for (int k = 0; k < FAN; ++k) {
-                    if (p0 + k * sharers >= n || mr >= rows) continue;   // (rows that are none hold anything)
-                    const float y[8] = {v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y, v[k][2].x, v[k][2].y, v[k][3].x, v[k][3].y};
-                    x.add(ml[k].x, ml[k].y, y);
-                }
+                for (int e = 0; e < 8; ++e) v[e] = lds.o[w][r][c0 + e];
+                x.add(lds.m[w][r], lds.l[w][r], v);
             }
-            if (sharers == 1) return;
+        }
+        if (level == levels) break;
+        if (writes) {
+            const uint32_t at = (slot * a.n_kv + kvh) * part_size;
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{x.o[0], x.o[1], x.o[2], x.o[3]}), parts, (r * LVR_D + c0) * 4, at, DEVICE);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{x.o[4], x.o[5], x.o[6], x.o[7]}), parts, (r * LVR_D + c0) * 4 + 16, at, DEVICE);
+            if (c0 == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(x.m), __float_as_uint(x.l)}, parts, (16 * LVR_D + r * 2) * 4, at, DEVICE);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) lds.arrived = atomicInc(a.ticket + ((int64_t)first_slot * a.n_kv + kvh) * LVR_CNT_STRIDE + level, (unsigned)n - 1u);
+        __syncthreads();
+        if (lds.arrived != (unsigned)n - 1u) return;
+        const int share = wave >> (2 - sharer_bits), mr = (wave & ((4 >> sharer_bits) - 1)) * 4 + (lane >> 4);   // whose turn, which row
+        x.clear();
+#pragma unroll 1
+        for (int p0 = share; p0 < n; p0 += fan) {
+            u32x2 ml[FAN];
+            u32x4 v[FAN][2];
+#pragma unroll
+            for (int k = 0; k < FAN; ++k) {   // past the last one the last once more
+                const uint32_t at = ((first_slot + (p0 + k * sharers < n ? p0 + k * sharers : n - 1) * apart) * a.n_kv + kvh) * part_size;
+                ml[k] = __builtin_amdgcn_raw_buffer_load_b64(parts, (16 * LVR_D + mr * 2) * 4, at, DEVICE);
+                v[k][0] = __builtin_amdgcn_raw_buffer_load_b128(parts, (mr * LVR_D + c0) * 4, at, DEVICE);
+                v[k][1] = __builtin_amdgcn_raw_buffer_load_b128(parts, (mr * LVR_D + c0) * 4 + 16, at, DEVICE);
+            }
+            asm volatile("" ::: "memory");   // all of them asked for before one is waited for
+#pragma unroll
+            for (int k = 0; k < FAN; ++k) {   // (rows that are none hold anything, and go nowhere)
+                if (p0 + k * sharers >= n) break;
+                const f32x4 y0 = __builtin_bit_cast(f32x4, v[k][0]), y1 = __builtin_bit_cast(f32x4, v[k][1]);
+                const float y[8] = {y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
+                x.add(__uint_as_float(ml[k][0]), __uint_as_float(ml[k][1]), y);
+            }
+        }
+        if (sharers > 1) {
             if (c0 == 0) {
                 lds.m[share][mr] = x.m;
                 lds.l[share][mr] = x.l;
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) lds.o[share][mr][c0 + e] = x.o[e];
-            __syncthreads();
-            from_lds(sharers);
-        };
-        put(first_part + t.split * step);
-        if (!last_of(slot0 + mine * fan, 0, in_mine)) return;
-        merge(first_part + mine * fan * step, step, in_mine);
-        if (fans > 1) {
-            put(first_part + mine * fan * step);
-            if (!last_of(slot0, 1, fans)) return;
-            merge(first_part, fan * step, fans);
+            sets = sharers;
         }
+        slot = first_slot;   // where the second level finds it
+        first_slot = slot0;
+        apart = fan;
+        n = fans;
     }
     if (!writes) return;
     const float inv = x.l == 0.f ? 0.f : 1.f / x.l;   // nothing seen: zeros
@@ -550,7 +635,6 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 // ---------------------------------------------------------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 template <typename KT>
 struct Rows128;
@@ -670,7 +754,7 @@ struct Rows128Lds {
     __align__(16) char k[2][Rows128<KT>::TK * Rows128<KT>::ROWB], v[2][Rows128<KT>::TK * Rows128<KT>::ROWB];
 };
 
-template <typename KT>
+template <typename KT, bool SINKS>
 __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, Rows128Lds<KT> &lds) {
     typedef Rows128<KT> R;
     constexpr int TK = R::TK, LPR = R::PIECES, RPI = 64 / LPR;   // lanes to a row, rows to a load of the wave
@@ -705,15 +789,17 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
         k_off[i] = (uint32_t)(R::key_of_k_row(r) - group) * (uint32_t)bt.row_stride + R::k_piece(r, piece) * 16;
         v_off[i] = (uint32_t)(r - group) * (uint32_t)bt.row_stride + R::v_piece(r, piece) * 16;
     }
+    // (entries as the table has them, so that nobody waits for them before the rows are asked for)
     auto pages_of = [&](int place) {
-        const int key = key_at(t, place) + 16 * (lane % (TK / 16));
-        return key < t.hi ? lvr_page_of(bt, t.seq, key) : -1;
+        const int key = key_at<SINKS>(t, place) + 16 * (lane % (TK / 16));
+        return key < t.hi && key < bt.table_width << bt.page_shift ? bt.table[(int64_t)t.seq * bt.table_width + (key >> bt.page_shift)] : -1;
     };
     constexpr bool FP4 = __is_same(KT, lvr_fp4_t);
     struct { uint32_t k[4], v[4], ks[4], vs[4]; } raw;   // of FP4: a lane's codes (eight of four rows each) and their scales, on their way
     const int dword = lane % 16, row_of = lane / 16;
-    auto load = [&](int place, int pages, int buf) {
-        const int k0 = key_at(t, place);
+    auto load = [&](int place, int pages, char *to_k, char *to_v) {
+        const int k0 = key_at<SINKS>(t, place);
+        pages = pages < bt.n_pages ? pages : -1;
         const int page = __builtin_amdgcn_readlane(pages, group / 16);
         const int64_t at = page < 0 ? kvh * bt.head_stride : lvr_row_at(bt, page, kvh, k0 + group);   // no page: some memory of the pool
         if constexpr (FP4) {
@@ -730,64 +816,67 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            load_to_lds(a.k_pages + at, k_off[i], lds.k[buf] + (wave * 4 + i) * 1024);
-            load_to_lds(a.v_pages + at, v_off[i], lds.v[buf] + (wave * 4 + i) * 1024);
+            load_to_lds(a.k_pages + at, k_off[i], to_k + (wave * 4 + i) * 1024);
+            load_to_lds(a.v_pages + at, v_off[i], to_v + (wave * 4 + i) * 1024);
         }
         return (uint32_t)__ballot(pages < 0) & ((1u << TK / 16) - 1u);   // groups without a page
     };
     // Of FP4: what was loaded for the tile at `place`, into LDS.  A row of V that no query row sees may be memory nobody has written.
-    auto unfold = [&](int place, uint32_t none, int buf) {
+    auto unfold = [&](int place, uint32_t none, char *to_k, char *to_v) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int key = group + 4 * i + row_of, kr = R::key_of_k_row(key);   // (that permutation is its own inverse)
-            *reinterpret_cast<lvr_bf16x8 *>(lds.k[buf] + kr * R::ROWB + R::k_piece(kr, dword) * 16) = lvr_fp4_values(raw.k[i], lvr_fp4_scale(raw.ks[i]));
-            const bool unseen = (none >> (group >> 4) & 1) || hidden(a, key_at(t, place) + key, t.lo, t.hi - 1);
-            *reinterpret_cast<lvr_bf16x8 *>(lds.v[buf] + key * R::ROWB + R::v_piece(key, dword) * 16) =
+            *reinterpret_cast<lvr_bf16x8 *>(to_k + kr * R::ROWB + R::k_piece(kr, dword) * 16) = lvr_fp4_values(raw.k[i], lvr_fp4_scale(raw.ks[i]));
+            const bool unseen = (none >> (group >> 4) & 1) || hidden<SINKS>(a, key_at<SINKS>(t, place) + key, t.lo, t.hi - 1);
+            *reinterpret_cast<lvr_bf16x8 *>(to_v + key * R::ROWB + R::v_piece(key, dword) * 16) =
                 lvr_fp4_values(unseen ? 0u : raw.v[i], unseen ? 1.f : lvr_fp4_scale(raw.vs[i]));
         }
     };
     auto arrived = [] {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // (the built-in wait: one in assembly is no news to the compiler, which would wait once more for whatever was loaded before)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
 
-    int buf = 0;
-    uint32_t none = 0, next_none = 0;
-    if (t.begin < t.end) none = load(t.begin, pages_of(t.begin), 0);
+    uint32_t none = 0;
+    if (t.begin < t.end) none = load(t.begin, pages_of(t.begin), lds.k[0], lds.v[0]);
     int pages = pages_of(t.begin + TK);
     if constexpr (FP4)
-        if (t.begin < t.end) unfold(t.begin, none, 0);
-    arrived();
-    for (int place = t.begin; place < t.end; place += TK, buf ^= 1, none = next_none) {   // uniform over the workgroup
-        const int k0 = key_at(t, place);
+        if (t.begin < t.end) unfold(t.begin, none, lds.k[0], lds.v[0]);
+    // A tile is worked on while the next one is on its way.  The buffers are told apart for the compiler, which else waits for what comes into one before it
+    // reads the other.
+    auto step = [&](int place, const char *__restrict k, char *__restrict v, char *__restrict next_k, char *__restrict next_v) __attribute__((always_inline)) {
+        const int k0 = key_at<SINKS>(t, place);
+        uint32_t next_none = 0;
         if (place + TK < t.end) {
-            next_none = load(place + TK, pages, buf ^ 1);
+            next_none = load(place + TK, pages, next_k, next_v);
             pages = pages_of(place + 2 * TK);
         }
-        if (!FP4 && (!all_seen(a, k0, TK, t.lo, t.hi) || none != 0)) {   // a row of V that no query row sees may be memory nobody has written
+        if (!FP4 && (!all_seen<SINKS>(a, k0, TK, t.lo, t.hi) || none != 0)) {   // a row of V that no query row sees may be memory nobody has written
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int key = srow + i * RPI;
-                if (hidden(a, k0 + key, t.lo, t.hi - 1) || (none >> (key >> 4) & 1))
-                    *reinterpret_cast<uint4 *>(lds.v[buf] + key * R::ROWB + piece * 16) = make_uint4(0, 0, 0, 0);
+                if (hidden<SINKS>(a, k0 + key, t.lo, t.hi - 1) || (none >> (key >> 4) & 1))
+                    *reinterpret_cast<uint4 *>(v + key * R::ROWB + piece * 16) = make_uint4(0, 0, 0, 0);
             }
             arrived();
         }
-        if (k0 < whi && (k0 + TK > wlo || k0 < a.sinks)) {
+        if (k0 < whi && (k0 + TK > wlo || (SINKS && k0 < a.sinks))) {
             f32x16 p[R::NT];
-            R::scores(lds.k[buf], q, n, h, p);
-            const bool partly = !all_seen(a, k0, TK, all_lo, all_hi) || none != 0;
+            R::scores(k, q, n, h, p);
+            const bool partly = !all_seen<SINKS>(a, k0, TK, all_lo, all_hi) || none != 0;
             if (partly) {
                 asm volatile("");   // a branch, not 32 selects in every tile
 #pragma unroll 1
-                for (int c = 0; c < TK * R::ROWB / 1024; ++c) redo |= R::odd(*reinterpret_cast<const uint4 *>(lds.v[buf] + c * 1024 + lane * 16));
+                for (int c = 0; c < TK * R::ROWB / 1024; ++c) redo |= R::odd(*reinterpret_cast<const uint4 *>(v + c * 1024 + lane * 16));
 #pragma unroll
                 for (int kt = 0; kt < R::NT; ++kt)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int key = R::key_of(h, kt, r);
-                        if (hidden(a, k0 + key, first, last) || (none >> (key >> 4) & 1)) p[kt][r] = -INFINITY;
+                        if (hidden<SINKS>(a, k0 + key, first, last) || (none >> (key >> 4) & 1)) p[kt][r] = -INFINITY;
                     }
             }
             float top = p[0][0];
@@ -809,18 +898,23 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
             for (int kt = 0; kt < R::NT; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) p[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[kt][r], a.unit, -base));
-            R::add(lds.v[buf], p, lane, o, l);
+            R::add(v, p, lane, o, l);
         }
         if constexpr (FP4)
-            if (place + TK < t.end) unfold(place + TK, next_none, buf ^ 1);
+            if (place + TK < t.end) unfold(place + TK, next_none, next_k, next_v);
+        none = next_none;
         arrived();
-    }
+    };
+    arrived();
+    int buf = 0;
+    for (int place = t.begin; place < t.end; place += TK, buf ^= 1)   // uniform over the workgroup
+        step(place, lds.k[buf], lds.v[buf], lds.k[buf ^ 1], lds.v[buf ^ 1]);
     l += __shfl_xor(l, 32, 64);
     if (__any(redo)) {
         for (int r = row0; r < row0 + 32 && r < t.rows; ++r) {
-            RowSum s = one_row<KT>(a, bt, t, kvh, r, t.begin, 1 << 30, 1 << 30);
+            RowSum s = one_row<KT, SINKS>(a, bt, t, kvh, r, t.begin, 1 << 30, 1 << 30);
             if (t.splits > 1) {
-                float *mine = partial<128>(a.part, t.slot, a.n_kv, kvh);
+                float *mine = partial128(a.part, t.slot, a.n_kv, kvh);
                 *reinterpret_cast<float2 *>(mine + (r - t.row0) * LVR_D + 2 * lane) = make_float2(s.o0, s.o1);
                 *reinterpret_cast<float2 *>(mine + 128 * LVR_D + (r - t.row0) * 2) = make_float2(s.m, s.l);
                 continue;
@@ -834,14 +928,14 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
     }
     if (!has_row) return;
     if (t.splits > 1) {
-        float *mine = partial<128>(a.part, t.slot, a.n_kv, kvh) + (wave * 32 + n) * LVR_D;
+        float *mine = partial128(a.part, t.slot, a.n_kv, kvh) + (wave * 32 + n) * LVR_D;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const float4 v = R::ELT == 2 ? make_float4(o[i >> 2][(i & 3) * 4], o[i >> 2][(i & 3) * 4 + 1], o[i >> 2][(i & 3) * 4 + 2], o[i >> 2][(i & 3) * 4 + 3])
                                          : make_float4(o[0][i], o[1][i], o[2][i], o[3][i]);
             *reinterpret_cast<float4 *>(mine + (R::ELT == 2 ? R::coordinate(h, i >> 2, (i & 3) * 4) : R::coordinate(h, 0, i))) = v;
         }
-        if (h == 0) *reinterpret_cast<float2 *>(partial<128>(a.part, t.slot, a.n_kv, kvh) + 128 * LVR_D + (wave * 32 + n) * 2) = make_float2(m, l);
+        if (h == 0) *reinterpret_cast<float2 *>(partial128(a.part, t.slot, a.n_kv, kvh) + 128 * LVR_D + (wave * 32 + n) * 2) = make_float2(m, l);
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;   // nothing seen: zeros
@@ -869,33 +963,33 @@ inline dim3 grid_of(int n_kv, int64_t pieces) {
 }
 
 // Tiles of 16 rows alone: batches in which every sequence brings a token or so.
-template <typename KT>
-__global__ void __launch_bounds__(256, 2) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
+template <typename KT, bool SINKS>
+__global__ void __launch_bounds__(256, __is_same(KT, lvr_fp4_t) ? 3 : 2) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
     __shared__ Rows16Lds lds;
     const int kvh = blockIdx.x;
     Tile t;
-    Division<false, Wave> d(a, bt);
-    if (d.divide(a.target) && d.template locate<false>(piece_of_block(), t)) rows16_piece<KT>(a, bt, t, kvh, lds);
+    Division<false, Wave, SINKS> d(a, bt);
+    if (d.divide(a.target) && d.template locate<false>(piece_of_block(), t)) rows16_piece<KT, SINKS>(a, bt, t, kvh, lds);
 }
 
 // Any batch: every sequence in the tiles that suit it.
-template <typename KT>
+template <typename KT, bool SINKS>
 __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs a, lvr_paged_batch bt) {
     __shared__ union { Rows16Lds narrow; Rows128Lds<KT> wide; } lds;
     const int kvh = blockIdx.x;
     Tile t;
-    Division<true, Wave> d(a, bt);
+    Division<true, Wave, SINKS> d(a, bt);
     if (!d.divide(a.target) || !d.template locate<false>(piece_of_block(), t)) return;
-    if (t.height == 128) rows128_piece<KT>(a, bt, t, kvh, lds.wide);
-    else rows16_piece<KT>(a, bt, t, kvh, lds.narrow);
+    if (t.height == 128) rows128_piece<KT, SINKS>(a, bt, t, kvh, lds.wide);
+    else rows16_piece<KT, SINKS>(a, bt, t, kvh, lds.narrow);
 }
 
 // Merges the runs of cut 128-row tiles.  16 rows of a tile at a time, 16 lanes to a row; the workgroups share them out.  A launch of its own, unlike
 // for tiles of 16 rows: a partial result of 128 rows is 66 KiB, and the last workgroup of a tile would read all of them alone.  Bound by that read:
 // 512 partial results (34 MB) 10 us.
-template <typename KT>
+template <typename KT, bool SINKS>
 __global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, lvr_paged_batch bt) {
-    Division<true, Wave> d(a, bt);
+    Division<true, Wave, SINKS> d(a, bt);
     if (!d.divide(a.target)) return;
     const int c0 = (threadIdx.x & 15) * 8;
     const int64_t step = (int64_t)a.n_kv * (128 * (LVR_D + 2));
@@ -904,7 +998,7 @@ __global__ void __launch_bounds__(256) paged_attention_merge_kernel(AttnArgs a, 
         Tile t;
         if (!d.template locate<true>(item / a.n_kv / 8, t)) return;
         if (t.splits == 1 || t.row0 + r >= t.rows) continue;
-        const float *first_part = partial<128>(a.part, t.slot, a.n_kv, kvh);
+        const float *first_part = partial128(a.part, t.slot, a.n_kv, kvh);
         Merged x;
         x.clear();
 #pragma unroll 4
@@ -944,22 +1038,28 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     const int type = pc->cfg.kv_dtype;
     const PagedLaunch launch = paged_launch(a, b, pc->cfg.n_q_heads, pc->cfg.n_kv_heads, type != LVR_F32);
     const dim3 grid = grid_of(a.n_kv, launch.pieces);
-#define LVR_BY_TYPE(KERNEL, GRID)                                                                                       \
-    do {                                                                                                                \
-        if (type == LVR_BF16) hipLaunchKernelGGL(KERNEL<lvr_bf16_t>, GRID, dim3(256), 0, st, a, b);                     \
-        else if (type == LVR_F32) hipLaunchKernelGGL(KERNEL<lvr_f32_t>, GRID, dim3(256), 0, st, a, b);                  \
-        else hipLaunchKernelGGL(KERNEL<lvr_fp4_t>, GRID, dim3(256), 0, st, a, b);                                       \
+#define LVR_LAUNCH(KERNEL, KT, GRID)                                                                                  \
+    do {                                                                                                              \
+        if (a.sinks) hipLaunchKernelGGL((KERNEL<KT, true>), GRID, dim3(256), 0, st, a, b);                            \
+        else hipLaunchKernelGGL((KERNEL<KT, false>), GRID, dim3(256), 0, st, a, b);                                   \
+    } while (0)
+#define LVR_BY_TYPE(KERNEL, GRID)                                             \
+    do {                                                                      \
+        if (type == LVR_BF16) LVR_LAUNCH(KERNEL, lvr_bf16_t, GRID);           \
+        else if (type == LVR_F32) LVR_LAUNCH(KERNEL, lvr_f32_t, GRID);        \
+        else LVR_LAUNCH(KERNEL, lvr_fp4_t, GRID);                             \
     } while (0)
     if (!launch.mixed) {
         LVR_BY_TYPE(paged_attention_rows16_kernel, grid);
         return hipGetLastError();
     }
     LVR_BY_TYPE(paged_attention_mixed_kernel, grid);
-#undef LVR_BY_TYPE
     if (a.target > 0) {   // (what it merges is fp32, what it writes fp32 or bf16)
         const dim3 merge(MERGE_WGS);
-        if (type == LVR_F32) hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_f32_t>, merge, dim3(256), 0, st, a, b);
-        else hipLaunchKernelGGL(paged_attention_merge_kernel<lvr_bf16_t>, merge, dim3(256), 0, st, a, b);
+        if (type == LVR_F32) LVR_LAUNCH(paged_attention_merge_kernel, lvr_f32_t, merge);
+        else LVR_LAUNCH(paged_attention_merge_kernel, lvr_bf16_t, merge);
     }
+#undef LVR_BY_TYPE
+#undef LVR_LAUNCH
     return hipGetLastError();
 }

@@ -80,7 +80,9 @@ __host__ __device__ __forceinline__ int token_of(const AttnArgs &a, int row) { r
 // A batch of up to 64 sequences stays in registers.  Of a larger one every wave reads the lengths anew, to divide it and to find its piece: single tokens over
 // 64 keys, 8 KV heads: 64 sequences 6.2 us, 256 25, 1024 168, 4096 1787 (the read of their keys: 2.8, 11, 45, 180); over 2048 keys 256 sequences 359 us and
 // 1024 1445, the read's rate.
-template <bool MIXED, typename WAVE>
+//
+// SINKS: a.sinks may be more than 0 (without it the code has nothing of that).
+template <bool MIXED, typename WAVE, bool SINKS = true>
 struct Division {
     const AttnArgs &a;
     const lvr_paged_batch &b;
@@ -104,7 +106,7 @@ struct Division {
             n = n < 0 ? 0 : (n > 1 << 30 ? 1 << 30 : n);
             const int rows = (s1 - s0) * G;
             tiles = wide(rows) ? (rows + 127) / 128 : (rows + 15) / 16;
-            const int reach = window ? window + 128 + ((a.sinks + 63) & ~63) : n;   // keys a tile can see, at most
+            const int reach = window ? window + 128 + (SINKS ? (a.sinks + 63) & ~63 : 0) : n;   // keys a tile can see, at most
             span = n < reach ? n : reach;
             if (span > b.table_width << b.page_shift) span = b.table_width << b.page_shift;
             if (span < 1) span = 1;
@@ -208,7 +210,7 @@ struct Division {
                 if (t.lo < 0) t.lo = 0;
                 int from = t.lo & ~63, to = t.hi;
                 t.fold = t.shift = 0;
-                if (a.sinks) {
+                if (SINKS && a.sinks) {
                     t.fold = (a.sinks + 63) & ~63;
                     if (from > t.fold) {
                         t.shift = from - t.fold;
