@@ -752,6 +752,7 @@ __device__ __forceinline__ void load_to_lds(const char *from, uint32_t offset, c
 template <typename KT>
 struct Rows128Lds {
     __align__(16) char k[2][Rows128<KT>::TK * Rows128<KT>::ROWB], v[2][Rows128<KT>::TK * Rows128<KT>::ROWB];
+    uint32_t odd[2][4];   // (FP4) whether a wave's rows of V have a block that is no number
 };
 
 template <typename KT, bool SINKS>
@@ -795,8 +796,13 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
         return key < t.hi && key < bt.table_width << bt.page_shift ? bt.table[(int64_t)t.seq * bt.table_width + (key >> bt.page_shift)] : -1;
     };
     constexpr bool FP4 = __is_same(KT, lvr_fp4_t);
-    struct { uint32_t k[4], v[4], ks[4], vs[4]; } raw;   // of FP4: a lane's codes (eight of four rows each) and their scales, on their way
-    const int dword = lane % 16, row_of = lane / 16;
+    // Of FP4: a lane brings a block of a row of K and of V, 32 codes and their scale, and makes four pieces of each.  Four rows of K side by side
+    // go to different banks; V's pieces are taken in an order that differs from row to row, so that they do.
+    struct { uint4 k, v; uint32_t ks, vs; } raw;
+    const int fp4_row = lane >> 2, fp4_block = lane & 3, fp4_key = group + fp4_row;
+    const uint32_t fp4_place = (uint32_t)fp4_row * (uint32_t)bt.row_stride + fp4_block * 16, fp4_scale = (uint32_t)fp4_row * ((uint32_t)bt.row_stride / 16) + fp4_block;
+    const int to_k0 = R::key_of_k_row(fp4_key) * R::ROWB + R::k_piece(R::key_of_k_row(fp4_key), fp4_block * 4) * 16;   // (that permutation is its own inverse)
+    const int to_v0 = fp4_key * R::ROWB + (R::v_piece(fp4_key, fp4_block * 4) ^ (fp4_key & 3)) * 16;
     auto load = [&](int place, int pages, char *to_k, char *to_v) {
         const int k0 = key_at<SINKS>(t, place);
         pages = pages < bt.n_pages ? pages : -1;
@@ -804,14 +810,10 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
         const int64_t at = page < 0 ? kvh * bt.head_stride : lvr_row_at(bt, page, kvh, k0 + group);   // no page: some memory of the pool
         if constexpr (FP4) {
             const int64_t sc = lvr_scales_at(bt, page < 0 ? 0 : page, kvh, page < 0 ? 0 : k0 + group);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t c = (uint32_t)(4 * i + row_of) * (uint32_t)bt.row_stride;
-                raw.k[i] = *reinterpret_cast<const uint32_t *>(a.k_pages + at + c + dword * 4);
-                raw.v[i] = *reinterpret_cast<const uint32_t *>(a.v_pages + at + c + dword * 4);
-                raw.ks[i] = (uint8_t)a.k_pages[sc + c / 16 + dword / 4];
-                raw.vs[i] = (uint8_t)a.v_pages[sc + c / 16 + dword / 4];
-            }
+            raw.k = *reinterpret_cast<const uint4 *>(a.k_pages + at + fp4_place);
+            raw.v = *reinterpret_cast<const uint4 *>(a.v_pages + at + fp4_place);
+            raw.ks = (uint8_t)a.k_pages[sc + fp4_scale];
+            raw.vs = (uint8_t)a.v_pages[sc + fp4_scale];
             return (uint32_t)__ballot(pages < 0) & ((1u << TK / 16) - 1u);
         }
 #pragma unroll
@@ -822,14 +824,23 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
         return (uint32_t)__ballot(pages < 0) & ((1u << TK / 16) - 1u);   // groups without a page
     };
     // Of FP4: what was loaded for the tile at `place`, into LDS.  A row of V that no query row sees may be memory nobody has written.
-    auto unfold = [&](int place, uint32_t none, char *to_k, char *to_v) {
+    auto unfold = [&](int place, uint32_t none, char *to_k, char *to_v, uint32_t *odd) {
+        const int k0 = key_at<SINKS>(t, place);
+        if (!all_seen<SINKS>(a, k0, TK, t.lo, t.hi) || none != 0)
+            if ((none >> (group >> 4) & 1) || hidden<SINKS>(a, k0 + fp4_key, t.lo, t.hi - 1)) {
+                raw.v = make_uint4(0, 0, 0, 0);
+                raw.vs = 127;
+            }
+        const bool some_odd = __any(raw.vs == 255);
+        if (lane == 0) odd[wave] = some_odd;
+        const bool swap1 = fp4_key & 1, swap2 = fp4_key & 2;
+        const uint32_t x0 = swap1 ? raw.v.y : raw.v.x, x1 = swap1 ? raw.v.x : raw.v.y, x2 = swap1 ? raw.v.w : raw.v.z, x3 = swap1 ? raw.v.z : raw.v.w;
+        const uint32_t kw[4] = {raw.k.x, raw.k.y, raw.k.z, raw.k.w}, vw[4] = {swap2 ? x2 : x0, swap2 ? x3 : x1, swap2 ? x0 : x2, swap2 ? x1 : x3};
+        const float ks = lvr_fp4_scale(raw.ks), vs = lvr_fp4_scale(raw.vs);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int key = group + 4 * i + row_of, kr = R::key_of_k_row(key);   // (that permutation is its own inverse)
-            *reinterpret_cast<lvr_bf16x8 *>(to_k + kr * R::ROWB + R::k_piece(kr, dword) * 16) = lvr_fp4_values(raw.k[i], lvr_fp4_scale(raw.ks[i]));
-            const bool unseen = (none >> (group >> 4) & 1) || hidden<SINKS>(a, key_at<SINKS>(t, place) + key, t.lo, t.hi - 1);
-            *reinterpret_cast<lvr_bf16x8 *>(to_v + key * R::ROWB + R::v_piece(key, dword) * 16) =
-                lvr_fp4_values(unseen ? 0u : raw.v[i], unseen ? 1.f : lvr_fp4_scale(raw.vs[i]));
+        for (int c = 0; c < 4; ++c) {
+            *reinterpret_cast<lvr_bf16x8 *>(to_k + (to_k0 ^ c * 16)) = lvr_fp4_values(kw[c], ks);
+            *reinterpret_cast<lvr_bf16x8 *>(to_v + (to_v0 ^ c * 16)) = lvr_fp4_values(vw[c], vs);
         }
     };
     auto arrived = [] {
@@ -844,10 +855,10 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
     if (t.begin < t.end) none = load(t.begin, pages_of(t.begin), lds.k[0], lds.v[0]);
     int pages = pages_of(t.begin + TK);
     if constexpr (FP4)
-        if (t.begin < t.end) unfold(t.begin, none, lds.k[0], lds.v[0]);
+        if (t.begin < t.end) unfold(t.begin, none, lds.k[0], lds.v[0], lds.odd[0]);
     // A tile is worked on while the next one is on its way.  The buffers are told apart for the compiler, which else waits for what comes into one before it
     // reads the other.
-    auto step = [&](int place, const char *__restrict k, char *__restrict v, char *__restrict next_k, char *__restrict next_v) __attribute__((always_inline)) {
+    auto step = [&](int place, int buf, const char *__restrict k, char *__restrict v, char *__restrict next_k, char *__restrict next_v) __attribute__((always_inline)) {
         const int k0 = key_at<SINKS>(t, place);
         uint32_t next_none = 0;
         if (place + TK < t.end) {
@@ -869,6 +880,8 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
             const bool partly = !all_seen<SINKS>(a, k0, TK, all_lo, all_hi) || none != 0;
             if (partly) {
                 asm volatile("");   // a branch, not 32 selects in every tile
+                if constexpr (FP4) redo |= (lds.odd[buf][0] | lds.odd[buf][1] | lds.odd[buf][2] | lds.odd[buf][3]) != 0;
+                else
 #pragma unroll 1
                 for (int c = 0; c < TK * R::ROWB / 1024; ++c) redo |= R::odd(*reinterpret_cast<const uint4 *>(v + c * 1024 + lane * 16));
 #pragma unroll
@@ -901,14 +914,14 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
             R::add(v, p, lane, o, l);
         }
         if constexpr (FP4)
-            if (place + TK < t.end) unfold(place + TK, next_none, next_k, next_v);
+            if (place + TK < t.end) unfold(place + TK, next_none, next_k, next_v, lds.odd[buf ^ 1]);
         none = next_none;
         arrived();
     };
     arrived();
     int buf = 0;
     for (int place = t.begin; place < t.end; place += TK, buf ^= 1)   // uniform over the workgroup
-        step(place, lds.k[buf], lds.v[buf], lds.k[buf ^ 1], lds.v[buf ^ 1]);
+        step(place, buf, lds.k[buf], lds.v[buf], lds.k[buf ^ 1], lds.v[buf ^ 1]);
     l += __shfl_xor(l, 32, 64);
     if (__any(redo)) {
         for (int r = row0; r < row0 + 32 && r < t.rows; ++r) {
@@ -957,7 +970,20 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
 // Launches are n_kv x pieces workgroups: those of a KV head follow each other on one die where there are eight of them (a die has its
 // own cache, and workgroups go to the eight dies in turn).
 constexpr int GRID_Y = 32768;
-__device__ __forceinline__ int piece_of_block() { return blockIdx.z * GRID_Y + blockIdx.y; }
+// Where a token's heads lie side by side in 4 bits, a line of memory holds rows of two heads and scales of all: there the heads of a piece follow each
+// other on one die, eight pieces on the eight dies (48 ragged single tokens 199 us with a KV head to a die, 170 so).
+template <typename KT>
+__device__ __forceinline__ int piece_of_block(const AttnArgs &a, const lvr_paged_batch &bt, int &kvh) {
+    const int piece = blockIdx.z * GRID_Y + blockIdx.y;
+    kvh = blockIdx.x;
+    if constexpr (__is_same(KT, lvr_fp4_t)) {
+        if (bt.row_stride == LVR_FP4_CODES || (piece | 7) >= (int)(gridDim.y * gridDim.z)) return piece;
+        const int in_eight = (piece & 7) * a.n_kv + kvh;   // of the workgroups of eight pieces
+        kvh = in_eight >> 3;
+        return (piece & ~7) + (in_eight & 7);
+    }
+    return piece;
+}
 inline dim3 grid_of(int n_kv, int64_t pieces) {
     return dim3((unsigned)n_kv, (unsigned)(pieces < GRID_Y ? pieces : GRID_Y), (unsigned)((pieces + GRID_Y - 1) / GRID_Y));
 }
@@ -966,20 +992,22 @@ inline dim3 grid_of(int n_kv, int64_t pieces) {
 template <typename KT, bool SINKS>
 __global__ void __launch_bounds__(256, __is_same(KT, lvr_fp4_t) ? 3 : 2) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
     __shared__ Rows16Lds lds;
-    const int kvh = blockIdx.x;
+    int kvh;
+    const int piece = piece_of_block<KT>(a, bt, kvh);
     Tile t;
     Division<false, Wave, SINKS> d(a, bt);
-    if (d.divide(a.target) && d.template locate<false>(piece_of_block(), t)) rows16_piece<KT, SINKS>(a, bt, t, kvh, lds);
+    if (d.divide(a.target) && d.template locate<false>(piece, t)) rows16_piece<KT, SINKS>(a, bt, t, kvh, lds);
 }
 
 // Any batch: every sequence in the tiles that suit it.
 template <typename KT, bool SINKS>
 __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs a, lvr_paged_batch bt) {
     __shared__ union { Rows16Lds narrow; Rows128Lds<KT> wide; } lds;
-    const int kvh = blockIdx.x;
+    int kvh;
+    const int piece = piece_of_block<KT>(a, bt, kvh);
     Tile t;
     Division<true, Wave, SINKS> d(a, bt);
-    if (!d.divide(a.target) || !d.template locate<false>(piece_of_block(), t)) return;
+    if (!d.divide(a.target) || !d.template locate<false>(piece, t)) return;
     if (t.height == 128) rows128_piece<KT, SINKS>(a, bt, t, kvh, lds.wide);
     else rows16_piece<KT, SINKS>(a, bt, t, kvh, lds.narrow);
 }
