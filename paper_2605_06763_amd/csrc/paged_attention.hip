@@ -692,6 +692,11 @@ struct Rows128<lvr_bf16_t> {
                 }
             }
     }
+    // Largest magnitudes, of each half of the words apart; whether one is an infinity or a NaN.
+    static __device__ __forceinline__ void largest(uint4 &m, const uint4 &v) {
+        typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+        m = __builtin_bit_cast(uint4, __builtin_elementwise_max(__builtin_bit_cast(u16x8, m), (u16x8)(__builtin_bit_cast(u16x8, v) & (uint16_t)0x7fff)));
+    }
     static __device__ __forceinline__ bool odd(const uint4 &v) { return Rows16<lvr_bf16_t>::odd_v(v); }
 };
 
@@ -732,6 +737,9 @@ struct Rows128<lvr_f32_t> {
             o[2] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, p[0][r], o[2], 0, 0, 0);
             o[3] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, p[0][r], o[3], 0, 0, 0);
         }
+    }
+    static __device__ __forceinline__ void largest(uint4 &m, const uint4 &v) {
+        m = __builtin_bit_cast(uint4, __builtin_elementwise_max(__builtin_bit_cast(u32x4, m), __builtin_bit_cast(u32x4, v) & 0x7fffffffu));
     }
     static __device__ __forceinline__ bool odd(const uint4 &v) {
         return (v.x & 0x7f800000u) == 0x7f800000u || (v.y & 0x7f800000u) == 0x7f800000u || (v.z & 0x7f800000u) == 0x7f800000u ||
@@ -880,17 +888,32 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
             const bool partly = !all_seen<SINKS>(a, k0, TK, all_lo, all_hi) || none != 0;
             if (partly) {
                 asm volatile("");   // a branch, not 32 selects in every tile
-                if constexpr (FP4) redo |= (lds.odd[buf][0] | lds.odd[buf][1] | lds.odd[buf][2] | lds.odd[buf][3]) != 0;
-                else
-#pragma unroll 1
-                for (int c = 0; c < TK * R::ROWB / 1024; ++c) redo |= R::odd(*reinterpret_cast<const uint4 *>(v + c * 1024 + lane * 16));
+                if constexpr (FP4) {
+                    redo |= (lds.odd[buf][0] | lds.odd[buf][1] | lds.odd[buf][2] | lds.odd[buf][3]) != 0;
+                } else {
+                    uint4 worst = make_uint4(0, 0, 0, 0);
+#pragma unroll 4
+                    for (int c = 0; c < TK * R::ROWB / 1024; ++c) R::largest(worst, *reinterpret_cast<const uint4 *>(v + c * 1024 + lane * 16));
+                    redo |= R::odd(worst);
+                }
+                // keys from_here .. from_here + count of the tile are seen, and with first keys among them those before sink_end
+                const int from_here = (last < first ? 1 << 30 : first) - k0 - R::key_of(h, 0, 0), count = last < first ? 0 : last - first;
+                const int sink_end = (a.sinks < last + 1 ? a.sinks : last + 1) - k0 - R::key_of(h, 0, 0);
+                const bool sink_here = SINKS && k0 < a.sinks;
 #pragma unroll
                 for (int kt = 0; kt < R::NT; ++kt)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const int key = R::key_of(h, kt, r);
-                        if (hidden<SINKS>(a, k0 + key, first, last) || (none >> (key >> 4) & 1)) p[kt][r] = -INFINITY;
+                        const int key = R::key_of(0, kt, r);   // (the lane's own 8 or 4 h is in from_here)
+                        if ((uint32_t)(key - from_here) > (uint32_t)count && !(sink_here && key < sink_end)) p[kt][r] = -INFINITY;
                     }
+                if (none != 0) {
+#pragma unroll
+                    for (int kt = 0; kt < R::NT; ++kt)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (none >> (R::key_of(h, kt, r) >> 4) & 1) p[kt][r] = -INFINITY;
+                }
             }
             float top = p[0][0];
 #pragma unroll
