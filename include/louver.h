@@ -458,8 +458,8 @@ int lvr_paged_append(lvr_paged *pc, void *k_pages_dev, void *v_pages_dev, const 
 
 /* lvr_paged_append with a norm of every row of K and q in the same pass, before the rotation: x becomes
  * x / sqrt(mean of x^2 over the head's coordinates + eps) * weight.  q_weight_dev, k_weight_dev: [head_dim] of the type of new rows, the same for
- * all heads, 16-byte aligned; NULL: ones.  eps >= 0 and finite (LVR_E_INVALID otherwise).  Squares are summed in 64 bits, the rest
- * is fp32 (64 bits for K on LVR_FP4 pages), rounded once at the end.  V is stored as it is. */
+ * all heads, 16-byte aligned; NULL: ones.  eps >= 0 and finite (LVR_E_INVALID otherwise).  Values of any size have the norm the
+ * formula gives (squares beyond the fp32 range are summed in 64 bits); the rest is fp32 (64 bits for K on LVR_FP4 pages), rounded once at the end.  V is stored as it is. */
 int lvr_paged_norm_append(lvr_paged *pc, void *k_pages_dev, void *v_pages_dev, const void *k_new_dev, const void *v_new_dev,
                           const void *q_dev, void *q_out_dev, const int64_t token_strides_host[3], const void *q_weight_dev,
                           const void *k_weight_dev, float eps, const int32_t *positions_dev, const int32_t *seq_start_dev,

@@ -168,12 +168,62 @@ __device__ __forceinline__ uint32_t row_max8(uint32_t v) {
     v = larger(v, dpp<DPP_XOR2>(v));
     return larger(v, dpp<DPP_MIRROR8>(v));
 }
+// The sines and cosines of a token's pairs, made by a lane each and handed round in LDS, the wave's own: a lane needs those of E pairs, and eight (or
+// four) lanes need the same.
+template <typename T>
+struct Turn { T sn, cs; };
+template <typename T>
+struct Turns {
+    Turn<T> of[PAIRS];
+    __device__ __forceinline__ void make(const AppendArgs &a, const Position &pos) {
+        const int pair = lvr_lane();
+        if (pair < a.rot / 2) {
+            const uint64_t phase = (uint64_t)(int64_t)pos.of(a, pair) * a.turns[pair];
+            Turn<T> t;
+            if constexpr (sizeof(T) == 8) sincos_turn(phase, t.sn, t.cs);
+            else sincos_turn((uint32_t)(phase >> 32), t.sn, t.cs);
+            of[pair] = t;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+};
+union WaveTurns {
+    Turns<float> f32;
+    Turns<double> f64;
+};
+
 // 1 / sqrt(sum of squares / 128 + eps).  Squares are summed in 64 bits: those of large bf16 and fp32 values pass the fp32 range.
 __device__ __forceinline__ double norm_of(double squares, float eps) {
     const double x = squares * (1. / LVR_D) + (double)eps;
     const double r = __builtin_amdgcn_rsq(x);
     if (x == __builtin_inf()) return 0.;
     return r * __builtin_fma(-0.5 * x * r, r, 1.5);   // the instruction's 2^-26 or so become 2^-50
+}
+// The sum of squares of what a lane has of a row.  bf16: two products a step, exact in fp32, and sums of 16 values in it; where they leave its range, as
+// for all else, in 64 bits.
+template <int ELT>
+__device__ __forceinline__ double squares_of(u32x4 r0, u32x4 r1) {
+    if constexpr (ELT == 2) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w0 = r0[i], w1 = r1[i];
+            s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w0), __builtin_bit_cast(bf16x2, w0), s, false);
+            s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w1), __builtin_bit_cast(bf16x2, w1), s, false);
+        }
+        if (!__any(!(s > 0x1p-90f && s < 0x1p120f))) return s;   // (squares below 2^-126 would be 2^-36 of it)
+    }
+    constexpr int E = 16 / ELT;
+    float x[E], y[E];
+    elements(r0, x);
+    elements(r1, y);
+    double squares = 0.;
+#pragma unroll
+    for (int e = 0; e < E; ++e) squares += (double)x[e] * x[e] + (double)y[e] * y[e];
+    return squares;
 }
 // The norm times a row's values, in fp32 without leaving its range on the way.
 struct Normed {
@@ -205,21 +255,21 @@ __device__ __forceinline__ uint32_t fp4_codes(const float (&x)[8], float scale) 
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
 // A value in 64 bits as an fp32 value that rounds to the same code and scale: cut to 21 bits, the last of which says whether anything was cut.  Beyond the range of
-// fp32 its largest number, which has the largest scale and code; below 2^-126, far under the least code, zero.
-__device__ __forceinline__ float sticky(double v) {
+// fp32 its largest number, which has the largest scale and code; below 2^-126, far under the least code, something that small.  `most` keeps the
+// largest upper half seen: infinities and NaN are told by it.
+__device__ __forceinline__ float sticky(double v, uint32_t &most) {
     const uint64_t u = __builtin_bit_cast(uint64_t, v);
-    const uint32_t hi = (uint32_t)(u >> 32), sign = hi & 0x80000000u;
-    const int32_t mag = (int32_t)(hi & 0x7fffffffu) - ((1023 - 127) << 20);   // exponent and 20 bits, with the bias of fp32
-    uint32_t bits = (uint32_t)mag << 3 | ((uint32_t)u != 0);
-    if (mag < 1 << 20) bits = 0;
-    if (mag >= 255 << 20) bits = (hi & 0x7ff00000u) == 0x7ff00000u ? 0x7f800000u : 0x7f7fffffu;   // (an infinity and a NaN mean the same here)
-    return __uint_as_float(sign | bits);
+    const uint32_t lo = (uint32_t)u, hi = (uint32_t)(u >> 32), mag = hi & 0x7fffffffu;
+    most = mag > most ? mag : most;
+    int32_t m = (int32_t)mag - ((1023 - 127) << 20);   // exponent and 20 bits, with the bias of fp32
+    m = m < 0 ? 0 : (m > (255 << 20) - 1 ? (255 << 20) - 1 : m);
+    return __uint_as_float((hi & 0x80000000u) | (uint32_t)m << 3 | (lo < 1 ? lo : 1));
 }
 
 // Eight K rows and eight V rows of one token into pages in 4 bits, by one wave; lanes hold pieces as in paged_append_kernel.  A code is that of the exact value: K is
 // normed and rotated in 64 bits, which fp32 would leave beside a border between two codes on either side of it.
 template <bool NEIGHBOURS, bool NORM>
-__device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_batch &b, int t, int row) {
+__device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_batch &b, int t, int row, Turns<double> &turns) {
     constexpr int E = 8, LANES = 8;
     const int li = lvr_lane() % LANES;
     const Pieces p = pieces_of<E, NEIGHBOURS>(li, a.rot);
@@ -235,9 +285,10 @@ __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_
     const int64_t slot = (int64_t)b.seq_len[seq] - b.seq_start[seq + 1] + t;
     const int page = lvr_page_of(b, seq, slot);
     if (page < 0) return;
-    const Position at(a, t, slot);
+    if (a.rot > 0) turns.make(a, Position(a, t, slot));
 
     float x[E], y[E];
+    uint32_t most0 = 0, most1 = 0;   // of what is normed or rotated
     elements(k0, x);
     elements(k1, y);
     if (NORM || p.rot0 || p.rot1) {   // (p.rot* differ from lane to lane of a row)
@@ -258,26 +309,24 @@ __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_
             float &fz = NEIGHBOURS ? (second ? y : x)[2 * (e % (E / 2)) + 1] : y[e];
             double u = fu, z = fz;
             if (NORM) {
-                u = u * norm * (double)(NEIGHBOURS ? (second ? wy : wx)[2 * (e % (E / 2))] : wx[e]);
-                z = z * norm * (double)(NEIGHBOURS ? (second ? wy : wx)[2 * (e % (E / 2)) + 1] : wy[e]);
+                u *= norm * (double)(NEIGHBOURS ? (second ? wy : wx)[2 * (e % (E / 2))] : wx[e]);
+                z *= norm * (double)(NEIGHBOURS ? (second ? wy : wx)[2 * (e % (E / 2)) + 1] : wy[e]);
             }
             if (NEIGHBOURS && second ? p.rot1 : p.rot0) {
-                const int pair = pair_of<E, NEIGHBOURS>(li, e);
-                double sn, cs;
-                sincos_turn((uint64_t)(int64_t)at.of(a, pair) * a.turns[pair], sn, cs);
-                const double first = u * cs - z * sn;
-                z = u * sn + z * cs;
+                const Turn<double> turn = turns.of[pair_of<E, NEIGHBOURS>(li, e)];
+                const double first = u * turn.cs - z * turn.sn;
+                z = u * turn.sn + z * turn.cs;
                 u = first;
             }
-            fu = sticky(u);
-            fz = sticky(z);
+            fu = sticky(u, NEIGHBOURS && second ? most1 : most0);
+            fz = sticky(z, NEIGHBOURS && !second ? most0 : most1);
         }
     }
 
     // the scales of the row's four blocks; a lane's pieces lie in one block each
     const int c0 = p.at0 / 32, c1 = p.at1 / 32;
-    auto store = [&](char *pages, const float (&x)[E], const float (&y)[E]) {
-        uint32_t m0 = 0, m1 = 0, packed = 0;
+    auto store = [&](char *pages, const float (&x)[E], const float (&y)[E], bool odd0, bool odd1) {
+        uint32_t m0 = odd0 ? 0x7f800000u : 0, m1 = odd1 ? 0x7f800000u : 0, packed = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const uint32_t bx = __float_as_uint(x[e]) & 0x7fffffffu, by = __float_as_uint(y[e]) & 0x7fffffffu;
@@ -295,10 +344,10 @@ __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_
         *reinterpret_cast<uint32_t *>(codes + p.at1 / 2) = fp4_codes(y, lvr_fp4_scale(packed >> 8 * c1 & 255));
         if (li == 0) *reinterpret_cast<uint32_t *>(pages + lvr_scales_at(b, page, row, slot)) = packed;
     };
-    store(a.k_pages, x, y);
+    store(a.k_pages, x, y, most0 >= 0x7ff00000u, most1 >= 0x7ff00000u);
     elements(v0, x);
     elements(v1, y);
-    store(a.v_pages, x, y);
+    store(a.v_pages, x, y, false, false);
 }
 
 // A wave takes PER times ROWS rows of one token.  A lane holds two pieces of a row, of E elements each: HALVES: the same one of both
@@ -315,6 +364,7 @@ __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_
 template <typename KT, bool NEIGHBOURS, int PER, bool STREAM, bool NORM, bool FP4>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_paged_batch b) {
     constexpr int ELT = sizeof(KT) == 4 ? 4 : 2, E = 16 / ELT, LANES = PAIRS / E, ROWS = 64 / LANES;
+    __shared__ WaveTurns turns[4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = lvr_lane(), li = lane % LANES;
     const uint32_t w = blockIdx.x * 4u + wave;
@@ -324,7 +374,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
     if constexpr (FP4) {
         const int of_kv = (a.n_kv + 7) / 8;
         if (group < of_kv) {
-            append_fp4<NEIGHBOURS, NORM>(a, b, t, group * 8 + lane / 8);
+            append_fp4<NEIGHBOURS, NORM>(a, b, t, group * 8 + lane / 8, turns[wave].f64);
             return;
         }
         group -= of_kv;
@@ -353,14 +403,13 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
     const int64_t slot = (int64_t)b.seq_len[seq] - b.seq_start[seq + 1] + t;
     const int page = lvr_page_of(b, seq, slot);
     float sn[E], cs[E];
-    if (rot0 || rot1) {
-        const Position pos(a, t, slot);
+    if (a.rot > 0) {
+        turns[wave].f32.make(a, Position(a, t, slot));
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int pair = pair_of<E, NEIGHBOURS>(li, e), p = pos.of(a, pair);
-            // the upper half of the product's lower 64 bits
-            const uint32_t lo = (uint32_t)a.turns[pair], hi = (uint32_t)(a.turns[pair] >> 32);
-            sincos_turn((uint32_t)p * hi + __umulhi((uint32_t)p, lo) - (p < 0 ? lo : 0u), sn[e], cs[e]);
+            const Turn<float> turn = turns[wave].f32.of[pair_of<E, NEIGHBOURS>(li, e)];   // (of pairs that are none: anything)
+            sn[e] = turn.sn;
+            cs[e] = turn.cs;
         }
     }
 #pragma unroll
@@ -372,10 +421,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
             float x[E], y[E], wx[E], wy[E];
             elements(r0[c], x);
             elements(r1[c], y);
-            double squares = 0.;
-#pragma unroll
-            for (int e = 0; e < E; ++e) squares += (double)x[e] * x[e] + (double)y[e] * y[e];
-            const Normed norm(norm_of(row_sum<LANES>(squares), a.eps));
+            const Normed norm(norm_of(row_sum<LANES>(squares_of<ELT>(r0[c], r1[c])), a.eps));
             elements(of_q ? qw0 : kw0, wx);
             elements(of_q ? qw1 : kw1, wy);
 #pragma unroll

@@ -342,12 +342,14 @@ def check_append(c, inv_freq=None, axis=None, positions=None, norm=False, weight
     axis = [0] * (rot // 2) if axis is None else axis
     kr, ks = rotated(k, pos, inv_freq, axis, rot, pairs) if rot else (k.double(), k.double().abs())
     qr, qs = rotated(q, pos, inv_freq, axis, rot, pairs) if rot else (q.double(), q.double().abs())
-    # a rotation as in test_gpu_paged.py; a norm before it: the rounding of 1 / sqrt, and two products
-    rel, off = HALF_STEP[c.dtype], (12 if rot else 0) * 2.0 ** -24 + (4 * 2.0 ** -24 if norm else 0)
+    # a rotation as in test_gpu_paged.py; a norm before it: the rounding of 1 / sqrt, and two products.  bf16 sums 16 squares of a lane in fp32, eight steps of at
+    # most 2^-23 of the sum each, of which the root halves the error: 8 * 2^-24; fp32 sums in 64 bits.
+    of_norm = (0 if not norm else 4 if c.dtype == "f32" else 12) * 2.0 ** -24
+    rel, off = HALF_STEP[c.dtype], (12 if rot else 0) * 2.0 ** -24 + of_norm
 
     def bound(y, size):
         t = rel * y.abs() + off * size
-        t[..., rot:] = (rel * y.abs() + 4 * 2.0 ** -24 * y.abs())[..., rot:] if norm else 0
+        t[..., rot:] = (rel * y.abs() + of_norm * y.abs())[..., rot:] if norm else 0
         return t
 
     inside = torch.zeros(c.T, dtype=torch.bool)
