@@ -1087,7 +1087,8 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.part = pc->part;
     a.ticket = pc->ticket;
     const int type = pc->cfg.kv_dtype;
-    const PagedLaunch launch = paged_launch(a, b, pc->cfg.n_q_heads, pc->cfg.n_kv_heads, type != LVR_F32);
+    a.uncut = type == LVR_FP4 ? UNCUT_FP4 : (type == LVR_BF16 && a.sinks ? UNCUT_BF16 : 0);
+    const PagedLaunch launch = paged_launch(a, b, pc->cfg.n_q_heads, pc->cfg.n_kv_heads, type != LVR_F32, type == LVR_FP4);
     const dim3 grid = grid_of(a.n_kv, launch.pieces);
 #define LVR_LAUNCH(KERNEL, KT, GRID)                                                                                  \
     do {                                                                                                              \

@@ -19,6 +19,11 @@ constexpr int MIN_RUN = 64;
 // fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 57 in a tile of 128 / 46 in four of 16,
 // eight such sequences of 4096 keys 41 / 58; fp32 171 / 98).  The rule goes by the rows alone, and for bf16 takes the side on which many sequences gain.
 constexpr int NARROW_BF16 = 32, NARROW_F32 = 64;
+constexpr int NARROW_FP4_ALONE = 64;   // of all sequences together, on pages in 4 bits (16 tokens, 32 heads on 8, over 32768 keys: 49 us in a tile of 128, 28 in four of 16)
+// Keys up to which a tile of 16 rows is not cut, on pages in 4 bits and on bf16 ones with first keys: a workgroup takes 0.6 us for 128 of them in 4 bits, merging
+// takes three (us uncut / in runs of 64: one token over 256 keys in 4 bits 6.1 / 8.8, 512 7.3 / 8.8, 16 of them over 512 7.8 / 11.0; bf16, a window of 64
+// with four first keys 8.6 / 9.8, of 192 9.3 / 9.4; fp32 12.4 / 11.8 and 15.2 / 11.4).
+constexpr int UNCUT_FP4 = 512, UNCUT_BF16 = 256;
 constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);   // partial results
 
 struct AttnArgs {
@@ -31,6 +36,7 @@ struct AttnArgs {
     int32_t g_shift;
     float unit;          // sigma * log2 e
     int32_t narrow;      // rows of a sequence up to which it is taken in tiles of 16
+    int32_t uncut;       // keys that a tile of 16 rows may see and is not cut
     int32_t target;      // pieces of work to make of the batch per KV head; 0: tiles are not cut
     float *part;
     uint32_t *ticket;    // a line for each slot of a cut tile
@@ -115,7 +121,7 @@ struct Division {
     __host__ __device__ __forceinline__ bool is_wide() const { return wide((s1 - s0) * G); }
     __host__ __device__ __forceinline__ void cut() {
         runs = 1;
-        if (L == NO_CUTS) return;
+        if (L == NO_CUTS || (span <= a.uncut && !is_wide())) return;
         int L1 = L;
         if (MIXED && any_wide && !is_wide()) L1 = L1 > 4 * MIN_RUN ? L1 >> 2 : (L1 < MIN_RUN ? L1 : MIN_RUN);
         if (MIXED) {
@@ -240,14 +246,14 @@ struct PagedLaunch {
     int64_t pieces;   // workgroups per KV head: at least as many as the division makes pieces
 };
 // Everything of `a` that the division reads but the window.
-inline PagedLaunch paged_launch(AttnArgs &a, const lvr_paged_batch &b, int n_q, int n_kv, bool bf16) {
+inline PagedLaunch paged_launch(AttnArgs &a, const lvr_paged_batch &b, int n_q, int n_kv, bool bf16, bool fp4 = false) {
     a.n_kv = n_kv;
     a.G = n_q / n_kv;
     a.g_shift = 28;
     while (1 << (a.g_shift - 28) < a.G) ++a.g_shift;
     a.g_mul = (uint32_t)((((uint64_t)1 << a.g_shift) + a.G - 1) / a.G);
     const int64_t rows = (int64_t)b.n_tokens * a.G;
-    a.narrow = bf16 ? NARROW_BF16 : NARROW_F32;
+    a.narrow = bf16 && !(fp4 && rows <= NARROW_FP4_ALONE) ? NARROW_BF16 : NARROW_F32;
     if (b.n_tokens <= b.n_seqs || rows <= a.narrow) {
         a.target = (b.n_seqs * a.n_kv <= FEW_TILES ? ROWS16_PIECES_FEW : ROWS16_PIECES) / a.n_kv;   // n_kv is at most 256
         return {false, rows / 16 + b.n_seqs + a.target};
