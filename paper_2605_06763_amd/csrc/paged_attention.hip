@@ -209,12 +209,9 @@ struct Rows16<lvr_bf16_t> {
     // itself; with it outputs are off by 1.9e-3 to 2.4e-3 of their root mean square, 1.6e-3 with fp32 weights, most of both the last rounding); l sums
     // them as rounded, which is what the second product sees.
     static __device__ __forceinline__ void add(const V &v, const float (&p)[2][4], f32x4 (&o)[8], float &l) {
-        const uint32_t pw[4] = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
+        uint32_t pw[4] = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
 #pragma unroll
         for (int c = 0; c < 4; ++c) l += lvr_bf16_lo(pw[c]) + lvr_bf16_hi(pw[c]);
-        add_rounded(v, pw, o);
-    }
-    static __device__ __forceinline__ void add_rounded(const V &v, const uint32_t (&pw)[4], f32x4 (&o)[8]) {
         const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -315,20 +312,38 @@ struct Rows16<lvr_fp4_t> {
         return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(own), J * 0x55, 0xf, 0xf, true));
     }
     static __device__ __forceinline__ uint32_t own_scale(const Values &v) { return v.scales >> (threadIdx.x & 12) * 2 & 255; }
+    // Two coordinates of all eight keys at a time: what is widened is used at once.
+    template <int M>
+    static __device__ __forceinline__ void add_pair(const V &v, const float (&scale)[8], bf16x8 pb, f32x4 (&o)[8]) {
+        uint32_t w[8], lo[4], hi[4];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) w[c] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[c >> 2].codes[c & 3], scale[c], M));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            lo[c] = __builtin_amdgcn_perm(w[2 * c + 1], w[2 * c], 0x05040100u);
+            hi[c] = __builtin_amdgcn_perm(w[2 * c + 1], w[2 * c], 0x07060302u);
+        }
+        o[2 * M] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), pb, o[2 * M], 0, 0, 0);
+        o[2 * M + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), pb, o[2 * M + 1], 0, 0, 0);
+    }
     static __device__ __forceinline__ void add(const V &v, const float (&p)[2][4], f32x4 (&o)[8], float &l) {
-        Rows16<lvr_bf16_t>::V wide;
+        float scale[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const float own = lvr_fp4_scale(own_scale(v[h]));
-            wide[h][0] = __builtin_bit_cast(uint4, lvr_fp4_values(v[h].codes[0], scale_of<0>(own)));
-            wide[h][1] = __builtin_bit_cast(uint4, lvr_fp4_values(v[h].codes[1], scale_of<1>(own)));
-            wide[h][2] = __builtin_bit_cast(uint4, lvr_fp4_values(v[h].codes[2], scale_of<2>(own)));
-            wide[h][3] = __builtin_bit_cast(uint4, lvr_fp4_values(v[h].codes[3], scale_of<3>(own)));
+            scale[4 * h] = scale_of<0>(own);
+            scale[4 * h + 1] = scale_of<1>(own);
+            scale[4 * h + 2] = scale_of<2>(own);
+            scale[4 * h + 3] = scale_of<3>(own);
         }
         const uint32_t pw[4] = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
 #pragma unroll
         for (int c = 0; c < 4; ++c) l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[c]), bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
-        Rows16<lvr_bf16_t>::add_rounded(wide, pw, o);
+        const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        add_pair<0>(v, scale, pb, o);
+        add_pair<1>(v, scale, pb, o);
+        add_pair<2>(v, scale, pb, o);
+        add_pair<3>(v, scale, pb, o);
     }
     static __device__ __forceinline__ int coordinate(int r, int u) { return Rows16<lvr_bf16_t>::coordinate(r, u); }
 };
@@ -488,20 +503,16 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
             work(key_of_turn(turn), x);
         }
     } else if (turns > 0) {
-        // Rows are asked for two turns ahead.  The last turns ask for rows that are there already, so that there are always as many loads
-        // behind the ones that are waited for.
-        Keys x, y, z;
+        // Rows are asked for a turn ahead.  The last turn asks for its own again, so that there are always as many loads behind the ones that
+        // are waited for.  (Two turns ahead take registers that a fourth workgroup on a compute unit needs: 2 to 5 % slower.)
+        Keys x, y;
         ask(0, x);
-        ask(1, y);
         for (int turn = 0;;) {
-            ask(turn + 2, z);
+            ask(turn + 1, y);
             work(key_of_turn(turn), x);
             if (++turn >= turns) break;
-            ask(turn + 2, x);
+            ask(turn + 1, x);
             work(key_of_turn(turn), y);
-            if (++turn >= turns) break;
-            ask(turn + 2, y);
-            work(key_of_turn(turn), z);
             if (++turn >= turns) break;
         }
     }
@@ -1013,7 +1024,7 @@ inline dim3 grid_of(int n_kv, int64_t pieces) {
 
 // Tiles of 16 rows alone: batches in which every sequence brings a token or so.
 template <typename KT, bool SINKS>
-__global__ void __launch_bounds__(256, __is_same(KT, lvr_fp4_t) ? 3 : 2) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
+__global__ void __launch_bounds__(256, __is_same(KT, lvr_fp4_t) ? 4 : 2) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
     __shared__ Rows16Lds lds;
     int kvh;
     const int piece = piece_of_block<KT>(a, bt, kvh);
