@@ -201,6 +201,7 @@ SINK_LENS = {
     "prompt": [(200, 200)],
     "tokens_before_the_cache": [(5, 3), (1, 0), (2, 200)],
 }
+MANY_LENS = [(1 + (i * 7) % 3, 3 + (i * 37) % 400) for i in range(70)] + [(0, 12)] * 70 + [(40, 300), (1, 600)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -223,6 +224,22 @@ def test_first_keys_over_heads_and_pages(hq, hkv, page, layout, dtype):
 def test_first_keys_cut_into_runs(hq, lens, window, sinks, dtype):
     with More(lens, dtype=dtype, hq=hq, hkv=1, page=64, seed=112) as c:
         check(c, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_first_keys_of_many_sequences(dtype):
+    with More(MANY_LENS, dtype=dtype, hq=4, hkv=2, seed=119) as c:
+        check(c, 40, 20)
+    with More([(1, 1 + (i * 53) % 700) for i in range(131)], dtype=dtype, hq=4, hkv=2, seed=118) as c:
+        check(c, 40, 20)
+
+
+@pytest.mark.parametrize("tokens", [8, 9, 16, 17])
+def test_a_few_tokens_of_one_sequence_in_4_bits(tokens):
+    """Up to 64 rows alone go in tiles of 16, more in tiles of 128."""
+    with More([(tokens, 3000)], dtype="fp4", hq=8, hkv=2, seed=117) as c:
+        check(c, plain=True)
+        check(c, 200, 10)
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -156,10 +156,10 @@ struct Alone {
     static float reciprocal(float v) { return 1.f / v; }
 };
 
-static int n_q, n_kv, bf16, page, width, window, sinks, n_seqs;
+static int n_q, n_kv, type, page, width, window, sinks, n_seqs;   // type: 0 fp32, 1 bf16, 2 pages in 4 bits
 static std::vector<int32_t> start, len;
 static void fail(const char *what) {
-    printf("%s: %d heads on %d, bf16 %d, page %d, table of %d, window %d, sinks %d, %d sequences (new, held):", what, n_q, n_kv, bf16, page, width, window, sinks, n_seqs);
+    printf("%s: %d heads on %d, type %d, page %d, table of %d, window %d, sinks %d, %d sequences (new, held):", what, n_q, n_kv, type, page, width, window, sinks, n_seqs);
     for (int i = 0; i < n_seqs && i < 40; ++i) printf(" (%d, %d)", start[i + 1] - start[i], len[i]);
     printf("\n");
     exit(1);
@@ -214,6 +214,7 @@ static void check(AttnArgs &a, const lvr_paged_batch &b, const PagedLaunch &laun
                 const bool seen = key < sinks || !window || key > p0 - window;   // by some row of the tile
                 OK(!seen || covered[key]);
             }
+            OK(height == 128 || p.size() == 1 || (window ? std::min(held, window + 128 + (sinks + 63) / 64 * 64) : held) > a.uncut);
             // no more than what the rows see and the ends of their tiles of 64
             if (window) OK(work <= window + sinks + height + 192);
         }
@@ -227,7 +228,7 @@ static void check(AttnArgs &a, const lvr_paged_batch &b, const PagedLaunch &laun
 
 int main() {
     long cases = 0;
-    while (scanf("%d %d %d %d %d %d %d %d", &n_q, &n_kv, &bf16, &page, &width, &window, &sinks, &n_seqs) == 8) {
+    while (scanf("%d %d %d %d %d %d %d %d", &n_q, &n_kv, &type, &page, &width, &window, &sinks, &n_seqs) == 8) {
         start.assign(n_seqs + 1, 0);
         len.assign(n_seqs, 0);
         for (int i = 0; i < n_seqs; ++i) {
@@ -246,7 +247,8 @@ int main() {
         AttnArgs a = {};
         a.window = window;
         a.sinks = sinks;
-        const PagedLaunch launch = paged_launch(a, b, n_q, n_kv, bf16);
+        a.uncut = type == 2 ? UNCUT_FP4 : (type == 1 && sinks ? UNCUT_BF16 : 0);
+        const PagedLaunch launch = paged_launch(a, b, n_q, n_kv, type != 0, type == 2);
         if (launch.mixed) check<true>(a, b, launch);
         else check<false>(a, b, launch);
         ++cases;
@@ -274,7 +276,7 @@ def test_every_key_a_row_sees_lies_in_one_run(tmp_path_factory):
         width = rng.choice([pages, pages, pages + 3, max(1, pages // 2), 1])
         window = rng.choice([0, 1, 16, size(8), size(13), size(13)])
         sinks = rng.choice([1, 4, 63, 64, 65, size(10), size(13)]) if window else 0
-        lines.append(" ".join(str(x) for x in (*heads, rng.randint(0, 1), page, width, window, sinks, len(lens), *(v for p in lens for v in p))))
+        lines.append(" ".join(str(x) for x in (*heads, rng.randint(0, 2), page, width, window, sinks, len(lens), *(v for p in lens for v in p))))
     r = subprocess.run([str(exe)], input="\n".join(lines), capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout
     assert int(r.stdout) == len(lines)
