@@ -97,4 +97,23 @@ __device__ __forceinline__ int lvr_seq_of(const lvr_paged_batch &b, int t) {
     }
     return before - 1;
 }
+// That sequence, and the token's position in it: of a batch of up to 63 sequences with one trip to memory.
+struct lvr_token {
+    int seq;            // -1 or n_seqs: none
+    int64_t position;
+};
+__device__ __forceinline__ lvr_token lvr_find_token(const lvr_paged_batch &b, int t) {
+    lvr_token x;
+    if (b.n_seqs < 64) {
+        const int lane = lvr_lane();
+        const int start = lane <= b.n_seqs ? b.seq_start[lane] : 0, len = lane < b.n_seqs ? b.seq_len[lane] : 0;
+        x.seq = __popcll(__ballot(lane <= b.n_seqs && start <= t)) - 1;
+        const int at = x.seq < 0 || x.seq >= b.n_seqs ? 0 : x.seq;
+        x.position = (int64_t)__builtin_amdgcn_readlane(len, at) - __builtin_amdgcn_readlane(start, at + 1) + t;
+        return x;
+    }
+    x.seq = lvr_seq_of(b, t);
+    x.position = x.seq < 0 || x.seq >= b.n_seqs ? 0 : (int64_t)b.seq_len[x.seq] - b.seq_start[x.seq + 1] + t;
+    return x;
+}
 #endif

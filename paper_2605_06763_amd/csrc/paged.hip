@@ -130,17 +130,15 @@ __device__ __forceinline__ Pieces pieces_of(int li, int rot) {
 template <int E, bool NEIGHBOURS>
 __device__ __forceinline__ int pair_of(int li, int e) { return NEIGHBOURS ? (e < E / 2 ? 0 : PAIRS / 2 - E / 2) + E * li / 2 + e : E * li + e; }
 
-struct Position {
-    int pos[4];
-    __device__ __forceinline__ Position(const AppendArgs &a, int t, int64_t slot) : pos{(int)slot, (int)slot, (int)slot, (int)slot} {
-        if (a.positions)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pos[i] = i < a.axes ? a.positions[(int64_t)t * a.axes + i] : 0;
-    }
-    __device__ __forceinline__ int of(const AppendArgs &a, int pair) const {
-        if (a.axes <= 1) return pos[0];
-        const int ax = a.axis[pair];
-        return ax < 2 ? (ax == 0 ? pos[0] : pos[1]) : (ax == 2 ? pos[2] : pos[3]);
+// What a lane needs to turn a pair, asked for before the token's position is known.
+struct Angle {
+    uint64_t turns = 0;
+    int position = 0;
+    __device__ __forceinline__ Angle(const AppendArgs &a, int t) {
+        const int pair = lvr_lane();
+        if (pair >= a.rot / 2) return;
+        turns = a.turns[pair];
+        if (a.positions) position = a.positions[(int64_t)t * a.axes + (a.axes > 1 ? a.axis[pair] : 0)];
     }
 };
 
@@ -175,10 +173,10 @@ struct Turn { T sn, cs; };
 template <typename T>
 struct Turns {
     Turn<T> of[PAIRS];
-    __device__ __forceinline__ void make(const AppendArgs &a, const Position &pos) {
+    __device__ __forceinline__ void make(const AppendArgs &a, const Angle &angle, int64_t slot) {
         const int pair = lvr_lane();
         if (pair < a.rot / 2) {
-            const uint64_t phase = (uint64_t)(int64_t)pos.of(a, pair) * a.turns[pair];
+            const uint64_t phase = (uint64_t)(int64_t)(a.positions ? angle.position : (int)slot) * angle.turns;
             Turn<T> t;
             if constexpr (sizeof(T) == 8) sincos_turn(phase, t.sn, t.cs);
             else sincos_turn((uint32_t)(phase >> 32), t.sn, t.cs);
@@ -277,15 +275,17 @@ __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_
     if (!real) row = a.n_kv - 1;   // nothing is made of it
     u32x4 k0 = load_piece(a.k + t * a.k_stride + (int64_t)row * (LVR_D * 2) + p.at0 * 2), k1 = load_piece(a.k + t * a.k_stride + (int64_t)row * (LVR_D * 2) + p.at1 * 2);
     u32x4 v0 = load_piece(a.v + t * a.v_stride + (int64_t)row * (LVR_D * 2) + p.at0 * 2), v1 = load_piece(a.v + t * a.v_stride + (int64_t)row * (LVR_D * 2) + p.at1 * 2);
+    const Angle angle(a, t);
     u32x4 w0, w1;
     if (NORM) w0 = weights_at<2>(a.k_weight, p.at0), w1 = weights_at<2>(a.k_weight, p.at1);
 
-    const int seq = lvr_seq_of(b, t);
+    const lvr_token at_batch = lvr_find_token(b, t);
+    const int seq = at_batch.seq;
+    const int64_t slot = at_batch.position;
     if (seq < 0 || seq >= b.n_seqs) return;
-    const int64_t slot = (int64_t)b.seq_len[seq] - b.seq_start[seq + 1] + t;
     const int page = lvr_page_of(b, seq, slot);
     if (page < 0) return;
-    if (a.rot > 0) turns.make(a, Position(a, t, slot));
+    if (a.rot > 0) turns.make(a, angle, slot);
 
     float x[E], y[E];
     uint32_t most0 = 0, most1 = 0;   // of what is normed or rotated
@@ -393,18 +393,20 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
         r0[c] = load_piece(src + at0 * ELT);
         r1[c] = load_piece(src + at1 * ELT);
     }
+    const Angle angle(a, t);
     if (NORM) {
         kw0 = weights_at<ELT>(a.k_weight, at0), kw1 = weights_at<ELT>(a.k_weight, at1);
         qw0 = weights_at<ELT>(a.q_weight, at0), qw1 = weights_at<ELT>(a.q_weight, at1);
     }
 
-    const int seq = lvr_seq_of(b, t);
+    const lvr_token at_batch = lvr_find_token(b, t);
+    const int seq = at_batch.seq;
+    const int64_t slot = at_batch.position;
     if (seq < 0 || seq >= b.n_seqs) return;
-    const int64_t slot = (int64_t)b.seq_len[seq] - b.seq_start[seq + 1] + t;
     const int page = lvr_page_of(b, seq, slot);
     float sn[E], cs[E];
     if (a.rot > 0) {
-        turns[wave].f32.make(a, Position(a, t, slot));
+        turns[wave].f32.make(a, angle, slot);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const Turn<float> turn = turns[wave].f32.of[pair_of<E, NEIGHBOURS>(li, e)];   // (of pairs that are none: anything)
