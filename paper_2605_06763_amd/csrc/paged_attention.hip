@@ -500,6 +500,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
         for (int turn = 0; turn < turns; ++turn) {   // uniform over the wave
             Keys x;
             ask(turn, x);
+            __builtin_amdgcn_sched_barrier(0);   // all loads on their way before one is waited for (fp32, 131072 keys: 200 us without, 187)
             work(key_of_turn(turn), x);
         }
     } else if (turns > 0) {
@@ -541,6 +542,31 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     }
     const int r = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * 8;
     const bool writes = t.row0 + r < t.rows;
+    Merged x;
+    auto from_lds = [&](int sets) {   // the sums of the waves' sets of keys, or of their shares of partials
+        __syncthreads();
+        x.clear();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = lds.o[w][r][c0 + e];
+            if (w < sets) x.add(lds.m[w][r], lds.l[w][r], v);
+        }
+    };
+    auto write = [&]() {
+        if (!writes) return;
+        const float inv = x.l == 0.f ? 0.f : 1.f / x.l;   // nothing seen: zeros
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = x.o[e] * inv;
+        store_row<R::ELT>(a, t, kvh, t.row0 + r, c0, y);
+    };
+    if (t.splits == 1) {
+        from_lds(4);
+        write();
+        return;
+    }
     // The last workgroup to end of every `fan` of a tile's runs merges those, and the last of these merges what they made, so that nobody
     // is left with all of them (one token over 8192 keys 13.1 us; all merged by one workgroup 15.2).  Four rows fill a wave, and where a tile has no
     // more the waves share the partials out; each takes up to FAN of them with all their loads in flight.  Partials cross
@@ -549,25 +575,15 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     // All of this is code that one workgroup in many runs, and fetches as it goes: it is kept short.
     const int rows = t.rows - t.row0, sharer_bits = rows <= 4 ? 2 : (rows <= 8 ? 1 : 0), sharers = 1 << sharer_bits, fan = FAN * sharers;
     const int slot0 = t.slot - t.split, fans = (t.splits + fan - 1) >> (FAN_BITS + sharer_bits), mine = t.split >> (FAN_BITS + sharer_bits);
-    const int levels = t.splits == 1 ? 0 : (fans == 1 ? 1 : 2);
+    const int levels = fans == 1 ? 1 : 2;
     int slot = t.slot, first_slot = slot0 + mine * fan, apart = 1, n = mine + 1 < fans ? fan : t.splits - mine * fan;
     const uint32_t part_size = 16 * (LVR_D + 2) * sizeof(float);
     const auto parts = __builtin_amdgcn_make_buffer_rsrc(a.part + (int64_t)WIDE_ROOM * 128 * (LVR_D + 2), 0, NARROW_ROOM * part_size, 0x00027000);
     constexpr int DEVICE = 16;   // sc1
-    Merged x;
     int sets = 4;
 #pragma unroll 1
     for (int level = 0;; ++level) {
-        if (level == 0 || sharers > 1) {   // the sums of the waves' sets of keys, or of their shares
-            __syncthreads();
-            x.clear();
-            for (int w = 0; w < sets; ++w) {
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = lds.o[w][r][c0 + e];
-                x.add(lds.m[w][r], lds.l[w][r], v);
-            }
-        }
+        if (level == 0 || sharers > 1) from_lds(sets);
         if (level == levels) break;
         if (writes) {
             const uint32_t at = (slot * a.n_kv + kvh) * part_size;
@@ -616,12 +632,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
         apart = fan;
         n = fans;
     }
-    if (!writes) return;
-    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;   // nothing seen: zeros
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = x.o[e] * inv;
-    store_row<R::ELT>(a, t, kvh, t.row0 + r, c0, y);
+    write();
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
@@ -1022,6 +1033,9 @@ inline dim3 grid_of(int n_kv, int64_t pieces) {
     return dim3((unsigned)n_kv, (unsigned)(pieces < GRID_Y ? pieces : GRID_Y), (unsigned)((pieces + GRID_Y - 1) / GRID_Y));
 }
 
+template <typename KT, bool SINKS>
+constexpr bool may_be_uncut = SINKS || __is_same(KT, lvr_fp4_t);
+
 // Tiles of 16 rows alone: batches in which every sequence brings a token or so.
 template <typename KT, bool SINKS>
 __global__ void __launch_bounds__(256, __is_same(KT, lvr_fp4_t) ? 4 : 2) paged_attention_rows16_kernel(AttnArgs a, lvr_paged_batch bt) {
@@ -1029,7 +1043,7 @@ __global__ void __launch_bounds__(256, __is_same(KT, lvr_fp4_t) ? 4 : 2) paged_a
     int kvh;
     const int piece = piece_of_block<KT>(a, bt, kvh);
     Tile t;
-    Division<false, Wave, SINKS> d(a, bt);
+    Division<false, Wave, SINKS, may_be_uncut<KT, SINKS>> d(a, bt);
     if (d.divide(a.target) && d.template locate<false>(piece, t)) rows16_piece<KT, SINKS>(a, bt, t, kvh, lds);
 }
 
@@ -1040,7 +1054,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
     int kvh;
     const int piece = piece_of_block<KT>(a, bt, kvh);
     Tile t;
-    Division<true, Wave, SINKS> d(a, bt);
+    Division<true, Wave, SINKS, may_be_uncut<KT, SINKS>> d(a, bt);
     if (!d.divide(a.target) || !d.template locate<false>(piece, t)) return;
     if (t.height == 128) rows128_piece<KT, SINKS>(a, bt, t, kvh, lds.wide);
     else rows16_piece<KT, SINKS>(a, bt, t, kvh, lds.narrow);

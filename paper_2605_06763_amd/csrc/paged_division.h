@@ -31,15 +31,15 @@ struct AttnArgs {
     char *out;
     int64_t q_stride;    // bytes per token
     int32_t n_kv, G, window;
-    int32_t sinks;       // first keys that stay visible beside a window; 0 without one.  window + sinks is at most 2^30
     uint32_t g_mul;      // row / G = row * g_mul >> g_shift
     int32_t g_shift;
     float unit;          // sigma * log2 e
     int32_t narrow;      // rows of a sequence up to which it is taken in tiles of 16
-    int32_t uncut;       // keys that a tile of 16 rows may see and is not cut
     int32_t target;      // pieces of work to make of the batch per KV head; 0: tiles are not cut
     float *part;
     uint32_t *ticket;    // a line for each slot of a cut tile
+    int32_t sinks;       // first keys that stay visible beside a window; 0 without one.  window + sinks is at most 2^30
+    int32_t uncut;       // keys that a tile of 16 rows may see and is not cut
 };
 
 // A piece of work: a tile of TM packed rows of one sequence against a run of the keys they see.
@@ -87,8 +87,8 @@ __host__ __device__ __forceinline__ int token_of(const AttnArgs &a, int row) { r
 // 64 keys, 8 KV heads: 64 sequences 6.2 us, 256 25, 1024 168, 4096 1787 (the read of their keys: 2.8, 11, 45, 180); over 2048 keys 256 sequences 359 us and
 // 1024 1445, the read's rate.
 //
-// SINKS: a.sinks may be more than 0 (without it the code has nothing of that).
-template <bool MIXED, typename WAVE, bool SINKS = true>
+// SINKS: a.sinks may be more than 0; UNCUT: a.uncut may be (without them the code has nothing of that).
+template <bool MIXED, typename WAVE, bool SINKS = true, bool UNCUT = true>
 struct Division {
     const AttnArgs &a;
     const lvr_paged_batch &b;
@@ -121,7 +121,7 @@ struct Division {
     __host__ __device__ __forceinline__ bool is_wide() const { return wide((s1 - s0) * G); }
     __host__ __device__ __forceinline__ void cut() {
         runs = 1;
-        if (L == NO_CUTS || (span <= a.uncut && !is_wide())) return;
+        if (L == NO_CUTS || (UNCUT && span <= a.uncut && !is_wide())) return;
         int L1 = L;
         if (MIXED && any_wide && !is_wide()) L1 = L1 > 4 * MIN_RUN ? L1 >> 2 : (L1 < MIN_RUN ? L1 : MIN_RUN);
         if (MIXED) {
