@@ -1,7 +1,7 @@
 // The paged cache: its handle, the calls' checks, and the kernels that move rows in (lvr_paged_append) and out
 // (lvr_paged_gather).  The attention over the pages is paged_attention.hip.
 //
-// Both kernels are bound by HBM: every row is read once and written once, in 16-byte accesses.
+// Both are bound by HBM where there is enough to move: every row is read once and written once, in 16-byte accesses (rows in 4 bits: of 4 to 16 bytes).
 #include <math.h>
 #include <stdlib.h>
 #include <string.h>
@@ -356,11 +356,13 @@ __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_
 // of its rows.  The angle is position times turns per position modulo one turn, which in 64-bit integers is one product with the
 // overflow dropped: no far position loses anything.
 //
-// Bound by HBM where there are tokens enough: 8192 tokens (48 rows each, bf16) 37 us on one axis and 41 to 44 on three, 5.4 and 4.6 to 4.9 TB/s read and written;
-// 1885 fp32 tokens of 80 rows 25 us, 6.2 TB/s.  One token: 4.2 us, the launch and three dependent trips (rows and lengths, table, store).
+// Bound by HBM where there are tokens enough: 8192 tokens (48 rows each, bf16) 36 us on one axis and 34 on three, 5.6 and 6.0 TB/s read and written;
+// 1885 fp32 tokens of 80 rows 24 us, 6.4 TB/s.  One token: 4.3 to 4.9 us a call, which the host takes 4.0 us to make; the kernel 2.7, the launch and three
+// dependent trips (rows and lengths, table, store).
 //
-// NORM: rows of K and q are normed first, the squares summed over the row's lanes.  FP4 (KT is the type of new rows then): the first waves of a
-// token take K and V, eight heads each, the others q.
+// NORM: rows of K and q are normed first, the squares summed over the row's lanes while the sines are made (8192 such tokens on three axes 38 us, one token
+// as without).  FP4 (KT is the type of new rows then): the first waves of a token take K and V, eight heads each, the others q.  Those need the largest
+// magnitude of every block after the norm and the rotation, in 64 bits: 8192 tokens of the same heads on one axis 35 us, 101 MB read and 76 written, 5.0 TB/s.
 template <typename KT, bool NEIGHBOURS, int PER, bool STREAM, bool NORM, bool FP4>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_paged_batch b) {
     constexpr int ELT = sizeof(KT) == 4 ? 4 : 2, E = 16 / ELT, LANES = PAIRS / E, ROWS = 64 / LANES;
@@ -505,7 +507,8 @@ __global__ void __launch_bounds__(256) paged_gather_kernel(const char *k_pages, 
     }
 }
 
-// Pages in 4 bits, as rows of bf16.  Four lanes' worth of codes are one block: a lane takes eight of them to 16 bytes.
+// Pages in 4 bits, as rows of bf16.  Four lanes' worth of codes are one block: a lane takes eight of them to 16 bytes.  Bound by the store of rows that are
+// 3.8 times as long as what is read: 32768 keys of 8 heads 30 us (134 MB written, 36 read), 5.7 TB/s.
 template <bool STREAM>
 __global__ void __launch_bounds__(256) paged_gather_fp4_kernel(const char *k_pages, const char *v_pages, char *K, char *V, int64_t n,
                                                                int32_t n_kv, lvr_paged_batch b) {

@@ -1,4 +1,4 @@
-// Attention of new tokens over the pages (lvr_paged_attention).
+// Attention of new tokens over the pages (lvr_paged_attention, lvr_paged_sink_attention).
 //
 // The query rows that share a KV head are packed: row = token * G + (head within the group), so that a token's G heads, and the
 // tokens of a chunk, fill the columns of a matrix instruction whatever G is.  Both products are taken transposed,
@@ -9,6 +9,11 @@
 // Softmax in one pass, base 2 (the logit is score * sigma * log2 e in one fused multiply-add with the running maximum).  The
 // maximum is raised, and what was summed so far rescaled, only when a score passes it by more than RAISE: until then
 // weights grow up to 2^RAISE, which costs nothing in fp32 sums, and no lane has to ask another one for a maximum.
+//
+// Pages in 4 bits are read as they are, a code and its scale making a bf16 value exactly; from there on everything is as for bf16 pages.  (Matrix
+// instructions that take the codes themselves would need weights in fewer bits than bf16, and add up with some 14 bits.)
+//
+// First keys that stay visible beside a window are the first places of what a tile sees, the window's follow them: nothing in between is read.
 #include "paged_division.h"
 
 namespace {
@@ -167,9 +172,10 @@ __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, i
 // coordinates each, and which coordinates share a result tile is free as well (tile u: coordinates 8 i + u).
 // bf16: two score tiles make one operand of 32 keys; a pair of V rows is woven into it by byte permutes.
 //
-// Bound by the read of K and V: 131072 keys of one sequence 99 us, 48 ragged sequences of up to 32768 keys 362 us (1.97 GB), both 5.4 TB/s.
-// Short contexts are bound by dependent trips (lengths, table, rows, products, partial results): 2048 keys 10 us, in runs of 64 keys, for which two of the
+// Bound by the read of K and V: 131072 keys of one sequence 98 us, 48 ragged sequences of up to 32768 keys 359 us (1.97 GB), both 5.5 TB/s.
+// Short contexts are bound by dependent trips (lengths, table, rows, products, partial results): 2048 keys 8.5 us, in runs of 64 keys, for which two of the
 // four waves have none.  Rows asked for a turn ahead: no gain, and fp32 spills; eight waves to a workgroup: 12.1 us at 2048 keys where four took 11.3.
+// First keys: 24 long sequences with a window of 4096 and four of them 89 us (403 MB, 4.5 TB/s), bound by the last pieces' end: 576 of one length on 256 compute units.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <typename KT>
 struct Rows16;
@@ -285,6 +291,10 @@ struct Rows16<lvr_f32_t> {
 
 // Pages in 4 bits.  Lanes (i, b) hold block b of a key's row, 32 coordinates with one scale, and of V the eight coordinates that they hold in bf16; both
 // become bf16 in registers, exactly.
+//
+// Bound by the read where a batch is even (5.6 TB/s): 131072 keys of one sequence 33 us (143 MB; the launch, the division and two merges take 8 of them), 48
+// ragged sequences of up to 32768 keys 109 us (525 MB, 4.8 TB/s: the pieces' starts and ends weigh four times as much as beside bf16 rows).  2048 keys 8.5 us as in
+// bf16, by the same dependent trips.
 template <>
 struct Rows16<lvr_fp4_t> {
     static constexpr int ELT = 2;
@@ -651,7 +661,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 // 32 rows to a wave and two workgroups to a compute unit: 128 KiB of LDS and up to 256 registers a lane, so that one workgroup's matrix
 // instructions meet the other's exponentials.  A prompt of 16384 tokens (32 heads on 8, 2.2 TFLOP): 2.1 to 2.25 ms on different cards, 980 to
 // 1050 TFLOP/s; matrix units busy 46 % and vector units 42 % of the clocks, where the library's product of 8192 x 8192 matrices reaches
-// 1148 TFLOP/s.  fp32, 8192 tokens: 134 TFLOP/s of the 154 the library reaches.  Tried without gain: the scores of the next tile made
+// 1148 to 1409 TFLOP/s.  fp32, 8192 tokens: 135 TFLOP/s of the 154 the library reaches.  Tried without gain: the scores of the next tile made
 // between the exponentials of this one (-2 %), wave priorities around the products, tiles through registers (653 TFLOP/s: the loads were
 // waited for at once).
 // ---------------------------------------------------------------------------------------------------------------------------
@@ -769,7 +779,9 @@ struct Rows128<lvr_f32_t> {
     }
 };
 
-// Pages in 4 bits: a tile becomes bf16 on its way into LDS and is worked on as such.
+// Pages in 4 bits: a tile becomes bf16 on its way into LDS and is worked on as such.  Codes pass through registers, a block and its scale a lane; they are asked
+// for a tile ahead and widened while this one's products run.  Bound as in bf16: the prompt of 16384 tokens 2.09 to 2.14 ms, widening hides behind the read that it saves
+// (matrix units busy 42 % and vector units 45 % of the clocks).
 template <>
 struct Rows128<lvr_fp4_t> : Rows128<lvr_bf16_t> {};
 

@@ -84,7 +84,7 @@ __host__ __device__ __forceinline__ int token_of(const AttnArgs &a, int row) { r
 // get there with the shortest runs).
 //
 // A batch of up to 64 sequences stays in registers.  Of a larger one every wave reads the lengths anew, to divide it and to find its piece: single tokens over
-// 64 keys, 8 KV heads: 64 sequences 6.2 us, 256 25, 1024 168, 4096 1787 (the read of their keys: 2.8, 11, 45, 180); over 2048 keys 256 sequences 359 us and
+// 64 keys, 8 KV heads: 64 sequences 7.1 us, 256 25, 1024 180, 4096 1848 (the read of their keys: 2.8, 11, 45, 180); over 2048 keys 256 sequences 359 us and
 // 1024 1445, the read's rate.
 //
 // SINKS: a.sinks may be more than 0; UNCUT: a.uncut may be (without them the code has nothing of that).
