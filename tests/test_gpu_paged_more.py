@@ -220,6 +220,13 @@ def test_first_keys_over_heads_and_pages(hq, hkv, page, layout, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens", [[(97, 208), (97, 107)], [(40, 41), (1, 300), (129, 129)]])
+def test_first_keys_with_a_kv_head_to_every_query_head(lens, dtype):
+    with More(lens, dtype=dtype, hq=8, hkv=8, page=16, layout="token", seed=133) as c:
+        check(c, 54, 4)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("hq, lens, window, sinks", [(8, [(1, 30000)], 6000, 3000), (4, [(17, 9000), (1, 9000)], 3000, 100), (2, [(200, 5000)], 1700, 900)])
 def test_first_keys_cut_into_runs(hq, lens, window, sinks, dtype):
     with More(lens, dtype=dtype, hq=hq, hkv=1, page=64, seed=112) as c:
@@ -444,6 +451,17 @@ def test_appends_of_many_rows(hq, hkv, lens, dtype):
         assert c.T * (hq + 2 * hkv) >= 16384
         check_append(c, f, norm=True, weights=weights_of(c))
         check_append(c, f, norm=False)
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [62, 63, 64, 65, 130])
+def test_appends_of_as_many_sequences_as_a_wave_has_lanes(n, dtype, norm):
+    """On both sides of 63 a token's sequence is found in different ways; among them sequences that bring nothing, the first and the last too."""
+    f = freqs(32)
+    lens = [((i * 5) % 4, 4 + (i * 37) % 60) for i in range(n - 1)] + [(0, 9)]
+    with More(lens, dtype=dtype, hq=2, hkv=2, rot_dim=32, inv_freq=f, seed=132, behind=2, gap=1) as c:
+        check_append(c, f, norm=norm, weights=weights_of(c))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
