@@ -78,7 +78,7 @@ __host__ __device__ __forceinline__ int token_of(const AttnArgs &a, int row) { r
 // A sequence's tiles are cut into runs of keys of one length, as many as make about `target` pieces of the batch (but none under
 // MIN_RUN keys; target 0: no cuts).  L is the keys of all tiles over target, where a tile sees half of the sequence's own new keys.
 // Tiles of 128 rows are cut into span / L runs, rounded, so that equal ones fill whole rounds of workgroups; beside them tiles of 16 rows,
-// whose partial results are small, into runs of a quarter of that.  Without tiles of 128 rows the number is rounded up.  There is
+// whose partial results are small, into runs of a quarter of that.  Without tiles of 128 rows the number is rounded up (but see level).  There is
 // room for the partial results of 2 * target pieces of cut 128-row tiles and for 3 * target pieces of cut tiles altogether, and the
 // launch has as many workgroups beside one for each tile: should there be more, L grows until there are not (prompts of a few hundred tokens
 // get there with the shortest runs).
@@ -133,6 +133,19 @@ struct Division {
         }
         run = (about<WAVE>(span, runs) + 64) & ~63;   // the last run takes what is left, whatever was rounded
     }
+    // Sequences of one tile each that all go into as many runs: where rounding up made more pieces than wanted, as many as are wanted at most.  Pieces of one
+    // length that pass a whole round by a few end late (us rounded up / so, 8 KV heads: 12 sequences of 8192 keys bf16 88 / 77, 4 bits 32.5 / 27.1, fp32 166 / 145; 20 of
+    // 4096 74 / 66; 5 of 8192 43.5 / 38.3; 3 of them 27.7 / 23.1).
+    __host__ __device__ __forceinline__ void level(int target) {
+        const uint64_t with = WAVE::ballot(tiles == 1);
+        if (with == 0) return;
+        const int r = WAVE::of(runs, __builtin_ctzll(with)), count = __builtin_popcountll(with);
+        if (r * count <= target || WAVE::any(tiles > 1 || (tiles == 1 && runs != r))) return;
+        const int less = divide_small<WAVE>(target, count);
+        if (less < 2) return;
+        runs = less;
+        run = (about<WAVE>(span, runs) + 64) & ~63;
+    }
     __host__ __device__ __forceinline__ Division(const AttnArgs &args, const lvr_paged_batch &bt) : a(args), b(bt), G(a.G), window(a.window), narrow(a.narrow) {}
     // false: seq_start is not ascending, no piece is where another expects it
     __host__ __device__ __forceinline__ bool divide(int target) {
@@ -158,7 +171,10 @@ struct Division {
         }
         if (!MIXED) {   // at most target pieces more than tiles, and at most 2 * target of cut tiles, since L is all keys over target
             n_wide = 0;
-            if (b.n_seqs <= LANES) cut();
+            if (b.n_seqs <= LANES) {
+                cut();
+                level(target);
+            }
             return true;
         }
         for (;; L = L < 1 << 28 ? (L + L / 2 + 63) & ~63 : NO_CUTS) {   // by half and never by less than 64: some 38 steps at most

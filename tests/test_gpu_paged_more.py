@@ -220,6 +220,15 @@ def test_first_keys_over_heads_and_pages(hq, hkv, page, layout, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("window, sinks", [(0, 0), (1300, 70)])
+@pytest.mark.parametrize("lens", [[(1, 1630)] * 5, [(1, 1168)] * 7, [(1, 1363)] * 3, [(1, 1630), (0, 1630), (0, 0)] * 5, [(1, 1630)] * 4 + [(1, 1400)]])
+def test_batches_of_one_length(lens, window, sinks, dtype):
+    """Lengths at which as many runs as are wanted are no whole number for each sequence."""
+    with More(lens, dtype=dtype, hq=8, hkv=8, page=32, seed=134) as c:
+        check(c, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("lens", [[(97, 208), (97, 107)], [(40, 41), (1, 300), (129, 129)]])
 def test_first_keys_with_a_kv_head_to_every_query_head(lens, dtype):
     with More(lens, dtype=dtype, hq=8, hkv=8, page=16, layout="token", seed=133) as c:
