@@ -661,9 +661,10 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 // 32 rows to a wave and two workgroups to a compute unit: 128 KiB of LDS and up to 256 registers a lane, so that one workgroup's matrix
 // instructions meet the other's exponentials.  A prompt of 16384 tokens (32 heads on 8, 2.2 TFLOP): 2.1 to 2.25 ms on different cards, 980 to
 // 1050 TFLOP/s; matrix units busy 46 % and vector units 42 % of the clocks, where the library's product of 8192 x 8192 matrices reaches
-// 1148 to 1409 TFLOP/s.  fp32, 8192 tokens: 135 TFLOP/s of the 154 the library reaches.  Tried without gain: the scores of the next tile made
-// between the exponentials of this one (-2 %), wave priorities around the products, tiles through registers (653 TFLOP/s: the loads were
-// waited for at once).
+// 1148 to 1409 TFLOP/s.  fp32, 8192 tokens: 135 TFLOP/s of the 154 the library reaches.  One workgroup to a compute unit takes 1.43 times as long as two,
+// whose instructions meet for the most part.  Tried without gain: the scores of the next tile made
+// between the exponentials of this one (-2 %), V's operands read a step ahead (bf16 0 to 1 %, 4 bits -1 %), priority for exponentials (-2 to -6 %), tiles through registers (653
+// TFLOP/s: the loads were waited for at once).
 // ---------------------------------------------------------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -686,17 +687,23 @@ struct Rows128<lvr_bf16_t> {
     static __device__ __forceinline__ int key_of(int h, int kt, int r) { return 32 * kt + 16 * (r >> 3) + 8 * h + (r & 7); }
     static __device__ __forceinline__ int coordinate(int h, int dt, int r) { return 32 * dt + 8 * (r >> 2) + 4 * h + (r & 3); }
     static __device__ __forceinline__ void scores(const char *k, const Q &q, int n, int h, f32x16 (&s)[NT]) {
+        // 32 keys' operands are read at once, the other 32 keys' while those are worked on (read as they are needed: 1 to 4 % slower)
+        static_assert(NT == 2, "");
+        bf16x8 f[NT][8];
+        s[0] = f32x16{0.f}, s[1] = f32x16{0.f};
+        auto read = [&](int kt, int st) { f[kt][st] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(k + (kt * 32 + n) * ROWB + k_piece(n, 2 * st + h) * 16)); };
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kt = 0; kt < NT; ++kt) {
-            f32x16 c = {0.f};
-            const char *row = k + (kt * 32 + n) * ROWB;
+        for (int st = 0; st < 8; ++st) read(0, st);
 #pragma unroll
-            for (int st = 0; st < 8; ++st) {
-                const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(row + k_piece(n, 2 * st + h) * 16));
-                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[st], c, 0, 0, 0);
-            }
-            s[kt] = c;
+        for (int st = 0; st < 8; ++st) {
+            __builtin_amdgcn_sched_barrier(0);
+            read(1, st);
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[0][st], q[st], s[0], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int st = 0; st < 8; ++st) s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[1][st], q[st], s[1], 0, 0, 0);
     }
     static __device__ __forceinline__ void add(const char *v, const f32x16 (&p)[NT], int lane, f32x16 (&o)[4], float &l) {
         const int i16 = lane & 15, key = (lane >> 5) * 8 + (i16 >> 2);
@@ -797,8 +804,12 @@ struct Rows128Lds {
     uint32_t odd[2][4];   // (FP4) whether a wave's rows of V have a block that is no number
 };
 
+// urgent: a second product goes before what the other workgroup on the compute unit has to do.  Two that begin together else stay in step, both at
+// their products and then both at their exponentials.  us without / with: bf16, prompt of 4096 160.6 / 153.4, 1000 new tokens of 12000 211 / 203; 4 bits 160 / 152 and 211 / 201;
+// fp32 prompt of 2048 349 / 317.  Not so where workgroups follow one another and are out of step by themselves: prompt of 16384 with it 2.06 to 2.12 ms and without 2.08 to 2.11,
+// 8192 with a window of 2048 297 and 288.  The rule is up to two rounds of pieces; four prompts of 1024 lose by it (64.0 / 65.6, 4 bits 64.8 / 68.5).
 template <typename KT, bool SINKS>
-__device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, Rows128Lds<KT> &lds) {
+__device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, bool urgent, Rows128Lds<KT> &lds) {
     typedef Rows128<KT> R;
     constexpr int TK = R::TK, LPR = R::PIECES, RPI = 64 / LPR;   // lanes to a row, rows to a load of the wave
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -968,7 +979,9 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
             for (int kt = 0; kt < R::NT; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) p[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[kt][r], a.unit, -base));
+            if (urgent) __builtin_amdgcn_s_setprio(1);
             R::add(v, p, lane, o, l);
+            if (urgent) __builtin_amdgcn_s_setprio(0);
         }
         if constexpr (FP4)
             if (place + TK < t.end) unfold(place + TK, next_none, next_k, next_v, lds.odd[buf ^ 1]);
@@ -1068,7 +1081,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
     Tile t;
     Division<true, Wave, SINKS, may_be_uncut<KT, SINKS>> d(a, bt);
     if (!d.divide(a.target) || !d.template locate<false>(piece, t)) return;
-    if (t.height == 128) rows128_piece<KT, SINKS>(a, bt, t, kvh, lds.wide);
+    if (t.height == 128) rows128_piece<KT, SINKS>(a, bt, t, kvh, d.n_wide * a.n_kv <= 2 * MIXED_PIECES, lds.wide);
     else rows16_piece<KT, SINKS>(a, bt, t, kvh, lds.narrow);
 }
 
