@@ -180,6 +180,8 @@ def _early_stream(stream):
     if _lib is None or _call is None:   # (the library is loaded by the first call)
         return None
     try:
+        if stream is None:              # as a number, without the steps of _stream: 0.2 us of the 4 that a small call takes the host
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         return _stream(stream)
     except Exception:
         return None

@@ -74,6 +74,15 @@ bool address(PyObject *o, void *&p) {
     return true;
 }
 
+// A stream: such an object, or its number.
+bool stream_of(PyObject *o, void *&p) {
+    if (!PyLong_CheckExact(o)) return address(o, p);
+    p = PyLong_AsVoidPtr(o);
+    if (!PyErr_Occurred()) return true;
+    PyErr_Clear();
+    return false;
+}
+
 constexpr int F32 = (int)at::kFloat, I32 = (int)at::kInt;
 
 // The library's functions, handed over by the binding once it has loaded the library.
@@ -115,7 +124,7 @@ PyObject *decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *h, *st;
     Held q, tau, out, idx, count;
     LVR_PLAIN(LVR_NOT_PLAIN(n == 7 && lib.decode_step && address(a[0], h) && held(a[1], F32, q) && held(a[2], F32, tau) && held(a[3], F32, out) &&
-                            held(a[4], I32, idx) && idx.n_dims > 0 && held(a[5], I32, count) && address(a[6], st));)
+                            held(a[4], I32, idx) && idx.n_dims > 0 && held(a[5], I32, count) && stream_of(a[6], st));)
     const int64_t cap = idx.dims[idx.n_dims - 1];
     return result_of([&] {
         return lib.decode_step(static_cast<lvr_index *>(h), (const float *)q.p, (const float *)tau.p, (float *)out.p, (int32_t *)idx.p,
@@ -129,7 +138,7 @@ PyObject *append_decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Held k, v, q, tau, out, idx, count;
     LVR_PLAIN(LVR_NOT_PLAIN(n == 9 && lib.append_decode_step && address(a[0], h) && held(a[1], -1, k) && k.n_dims > 2 && held(a[2], -1, v) &&
                             held(a[3], F32, q) && held(a[4], F32, tau) && held(a[5], F32, out) && held(a[6], I32, idx) && idx.n_dims > 0 &&
-                            held(a[7], I32, count) && address(a[8], st));)
+                            held(a[7], I32, count) && stream_of(a[8], st));)
     const int64_t cap = idx.dims[idx.n_dims - 1], m = k.dims[2];
     return result_of([&] {
         return lib.append_decode_step(static_cast<lvr_index *>(h), k.p, v.p, m, (const float *)q.p, (const float *)tau.p, (float *)out.p,
@@ -142,7 +151,7 @@ PyObject *query(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *h, *st;
     Held q, tau, idx, count;
     LVR_PLAIN(LVR_NOT_PLAIN(n == 6 && lib.query && address(a[0], h) && held(a[1], F32, q) && held(a[2], F32, tau) && held(a[3], I32, idx) &&
-                            idx.n_dims > 0 && held(a[4], I32, count) && address(a[5], st));)
+                            idx.n_dims > 0 && held(a[4], I32, count) && stream_of(a[5], st));)
     const int64_t cap = idx.dims[idx.n_dims - 1];
     return result_of([&] {
         return lib.query(static_cast<lvr_index *>(h), (const float *)q.p, (const float *)tau.p, (int32_t *)idx.p, (int32_t *)count.p, cap, st);
@@ -154,7 +163,7 @@ PyObject *sparse_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *h, *st;
     Held q, idx, count, out;
     LVR_PLAIN(LVR_NOT_PLAIN(n == 6 && lib.sparse_attention && address(a[0], h) && held(a[1], F32, q) && held(a[2], I32, idx) && idx.n_dims > 0 &&
-                            held(a[3], I32, count) && held(a[4], F32, out) && address(a[5], st));)
+                            held(a[3], I32, count) && held(a[4], F32, out) && stream_of(a[5], st));)
     const int64_t cap = idx.dims[idx.n_dims - 1];
     return result_of([&] {
         return lib.sparse_attention(static_cast<lvr_index *>(h), (const float *)q.p, (const int32_t *)idx.p, (const int32_t *)count.p, cap,
@@ -166,7 +175,7 @@ PyObject *sparse_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyObject *dense_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *h, *st;
     Held q, out;
-    LVR_PLAIN(LVR_NOT_PLAIN(n == 4 && lib.dense_attention && address(a[0], h) && held(a[1], F32, q) && held(a[2], F32, out) && address(a[3], st));)
+    LVR_PLAIN(LVR_NOT_PLAIN(n == 4 && lib.dense_attention && address(a[0], h) && held(a[1], F32, q) && held(a[2], F32, out) && stream_of(a[3], st));)
     return result_of([&] { return lib.dense_attention(static_cast<lvr_index *>(h), (const float *)q.p, (float *)out.p, st); });
 }
 
@@ -181,7 +190,7 @@ PyObject *sparse_attention_static(PyObject *, PyObject *const *a, Py_ssize_t n) 
         LVR_NOT_PLAIN(n == 8 && lib.sparse_attention_static && is_plain(a[0], K) && is_plain(a[1], V) && K->dim() == 4 && K->sizes() == V->sizes() &&
                       K->scalar_type() == V->scalar_type() && (K->scalar_type() == at::kBFloat16 || K->scalar_type() == at::kFloat) &&
                       held(a[2], F32, q) && q.n_dims > 1 && held(a[3], I32, idx) && idx.n_dims > 0 && held(a[4], I32, count) &&
-                      held(a[5], F32, out) && PyFloat_CheckExact(a[6]) && address(a[7], st));
+                      held(a[5], F32, out) && PyFloat_CheckExact(a[6]) && stream_of(a[7], st));
         scale = PyFloat_AS_DOUBLE(a[6]);
         kp = K->data_ptr();
         vp = V->data_ptr();)
@@ -259,7 +268,7 @@ struct Paged {
     // (h, address of its configuration, its device, ..., stream)
     bool begin(PyObject *o_h, PyObject *o_cfg, PyObject *o_device, PyObject *o_stream) {
         void *hp;
-        if (!address(o_h, hp) || !PyLong_CheckExact(o_cfg) || !PyLong_CheckExact(o_device) || !address(o_stream, stream)) return false;
+        if (!address(o_h, hp) || !PyLong_CheckExact(o_cfg) || !PyLong_CheckExact(o_device) || !stream_of(o_stream, stream)) return false;
         device = (int)PyLong_AsLong(o_device);
         h = static_cast<lvr_paged *>(hp);
         c = static_cast<const lvr_paged_config *>(PyLong_AsVoidPtr(o_cfg));
