@@ -21,6 +21,7 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float RAISE = 8.f;
 constexpr int MERGE_WGS = 1024;
+constexpr int COMPUTE_UNITS = 256, IN_STEP_RUN = 1024;
 constexpr int FAN_BITS = 3, FAN = 1 << FAN_BITS;   // partial results of 16-row tiles that a wave merges at a time
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -364,7 +365,8 @@ struct Rows16Lds {
     unsigned arrived;
 };
 
-template <typename KT, bool SINKS>
+// ALONE: there are tiles of 16 rows alone
+template <typename KT, bool SINKS, bool ALONE>
 __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, Rows16Lds &lds) {
     typedef Rows16<KT> R;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -400,7 +402,16 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     for (int j = 0; j < 4; ++j) v_place[j] = (4 * b + j) * row + i * 4;
     const int first_place = t.begin + wave * 32, turns = first_place < t.end ? (t.end - first_place + 127) / 128 : 0;
     auto key_of_turn = [&](int turn) { return key_at<SINKS>(t, first_place + turn * 128); };
-    // The pages of 32 turns are looked up at once, by one lane for each 16 keys, which lie in one page.  Where there is none, some memory of the pool.
+    // fp32, tiles of a sequence that read the same long runs, a workgroup to a compute unit at most: all loads of a turn go before its products,
+    // which keeps the tiles together.  us so / with the loads among the products, one sequence, 32 heads on 8: 8 tokens over 32768 keys 66 / 71,
+    // 16 tokens 101 / 111, over 131072 keys 364 / 400.  With more workgroups the products of one hide the loads of another, and short runs end
+    // sooner: 8 x 16 tokens over 32768 keys 869 / 752, 12 tokens of one sequence 152 / 136, one token over 64 keys 6.7 / 6.4, 2048 keys
+    // 12.1 / 11.6.  bf16: no gain (one token over 64 keys 4.85 / 4.75, 131072 keys 97 / 97).
+    const bool in_step = ALONE && __is_same(KT, lvr_f32_t) && t.rows > 16 && t.end - t.begin >= IN_STEP_RUN &&
+                         (int64_t)bt.n_seqs * ((t.rows + 15) >> 4) * t.splits * a.n_kv <= COMPUTE_UNITS;
+    // There, and on pages in 4 bits, the pages of 32 turns are looked up at once, by one lane for each 16 keys, which lie in one page.  Where there is
+    // none, some memory of the pool.  (Other tiles often end after a turn or two: 1024 single tokens over 200 keys, bf16, 260 us so, 250 with a
+    // look-up for each 16 keys.)
     struct {
         int page;                   // or, of FP4, what is added to a pool's address for the codes (low, high), and to that for the scales
         uint32_t low, high;
@@ -419,6 +430,15 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
             place_of.high = (uint32_t)(at >> 32);
             place_of.scales = (int32_t)bt.scales + (none ? 0 : (int32_t)(in_page / 16) - (int32_t)in_page);
             without = __ballot(none);
+        }
+    };
+    auto ask_rows = [&](int page, int key, Keys &x, int h) {   // (not FP4)
+        if constexpr (!FP4) {
+            const int64_t at = lvr_row_at(bt, page < 0 ? 0 : page, kvh, page < 0 ? 0 : key);   // no page: some memory of the pool
+            const char *kp = a.k_pages + at, *vp = a.v_pages + at;
+            R::load_k(kp + i * bt.row_stride, b, x.k[h]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) R::load_v(vp + (4 * b + j) * bt.row_stride, i, x.v[h][j]);
         }
     };
     auto ask = [&](int turn, Keys &x) {
@@ -447,45 +467,32 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
             } else {
                 const int page = __builtin_amdgcn_readlane(place_of.page, who);
                 x.none[h] = page < 0;
-                const int64_t at = lvr_row_at(bt, x.none[h] ? 0 : page, kvh, x.none[h] ? 0 : k0 + h * 16);
-                const char *kp = a.k_pages + at, *vp = a.v_pages + at;
-                R::load_k(kp + i * bt.row_stride, b, x.k[h]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) R::load_v(vp + (4 * b + j) * bt.row_stride, i, x.v[h][j]);
+                ask_rows(page, k0 + h * 16, x, h);
             }
         }
     };
-    auto work = [&](int k0, Keys &x) {
-        const bool partly = !all_seen<SINKS>(a, k0, 32, row_begin, row_end) || x.none[0] || x.none[1];
-        float p[2][4];
+    // 16 keys from `key0` on, not all of which every row of the tile sees; whether V has a value that some rows must not meet.
+    auto hide = [&](int key0, bool none, float (&p)[4], auto &v) {
         bool poison = false;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const f32x4 s = R::score(x.k[h], q);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p[h][j] = s[j];
+        for (int j = 0; j < 4; ++j) {
+            const int key = key0 + 4 * b + j;
+            if (none || hidden<SINKS>(a, key, first, last)) p[j] = -INFINITY;
+            // a row of V that no query row sees is memory nobody has written; one that some see meets the others with
+            // weight zero, which an infinity or a NaN would survive
+            const bool unseen = none || hidden<SINKS>(a, key, t.lo, t.hi - 1);
+            if constexpr (FP4) v.codes[j] = unseen ? 0 : v.codes[j];
+            else if (unseen) R::zero_v(v[j]);
+            else if (R::odd_v(v[j])) poison = true;
         }
-        if (partly) {
-            if (FP4) asm volatile("");   // one branch
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = k0 + h * 16 + 4 * b + j;
-                    if (x.none[h] || hidden<SINKS>(a, key, first, last)) p[h][j] = -INFINITY;
-                    // a row of V that no query row sees is memory nobody has written; one that some see meets the others with
-                    // weight zero, which an infinity or a NaN would survive
-                    const bool unseen = x.none[h] || hidden<SINKS>(a, key, t.lo, t.hi - 1);
-                    if constexpr (FP4) x.v[h].codes[j] = unseen ? 0 : x.v[h].codes[j];
-                    else if (unseen) R::zero_v(x.v[h][j]);
-                    else if (R::odd_v(x.v[h][j])) poison = true;
-                }
-                if constexpr (FP4) {   // the key whose scales this lane has
-                    if (x.none[h] || hidden<SINKS>(a, k0 + h * 16 + 4 * b + (i & 3), t.lo, t.hi - 1)) x.v[h].scales = 0x7f7f7f7f;
-                    else if (R::own_scale(x.v[h]) == 255) poison = true;
-                }
-            }
+        if constexpr (FP4) {   // the key whose scales this lane has
+            if (none || hidden<SINKS>(a, key0 + 4 * b + (i & 3), t.lo, t.hi - 1)) v.scales = 0x7f7f7f7f;
+            else if (R::own_scale(v) == 255) poison = true;
         }
+        return poison;
+    };
+    // The scores become weights.
+    auto weigh = [&](float (&p)[2][4]) {
         float top = p[0][0];
 #pragma unroll
         for (int c = 1; c < 8; ++c) top = fmaxf(top, p[c >> 2][c & 3]);
@@ -503,28 +510,69 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
         const float base = m == -INFINITY ? 0.f : m;   // nothing seen so far: every weight below is 2^-inf
 #pragma unroll
         for (int c = 0; c < 8; ++c) p[c >> 2][c & 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[c >> 2][c & 3], a.unit, -base));
+    };
+    auto work = [&](int k0, Keys &x) {
+        const bool partly = !all_seen<SINKS>(a, k0, 32, row_begin, row_end) || x.none[0] || x.none[1];
+        float p[2][4];
+        bool poison = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 s = R::score(x.k[h], q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[h][j] = s[j];
+        }
+        if (partly) {
+            if (FP4) asm volatile("");   // one branch
+#pragma unroll
+            for (int h = 0; h < 2; ++h) poison |= hide(k0 + h * 16, x.none[h], p[h], x.v[h]);
+        }
+        weigh(p);
         redo |= poison;
         R::add(x.v, p, o, l);
     };
-    if constexpr (!FP4) {
+    if constexpr (FP4) {
+        if (turns > 0) {
+            // Rows are asked for a turn ahead.  The last turn asks for its own again, so that there are always as many loads behind the ones that
+            // are waited for.  (Two turns ahead take registers that a fourth workgroup on a compute unit needs: 2 to 5 % slower.)
+            Keys x, y;
+            ask(0, x);
+            for (int turn = 0;;) {
+                ask(turn + 1, y);
+                work(key_of_turn(turn), x);
+                if (++turn >= turns) break;
+                ask(turn + 1, x);
+                work(key_of_turn(turn), y);
+                if (++turn >= turns) break;
+            }
+        }
+    } else if (in_step) {
         for (int turn = 0; turn < turns; ++turn) {   // uniform over the wave
             Keys x;
             ask(turn, x);
-            __builtin_amdgcn_sched_barrier(0);   // all loads on their way before one is waited for (fp32, 131072 keys: 200 us without, 187)
+            __builtin_amdgcn_sched_barrier(0);   // all loads on their way before one is waited for
             work(key_of_turn(turn), x);
         }
-    } else if (turns > 0) {
-        // Rows are asked for a turn ahead.  The last turn asks for its own again, so that there are always as many loads behind the ones that
-        // are waited for.  (Two turns ahead take registers that a fourth workgroup on a compute unit needs: 2 to 5 % slower.)
-        Keys x, y;
-        ask(0, x);
-        for (int turn = 0;;) {
-            ask(turn + 1, y);
-            work(key_of_turn(turn), x);
-            if (++turn >= turns) break;
-            ask(turn + 1, x);
-            work(key_of_turn(turn), y);
-            if (++turn >= turns) break;
+    } else {
+        for (int place = first_place; place < t.end; place += 128) {   // uniform over the wave
+            const int k0 = key_at<SINKS>(t, place);
+            Keys x;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {   // 16 keys: one page
+                const int key = k0 + h * 16, page = key < t.hi ? __builtin_amdgcn_readfirstlane(lvr_page_of(bt, t.seq, key)) : -1;
+                x.none[h] = page < 0;
+                ask_rows(page, key, x, h);
+            }
+            const bool partly = !all_seen<SINKS>(a, k0, 32, row_begin, row_end) || x.none[0] || x.none[1];
+            float p[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {   // (masked one by one, so that the second half's loads may follow the first half's products)
+                const f32x4 s = R::score(x.k[h], q);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[h][j] = s[j];
+                if (partly) redo |= hide(k0 + h * 16, x.none[h], p[h], x.v[h]);
+            }
+            weigh(p);
+            R::add(x.v, p, o, l);
         }
     }
     l += __shfl_xor(l, 16, 64);
@@ -1069,7 +1117,7 @@ __global__ void __launch_bounds__(256, __is_same(KT, lvr_fp4_t) ? 4 : 2) paged_a
     const int piece = piece_of_block<KT>(a, bt, kvh);
     Tile t;
     Division<false, Wave, SINKS, may_be_uncut<KT, SINKS>> d(a, bt);
-    if (d.divide(a.target) && d.template locate<false>(piece, t)) rows16_piece<KT, SINKS>(a, bt, t, kvh, lds);
+    if (d.divide(a.target) && d.template locate<false>(piece, t)) rows16_piece<KT, SINKS, true>(a, bt, t, kvh, lds);
 }
 
 // Any batch: every sequence in the tiles that suit it.
@@ -1082,7 +1130,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
     Division<true, Wave, SINKS, may_be_uncut<KT, SINKS>> d(a, bt);
     if (!d.divide(a.target) || !d.template locate<false>(piece, t)) return;
     if (t.height == 128) rows128_piece<KT, SINKS>(a, bt, t, kvh, d.n_wide * a.n_kv <= 2 * MIXED_PIECES, lds.wide);
-    else rows16_piece<KT, SINKS>(a, bt, t, kvh, lds.narrow);
+    else rows16_piece<KT, SINKS, false>(a, bt, t, kvh, lds.narrow);
 }
 
 // Merges the runs of cut 128-row tiles.  16 rows of a tile at a time, 16 lanes to a row; the workgroups share them out.  A launch of its own, unlike
