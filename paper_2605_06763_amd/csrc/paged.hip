@@ -416,6 +416,9 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
             cs[e] = turn.cs;
         }
     }
+    // The rows were asked for before the token's place and are there by now.  Told so, the compiler waits for nothing between the stores; else each pair
+    // of them for the one before (fp32, 8192 tokens 73.2 us without this and 69.9 with it, unrotated 73.0 and 69.6; bf16 gains nothing).
+    if (ELT == 4) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
 #pragma unroll
     for (int c = 0; c < PER; ++c) {
         const int row = row0 + c * ROWS;
