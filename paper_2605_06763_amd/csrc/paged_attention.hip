@@ -853,9 +853,17 @@ struct Rows128Lds {
 };
 
 // urgent: a second product goes before what the other workgroup on the compute unit has to do.  Two that begin together else stay in step, both at
-// their products and then both at their exponentials.  us without / with: bf16, prompt of 4096 160.6 / 153.4, 1000 new tokens of 12000 211 / 203; 4 bits 160 / 152 and 211 / 201;
-// fp32 prompt of 2048 349 / 317.  Not so where workgroups follow one another and are out of step by themselves: prompt of 16384 with it 2.06 to 2.12 ms and without 2.08 to 2.11,
-// 8192 with a window of 2048 297 and 288.  The rule is up to two rounds of pieces; four prompts of 1024 lose by it (64.0 / 65.6, 4 bits 64.8 / 68.5).
+// their products and then both at their exponentials.  us without / with, bf16, fp32, 4 bits:
+//   one round of pieces: 1000 new tokens of 12000            215 / 209    1505 / 1486    216 / 204
+//                        two sequences of 512 new of 8192     157 / 153   1049 / 1037    157 / 150
+//   two rounds, one or two sequences: prompt of 4096          164 / 158   1161 / 1096    164 / 155
+//               prompt of 2048                                 65 / 64     350 / 319      66 / 62
+//               two prompts of 2048                            94 / 93     618 / 581      93 / 93
+//   two rounds, more of them: four prompts of 1024             66 / 68     397 / 415      66 / 69
+//               16 ragged ones of up to 500 new of 3000        62 / 67     305 / 331      61 / 64
+//               four of 1024 new of 4096, a window of 1000     98 / 104    550 / 554      93 / 98
+// (A prompt of 3000, a round and a half, loses by it: 94 / 98, 627 / 628, 93 / 98.)
+// In three rounds workgroups are out of step by themselves (prompt of 16384 nothing, of 8192 with a window of 2048 288 / 297).
 template <typename KT, bool SINKS>
 __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, bool urgent, Rows128Lds<KT> &lds) {
     typedef Rows128<KT> R;
@@ -1129,7 +1137,7 @@ __global__ void __launch_bounds__(256, 2) paged_attention_mixed_kernel(AttnArgs 
     Tile t;
     Division<true, Wave, SINKS, may_be_uncut<KT, SINKS>> d(a, bt);
     if (!d.divide(a.target) || !d.template locate<false>(piece, t)) return;
-    if (t.height == 128) rows128_piece<KT, SINKS>(a, bt, t, kvh, d.n_wide * a.n_kv <= 2 * MIXED_PIECES, lds.wide);
+    if (t.height == 128) rows128_piece<KT, SINKS>(a, bt, t, kvh, d.n_wide * a.n_kv <= (bt.n_seqs <= 2 ? 2 : 1) * MIXED_PIECES, lds.wide);
     else rows16_piece<KT, SINKS, false>(a, bt, t, kvh, lds.narrow);
 }
 
