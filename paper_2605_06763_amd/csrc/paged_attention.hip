@@ -1187,13 +1187,12 @@ hipError_t lvr_launch_paged_attention(lvr_paged *pc, const lvr_paged_batch &b, c
     a.q = static_cast<const char *>(q);
     a.out = static_cast<char *>(out);
     a.q_stride = q_stride_bytes;
-    a.window = (int64_t)window + sinks < 1 << 30 ? window : 0;   // no sequence is longer
-    a.sinks = a.window ? sinks : 0;
+    a.window = window;
+    a.sinks = sinks;
     a.unit = pc->sigma * LOG2E;
     a.part = pc->part;
     a.ticket = pc->ticket;
     const int type = pc->cfg.kv_dtype;
-    a.uncut = type == LVR_FP4 ? UNCUT_FP4 : (type == LVR_BF16 && a.sinks ? UNCUT_BF16 : 0);
     const PagedLaunch launch = paged_launch(a, b, pc->cfg.n_q_heads, pc->cfg.n_kv_heads, type != LVR_F32, type == LVR_FP4);
     const dim3 grid = grid_of(a.n_kv, launch.pieces);
 #define LVR_LAUNCH(KERNEL, KT, GRID)                                                                                  \

@@ -20,9 +20,10 @@ constexpr int MIN_RUN = 64;
 // eight such sequences of 4096 keys 41 / 58; fp32 171 / 98).  The rule goes by the rows alone, and for bf16 takes the side on which many sequences gain.
 constexpr int NARROW_BF16 = 32, NARROW_F32 = 64;
 constexpr int NARROW_FP4_ALONE = 64;   // of all sequences together, on pages in 4 bits (16 tokens, 32 heads on 8, over 32768 keys: 49 us in a tile of 128, 28 in four of 16)
-// Keys up to which a tile of 16 rows is not cut, on pages in 4 bits and on bf16 ones with first keys: a workgroup takes 0.6 us for 128 of them in 4 bits, merging
-// takes three (us uncut / in runs of 64: one token over 256 keys in 4 bits 6.1 / 8.8, 512 7.3 / 8.8, 16 of them over 512 7.8 / 11.0; bf16, a window of 64
-// with four first keys 8.6 / 9.8, of 192 9.3 / 9.4; fp32 12.4 / 11.8 and 15.2 / 11.4).
+// Keys up to which a tile of 16 rows is not cut, on pages in 4 bits and on bf16 ones with first keys: a workgroup takes 0.6 us for 128 of them in
+// 4 bits, merging takes three.  us uncut / in runs of 64: one token over 256 keys in 4 bits 6.1 / 8.8, 512 7.3 / 8.8, 16 of them over 512 7.8 / 11.0;
+// bf16, a window of 64 with four first keys 8.6 / 9.8, of 192 9.3 / 9.4; fp32 12.4 / 11.8 and 15.2 / 11.4.  bf16 without first keys is cut from 64
+// keys on, as it was before there was this rule; it would gain as much by it (one token over 100 keys 5.7 / 8.4, 200 7.0 / 8.4, 256 6.6 / 8.2).
 constexpr int UNCUT_FP4 = 512, UNCUT_BF16 = 256;
 constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);   // partial results
 
@@ -261,13 +262,17 @@ struct PagedLaunch {
     bool mixed;
     int64_t pieces;   // workgroups per KV head: at least as many as the division makes pieces
 };
-// Everything of `a` that the division reads but the window.
+// Everything of `a` that the division reads.  In: a.window and a.sinks as the call has them (0 or more).  No sequence is longer than 2^30 keys: a
+// window that with the first keys reaches as far hides nothing and is none, and without a window there are no first keys.
 inline PagedLaunch paged_launch(AttnArgs &a, const lvr_paged_batch &b, int n_q, int n_kv, bool bf16, bool fp4 = false) {
     a.n_kv = n_kv;
     a.G = n_q / n_kv;
     a.g_shift = 28;
     while (1 << (a.g_shift - 28) < a.G) ++a.g_shift;
     a.g_mul = (uint32_t)((((uint64_t)1 << a.g_shift) + a.G - 1) / a.G);
+    if ((int64_t)a.window + a.sinks >= 1 << 30) a.window = 0;
+    if (!a.window) a.sinks = 0;
+    a.uncut = fp4 ? UNCUT_FP4 : (bf16 && a.sinks ? UNCUT_BF16 : 0);
     const int64_t rows = (int64_t)b.n_tokens * a.G;
     a.narrow = bf16 && !(fp4 && rows <= NARROW_FP4_ALONE) ? NARROW_BF16 : NARROW_F32;
     if (b.n_tokens <= b.n_seqs || rows <= a.narrow) {
