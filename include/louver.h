@@ -407,10 +407,12 @@ int lvr_length(const lvr_index *ix, int64_t *n_host, int64_t *n_indexed_host);
  * kv_dtype LVR_FP4: the pages hold 4 bits a coordinate; new K, V and q, outputs and gathered rows are bf16.  A row is four blocks of
  * 32 coordinates, each with a scale 2^e: e is the least whole number with A <= 7 * 2^e, A the block's largest magnitude, held to
  * -120 .. 125, and a coordinate becomes the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e with its sign (between two the one
- * whose code is even): off by at most 2^e (2^e / 2 below 4 * 2^e, 2^e / 4 below 2 * 2^e).  The codes are those of the exact value: a
- * row of K is normed and rotated in 64 bits before it is rounded, once.  A block with an infinity or a NaN reads as NaN.  A page is
- *   codes   n_kv_heads * page_size rows of 64 bytes, [head][token] or [token][head]: coordinate 2 i of a row in the low half of its byte i, 2 i + 1 in
- *           the high half; a code is the place in the list above, plus 8 for a sign
+ * whose code is even): off by at most 2^e (2^e / 2 below 4 * 2^e, 2^e / 4 below 2 * 2^e).  Magnitudes beyond 7 * 2^125 become
+ * 6 * 2^125, however far that is.  A row of K is normed and rotated in 64 bits and rounded once from there, the angle good to
+ * |position| * 2^-64 of a turn: its codes are the exact value's but where that lies as near as this to the border of two.
+ * A block with an infinity or a NaN reads as NaN.  A page is
+ *   codes   n_kv_heads * page_size rows of 64 bytes, [head][token] or [token][head]: coordinate 2 i of a row in the low half
+ *           of its byte i, 2 i + 1 in the high half; a code is the place in the list above, plus 8 for a sign
  *   scales  behind them, in the same order, 4 bytes a row: the byte of a block is e + 127, 255 for no number
  * page_strides are bytes then: {page, at least n_kv_heads * page_size * 68; head, token of the codes: 64 * page_size and 64, or 64 and
  * 64 * n_kv_heads (LVR_E_UNSUPPORTED otherwise)}. */
@@ -471,9 +473,10 @@ int lvr_paged_norm_append(lvr_paged *pc, void *k_pages_dev, void *v_pages_dev, c
  * negative: LVR_E_INVALID).  Softmax over those keys of sigma <q, k>; a token with no key to attend gives
  * zeros, and so does one whose every score is minus infinity (in fp32).  K and V of keys that no token sees may hold anything, infinities and NaN included; a value that is
  * infinite or NaN reaches the tokens that see it and no others.
- *   q_dev    [n_tokens][n_q_heads][head_dim] of kv_dtype, q_token_stride elements between tokens
- *   out_dev  [n_tokens][n_q_heads][head_dim] of kv_dtype, contiguous, apart from q
- * Sums, maxima and the output are held in fp32; bf16 caches round the probabilities to bf16 before they meet V.
+ *   q_dev    [n_tokens][n_q_heads][head_dim] of kv_dtype (LVR_FP4: bf16), q_token_stride elements between tokens
+ *   out_dev  [n_tokens][n_q_heads][head_dim] of the same type, contiguous, apart from q
+ * Sums, maxima and the output are held in fp32; on bf16 and LVR_FP4 pages the probabilities are rounded to bf16 before they
+ * meet V, which leaves outputs off by 1.9e-3 to 2.4e-3 of their root mean square where their own rounding to bf16 alone is 1.6e-3.
  * Launches kernels only (no allocation, no host synchronisation, no memset): the call may be recorded under HIP graph
  * capture.  Calls on one lvr_paged share its work space and must be ordered by the caller, those of replayed graphs
  * among them. */

@@ -236,9 +236,11 @@ __device__ __forceinline__ u32x4 weights_at(const char *w, int at) {
     return w ? load_piece(w + at * ELT) : u32x4{one, one, one, one};
 }
 
-// Pages in 4 bits.  The least e with A <= 7 * 2^e, A the largest magnitude of 32 values: 7 rounds to 6, the largest code, and 6.99 is no further from it
-// than 5 from 4, so that no value is off by more than 2^e, half of the widest gap.  As a scale byte e + 127, held between 7 and 252: all products of a code and a scale
-// are normal bf16 values then, and so is what lies between two of them.  Bits of A in, as the order of fp32 has them; 255 for infinities and NaN.
+// Pages in 4 bits.  The least e with A <= 7 * 2^e, A the largest magnitude of 32 values: 7 rounds to 6, the largest code, and 6.99 is no further
+// from it than 5 from 4, so that no value is off by more than 2^e, half of the widest gap.  As a scale byte e + 127, held between 7 and 252: all
+// products of a code and a scale are normal bf16 values then, and so is what lies between two of them.  (bf16 goes up to 7.97 * 2^125: from 7 * 2^125
+// on values become 6 * 2^125, off by up to twice as much, and keys that a norm's weight or a rotation takes further by more.)  Bits of A in, as the
+// order of fp32 has them; 255 for infinities and NaN.
 __device__ __forceinline__ uint32_t fp4_scale_byte(uint32_t bits) {
     if (bits >= 0x7f800000u) return 255;
     const int s = (int)((bits + 0x1fffffu) >> 23) - 2;   // 7 = 1.75 * 4: past a mantissa of 1.75 the next power of two
@@ -264,8 +266,9 @@ __device__ __forceinline__ float sticky(double v, uint32_t &most) {
     return __uint_as_float((hi & 0x80000000u) | (uint32_t)m << 3 | (lo < 1 ? lo : 1));
 }
 
-// Eight K rows and eight V rows of one token into pages in 4 bits, by one wave; lanes hold pieces as in paged_append_kernel.  A code is that of the exact value: K is
-// normed and rotated in 64 bits, which fp32 would leave beside a border between two codes on either side of it.
+// Eight K rows and eight V rows of one token into pages in 4 bits, by one wave; lanes hold pieces as in paged_append_kernel.  K is normed and rotated in
+// 64 bits: values beside a border between two codes, which fp32 would leave on either side of it, go to the exact value's but within 2^-49 of the border,
+// relative to a pair's size, and the angle's |position| * 2^-64 of a turn.
 template <bool NEIGHBOURS, bool NORM>
 __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_batch &b, int t, int row, Turns<double> &turns) {
     constexpr int E = 8, LANES = 8;
