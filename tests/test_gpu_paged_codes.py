@@ -1,5 +1,5 @@
 """How far values of a page in 4 bits may be from what was stored, on the GPU: by the bounds that the header states, at the ends of the range and at far
-positions."""
+positions; and rows past the caches against the definition."""
 import math
 from fractions import Fraction
 
@@ -85,3 +85,31 @@ def test_codes_of_keys_at_far_positions(pairs):
             return levels[torch.searchsorted(middle, t.clamp(-6, 6).contiguous())]
         assert (got / step >= nearest((x - off) / step)).all() and (got / step <= nearest((x + off) / step)).all()
         assert (off / step).max() < 1e-7
+
+
+def test_rows_past_the_caches_are_the_codes_values():
+    """Past 192 MiB of rows the gather stores around the caches: every row against the definition, page by page."""
+    n, heads, page, pages = 100003, 8, 64, 1563
+    g = torch.Generator(device="cuda").manual_seed(182)
+    h = L.lvr_paged_create(L.make_paged_config(n_q_heads=heads, n_kv_heads=heads, kv_dtype=L.LVR_FP4, page_size=page, n_pages=pages, layout="token"))
+    try:
+        assert n * heads * 256 >= 192 << 20
+        kp, vp = (torch.randint(0, 256, (pages, heads * page * 68), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2))
+        for p in (kp, vp):
+            p[:, heads * page * 64:].clamp_(7, 252)
+        table = torch.randperm(pages, generator=g, device="cuda").to(torch.int32)[None].contiguous()
+        K, V = (torch.full((1, heads, n, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        L.lvr_paged_gather(h, kp, vp, torch.tensor([n], dtype=torch.int32, device="cuda"), table, K, V)
+        levels = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device="cuda")
+        levels = torch.cat([levels, -levels])
+        for pool, rows in ((kp, K), (vp, V)):
+            for p0 in range(0, pages, 100):
+                ids = table[0, p0:p0 + 100].long()
+                b = pool[ids, :heads * page * 64].view(-1, page, heads, 64).int()
+                s = pool[ids, heads * page * 64:].view(-1, page, heads, 4).long() - 127
+                s = (s + 1023 << 52).view(torch.float64)      # 2^s, exactly (pow on the GPU is off by a unit of the last place for some whole numbers)
+                x = levels[torch.stack([b & 15, b >> 4], dim=-1).flatten(-2)].unflatten(-1, (4, 32)) * s[..., None]
+                x = x.flatten(-2).flatten(0, 1).transpose(0, 1)[:, :n - p0 * page]      # [head][position][128]
+                assert torch.equal(rows[0, :, p0 * page:p0 * page + x.shape[1]].double(), x)
+    finally:
+        L.lvr_paged_destroy(h)
