@@ -25,3 +25,10 @@ def test_stores_of_fp32_rows_do_not_wait_for_each_other(listing, pairs):
     stores = [i for i, x in enumerate(code) if x.startswith("global_store")]
     assert len(stores) == 12
     assert not [x for x in code[stores[0]:] if x.startswith("s_waitcnt") and "vmcnt" in x]
+
+
+@pytest.mark.parametrize("kernel, n", [("paged_gather_kernelI", 4), ("paged_gather_fp4_kernelI", 2)])
+def test_gathers_read_two_lines_of_arguments(listing, kernel, n):
+    """Nothing of what the runtime puts behind a kernel's own arguments, which are two lines of 64 bytes."""
+    sizes = re.findall(r"\.amdhsa_kernel \S*" + kernel + r".*?\.amdhsa_kernarg_size (\d+)", listing, re.S)
+    assert [int(x) for x in sizes] == [128] * n
