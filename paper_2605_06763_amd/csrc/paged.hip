@@ -420,8 +420,9 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
         }
     }
     // The rows were asked for before the token's place and are there by now.  Told so, the compiler waits for nothing between the stores; else each pair
-    // of them for the one before (fp32, 8192 tokens 73.2 us without this and 69.9 with it, unrotated 73.0 and 69.6; bf16 gains nothing).
-    if (ELT == 4) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    // of them for the one before (fp32, 8192 tokens 73.2 us without this and 69.9 with it, unrotated 73.0 and 69.6; 2000 tokens of 32 rows 11.2 and
+    // 12.0).  bf16 gains nothing, norms lose where the last group of rows is a small one (8192 tokens of 10 rows 15.4 and 16.2).
+    if (ELT == 4 && !NORM) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
 #pragma unroll
     for (int c = 0; c < PER; ++c) {
         const int row = row0 + c * ROWS;

@@ -867,7 +867,8 @@ struct Rows128Lds {
 //   two rounds, more of them: four prompts of 1024             66 / 68     397 / 415      66 / 69
 //               16 ragged ones of up to 500 new of 3000        62 / 67     305 / 331      61 / 64
 //               four of 1024 new of 4096, a window of 1000     98 / 104    550 / 554      93 / 98
-// (A prompt of 3000, a round and a half, loses by it: 94 / 98, 627 / 628, 93 / 98.)
+// Batches of one round and a half go either way: a prompt of 3000 loses by it (94 / 98, 627 / 628, 93 / 98), three prompts of 1000 would gain (53 / 53, 290 /
+// 287, 56 / 55), the 16 ragged ones are such a batch too.
 // In three rounds workgroups are out of step by themselves (prompt of 16384 nothing, of 8192 with a window of 2048 288 / 297).
 template <typename KT, bool SINKS>
 __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, bool urgent, Rows128Lds<KT> &lds) {
