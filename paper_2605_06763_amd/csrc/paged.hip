@@ -199,8 +199,8 @@ __device__ __forceinline__ double norm_of(double squares, float eps) {
     if (x == __builtin_inf()) return 0.;
     return r * __builtin_fma(-0.5 * x * r, r, 1.5);   // the instruction's 2^-26 or so become 2^-50
 }
-// The sum of squares of what a lane has of a row.  bf16: two products a step, exact in fp32, and sums of 16 values in it; where they leave its range, as
-// for all else, in 64 bits.
+// The sum of squares of what a lane has of a row.  bf16: two products a step, exact in fp32, and sums of 16 values in it; where they leave its range,
+// as for all else, in 64 bits.
 template <int ELT>
 __device__ __forceinline__ double squares_of(u32x4 r0, u32x4 r1) {
     if constexpr (ELT == 2) {
@@ -254,9 +254,9 @@ __device__ __forceinline__ uint32_t fp4_codes(const float (&x)[8], float scale) 
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
-// A value in 64 bits as an fp32 value that rounds to the same code and scale: cut to 21 bits, the last of which says whether anything was cut.  Beyond the range of
-// fp32 its largest number, which has the largest scale and code; below 2^-126, far under the least code, something that small.  `most` keeps the
-// largest upper half seen: infinities and NaN are told by it.
+// A value in 64 bits as an fp32 value that rounds to the same code and scale: cut to 21 bits, the last of which says whether anything was cut.  Beyond
+// the range of fp32 its largest number, which has the largest scale and code; below 2^-126, far under the least code, something that small.  `most`
+// keeps the largest upper half seen: infinities and NaN are told by it.
 __device__ __forceinline__ float sticky(double v, uint32_t &most) {
     const uint64_t u = __builtin_bit_cast(uint64_t, v);
     const uint32_t lo = (uint32_t)u, hi = (uint32_t)(u >> 32), mag = hi & 0x7fffffffu;
@@ -266,9 +266,9 @@ __device__ __forceinline__ float sticky(double v, uint32_t &most) {
     return __uint_as_float((hi & 0x80000000u) | (uint32_t)m << 3 | (lo < 1 ? lo : 1));
 }
 
-// Eight K rows and eight V rows of one token into pages in 4 bits, by one wave; lanes hold pieces as in paged_append_kernel.  K is normed and rotated in
-// 64 bits: values beside a border between two codes, which fp32 would leave on either side of it, go to the exact value's but within 2^-49 of the border,
-// relative to a pair's size, and the angle's |position| * 2^-64 of a turn.
+// Eight K rows and eight V rows of one token into pages in 4 bits, by one wave; lanes hold pieces as in paged_append_kernel.  K is normed and rotated
+// in 64 bits: values beside a border between two codes, which fp32 would leave on either side of it, go to the exact value's but within 2^-49 of the
+// border, relative to a pair's size, and the angle's |position| * 2^-64 of a turn.
 template <bool NEIGHBOURS, bool NORM>
 __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_batch &b, int t, int row, Turns<double> &turns) {
     constexpr int E = 8, LANES = 8;
@@ -360,12 +360,13 @@ __device__ __forceinline__ void append_fp4(const AppendArgs &a, const lvr_paged_
 // overflow dropped: no far position loses anything.
 //
 // Bound by HBM where there are tokens enough: 8192 tokens (48 rows each, bf16) 36 us on one axis and 34 on three, 5.6 and 6.0 TB/s read and written;
-// 1885 fp32 tokens of 80 rows 24 us, 6.4 TB/s.  One token: 4.3 to 4.9 us a call, which the host takes 4.0 us to make; the kernel 2.7, the launch and three
-// dependent trips (rows and lengths, table, store).
+// 1885 fp32 tokens of 80 rows 24.5 us, 6.3 TB/s.  One token: 4.3 to 4.9 us a call, which the host takes 4.0 us to make; the kernel 2.7, the launch and
+// three dependent trips (rows and lengths, table, store).
 //
-// NORM: rows of K and q are normed first, the squares summed over the row's lanes while the sines are made (8192 such tokens on three axes 38 us, one token
-// as without).  FP4 (KT is the type of new rows then): the first waves of a token take K and V, eight heads each, the others q.  Those need the largest
-// magnitude of every block after the norm and the rotation, in 64 bits: 8192 tokens of the same heads on one axis 35 us, 101 MB read and 76 written, 5.0 TB/s.
+// NORM: rows of K and q are normed first, the squares summed over the row's lanes while the sines are made (8192 such tokens on three axes 38 us, one
+// token as without).  FP4 (KT is the type of new rows then): the first waves of a token take K and V, eight heads each, the others q.  Those need the
+// largest magnitude of every block after the norm and the rotation, in 64 bits: 8192 tokens of the same heads on one axis 35 us, 101 MB read and 76
+// written, 5.0 TB/s.
 template <typename KT, bool NEIGHBOURS, int PER, bool STREAM, bool NORM, bool FP4>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_paged_batch b) {
     constexpr int ELT = sizeof(KT) == 4 ? 4 : 2, E = 16 / ELT, LANES = PAIRS / E, ROWS = 64 / LANES;
@@ -419,9 +420,9 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
             cs[e] = turn.cs;
         }
     }
-    // The rows were asked for before the token's place and are there by now.  Told so, the compiler waits for nothing between the stores; else each pair
-    // of them for the one before (fp32, 8192 tokens 73.2 us without this and 69.9 with it, unrotated 73.0 and 69.6; 2000 tokens of 32 rows 11.2 and
-    // 12.0).  bf16 gains nothing, norms lose where the last group of rows is a small one (8192 tokens of 10 rows 15.4 and 16.2).
+    // The rows were asked for before the token's place and are there by now.  Told so, the compiler waits for nothing between the stores; else each
+    // pair of them for the one before (fp32, 8192 tokens 73.2 us without this and 69.9 with it, unrotated 73.0 and 69.6; 2000 tokens of 32 rows 11.2
+    // and 12.0).  bf16 gains nothing, norms lose where the last group of rows is a small one (8192 tokens of 10 rows 15.4 and 16.2).
     if (ELT == 4 && !NORM) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
 #pragma unroll
     for (int c = 0; c < PER; ++c) {
@@ -479,7 +480,8 @@ __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a, lvr_pag
 
 // A wave takes 16 rows of one head, which lie in one page: one table entry, then 64 pieces of 16 bytes to an access, one behind the other
 // where the rows are.  131072 keys of 8 heads 191 us, 5.6 TB/s read and written.
-// wgs: the workgroups of the launch, which lie behind the arguments otherwise, in a line of memory more (2000 keys of 8 heads 4.94 us so, 4.81 as it is).
+// wgs: the workgroups of the launch, which lie behind the arguments otherwise, in a line of memory more (2000 keys of 8 heads 4.94 us so, 4.81 as
+// it is).
 template <typename KT, bool STREAM>
 __global__ void __launch_bounds__(256) paged_gather_kernel(const char *k_pages, const char *v_pages, char *K, char *V, int64_t n,
                                                            int32_t n_kv, int32_t wgs, lvr_paged_batch b) {
@@ -515,8 +517,8 @@ __global__ void __launch_bounds__(256) paged_gather_kernel(const char *k_pages, 
     }
 }
 
-// Pages in 4 bits, as rows of bf16.  Four lanes' worth of codes are one block: a lane takes eight of them to 16 bytes.  Bound by the store of rows that are
-// 3.8 times as long as what is read: 32768 keys of 8 heads 30 us (134 MB written, 36 read), 5.7 TB/s.
+// Pages in 4 bits, as rows of bf16.  Four lanes' worth of codes are one block: a lane takes eight of them to 16 bytes.  Bound by the store of rows
+// that are 3.8 times as long as what is read: 32768 keys of 8 heads 30 us (134 MB written, 36 read), 5.7 TB/s.
 template <bool STREAM>
 __global__ void __launch_bounds__(256) paged_gather_fp4_kernel(const char *k_pages, const char *v_pages, char *K, char *V, int64_t n,
                                                                int32_t n_kv, int32_t wgs, lvr_paged_batch b) {

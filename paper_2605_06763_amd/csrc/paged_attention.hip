@@ -173,10 +173,11 @@ __device__ __noinline__ RowSum one_row(AttnArgs a, lvr_paged_batch bt, Tile t, i
 // coordinates each, and which coordinates share a result tile is free as well (tile u: coordinates 8 i + u).
 // bf16: two score tiles make one operand of 32 keys; a pair of V rows is woven into it by byte permutes.
 //
-// Bound by the read of K and V: 131072 keys of one sequence 98 us, 48 ragged sequences of up to 32768 keys 359 us (1.97 GB), both 5.5 TB/s.
-// Short contexts are bound by dependent trips (lengths, table, rows, products, partial results): 2048 keys 8.5 us, in runs of 64 keys, for which two of the
-// four waves have none.  Rows asked for a turn ahead: no gain, and fp32 spills; eight waves to a workgroup: 12.1 us at 2048 keys where four took 11.3.
-// First keys: 24 long sequences with a window of 4096 and four of them 89 us (403 MB, 4.5 TB/s), bound by the last pieces' end: 576 of one length on 256 compute units.
+// Bound by the read of K and V: 131072 keys of one sequence 98 us, 48 ragged sequences of up to 32768 keys 361 us (1.97 GB), both 5.5 TB/s.
+// Short contexts are bound by dependent trips (lengths, table, rows, products, partial results): 2048 keys 8.5 us, in runs of 64 keys, for which two
+// of the four waves have none.  Rows asked for a turn ahead: no gain, and fp32 spills; eight waves to a workgroup: 12.1 us at 2048 keys where four
+// took 11.3.  First keys: 24 sequences, 21 of them longer than a window of 4096 and four first keys, 89 us (387 MB, 4.3 TB/s): 560 pieces of 1018 to
+// 1472 keys on 256 compute units, bound by the end of the last.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <typename KT>
 struct Rows16;
@@ -290,12 +291,12 @@ struct Rows16<lvr_f32_t> {
     static __device__ __forceinline__ int coordinate(int r, int u) { return u < 4 ? 4 * r + u : 64 + 4 * r + u - 4; }
 };
 
-// Pages in 4 bits.  Lanes (i, b) hold block b of a key's row, 32 coordinates with one scale, and of V the eight coordinates that they hold in bf16; both
-// become bf16 in registers, exactly.
+// Pages in 4 bits.  Lanes (i, b) hold block b of a key's row, 32 coordinates with one scale, and of V the eight coordinates that they hold in bf16;
+// both become bf16 in registers, exactly.
 //
-// Bound by the read where a batch is even (5.6 TB/s): 131072 keys of one sequence 33 us (143 MB; the launch, the division and two merges take 8 of them), 48
-// ragged sequences of up to 32768 keys 109 us (525 MB, 4.8 TB/s: the pieces' starts and ends weigh four times as much as beside bf16 rows).  2048 keys 8.5 us as in
-// bf16, by the same dependent trips.
+// Bound by the read where a batch is even (5.6 TB/s): 131072 keys of one sequence 33 us (143 MB; the launch, the division and two merges take 8 of
+// them), 48 ragged sequences of up to 32768 keys 111 us (522 MB, 4.7 TB/s: the pieces' starts and ends weigh four times as much as beside bf16 rows).
+// 2048 keys 8.5 us as in bf16, by the same dependent trips.  Weights are rounded to bf16 as there: see Rows16<lvr_bf16_t>::add.
 template <>
 struct Rows16<lvr_fp4_t> {
     static constexpr int ELT = 2;
@@ -449,8 +450,8 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
         for (int h = 0; h < 2; ++h) {
             const int who = 2 * (turn & 31) + h;
             if constexpr (FP4) {
-                // One address for the wave and a lane's 32-bit place behind it, in the load itself (the places are made opaque here, or they are widened
-                // before the loop and added up in registers that loads are on their way to).
+                // One address for the wave and a lane's 32-bit place behind it, in the load itself (the places are made opaque here, or they
+                // are widened before the loop and added up in registers that loads are on their way to).
                 x.none[h] = without >> who & 1;
                 const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(place_of.high, who) << 32 | (uint32_t)__builtin_amdgcn_readlane(place_of.low, who);
                 const int32_t scales = __builtin_amdgcn_readlane(place_of.scales, who);
@@ -474,9 +475,9 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
     // 16 keys from `key0` on, not all of which every row of the tile sees; whether V has a value that some rows must not meet.
     auto hide = [&](int key0, bool none, float (&p)[4], auto &v) {
         bool poison = false;
-        // Without a page nothing is seen.  A bound that says so saves a branch for each of the four where this is most of the work: us with the bound / with
-        // branches, one token, bf16 and a window of 64 8.6 / 8.9, 250 keys 8.7 / 9.0, fp32 10.4 / 10.7 and 10.5 / 10.7.  Beside tiles of 128 rows
-        // fp32 loses by it (30 x 16 tokens over 3000 keys 298 / 287), and 4 bits have no registers for it.
+        // Without a page nothing is seen.  A bound that says so saves a branch for each of the four where this is most of the work: us with the
+        // bound / with branches, one token, bf16 and a window of 64 8.6 / 8.9, 250 keys 8.7 / 9.0, fp32 10.4 / 10.7 and 10.5 / 10.7.  Beside tiles
+        // of 128 rows fp32 loses by it (30 x 16 tokens over 3000 keys 298 / 287), and 4 bits have no registers for it.
         constexpr bool BY_BOUND = ALONE && !FP4;
         const int row_last = BY_BOUND && none ? -1 : last;
 #pragma unroll
@@ -712,12 +713,16 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 // conflicts counted; fp32, whose V rows lie as they are: conflicts in 13 % of the clocks that LDS works).
 //
 // 32 rows to a wave and two workgroups to a compute unit: 128 KiB of LDS and up to 256 registers a lane, so that one workgroup's matrix
-// instructions meet the other's exponentials.  A prompt of 16384 tokens (32 heads on 8, 2.2 TFLOP): 2.1 to 2.25 ms on different cards, 980 to
-// 1050 TFLOP/s; matrix units busy 46 % and vector units 42 % of the clocks, where the library's product of 8192 x 8192 matrices reaches
-// 1148 to 1409 TFLOP/s.  fp32, 8192 tokens: 135 TFLOP/s of the 154 the library reaches.  One workgroup to a compute unit takes 1.43 times as long as two,
-// whose instructions meet for the most part.  Tried without gain: the scores of the next tile made
-// between the exponentials of this one (-2 %), V's operands read a step ahead (bf16 0 to 1 %, 4 bits -1 %), priority for exponentials (-2 to -6 %), tiles through registers (653
-// TFLOP/s: the loads were waited for at once).
+// instructions meet the other's exponentials.  A prompt of 16384 tokens (32 heads on 8, 2.2 TFLOP): 2.08 to 2.15 ms on different cards, 1020 to
+// 1060 TFLOP/s; matrix units busy 49 % and vector units 43 % of the clocks, where the library's product of 8192 x 8192 matrices reaches
+// 1148 to 1409 TFLOP/s.  fp32, 8192 tokens: 135 TFLOP/s of the 154 the library reaches.  One workgroup to a compute unit takes 1.43 times as long as
+// two, whose instructions meet for the most part.  Tried without gain: the scores of the next tile made between the exponentials of this one (-2 %),
+// V's operands read a step ahead (bf16 0 to 1 %, 4 bits -1 %), priority for exponentials (-2 to -6 %), tiles through registers (653 TFLOP/s: the
+// loads were waited for at once).
+//
+// A tile's loads are not waited for before its products, which overlaps them where few workgroups are left: 40 ragged sequences of up to 20 new tokens
+// of 20000 378 us with such a wait and 285 without.  Even batches of few rows over long runs, bound by the read, lose a little by it: 8 x 16 tokens
+// over 32768 keys 194 and 199.
 // ---------------------------------------------------------------------------------------------------------------------------
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -839,9 +844,9 @@ struct Rows128<lvr_f32_t> {
     }
 };
 
-// Pages in 4 bits: a tile becomes bf16 on its way into LDS and is worked on as such.  Codes pass through registers, a block and its scale a lane; they are asked
-// for a tile ahead and widened while this one's products run.  Bound as in bf16: the prompt of 16384 tokens 2.09 to 2.14 ms, widening hides behind the read that it saves
-// (matrix units busy 42 % and vector units 45 % of the clocks).
+// Pages in 4 bits: a tile becomes bf16 on its way into LDS and is worked on as such.  Codes pass through registers, a block and its scale a lane; they
+// are asked for a tile ahead and widened while this one's products run.  Bound as in bf16: the prompt of 16384 tokens 2.06 to 2.14 ms, widening hides
+// behind the read that it saves (matrix units busy 44 % and vector units 46 % of the clocks).
 template <>
 struct Rows128<lvr_fp4_t> : Rows128<lvr_bf16_t> {};
 
@@ -867,8 +872,8 @@ struct Rows128Lds {
 //   two rounds, more of them: four prompts of 1024             66 / 68     397 / 415      66 / 69
 //               16 ragged ones of up to 500 new of 3000        62 / 67     305 / 331      61 / 64
 //               four of 1024 new of 4096, a window of 1000     98 / 104    550 / 554      93 / 98
-// Batches of one round and a half go either way: a prompt of 3000 loses by it (94 / 98, 627 / 628, 93 / 98), three prompts of 1000 would gain (53 / 53, 290 /
-// 287, 56 / 55), the 16 ragged ones are such a batch too.
+// Batches of one round and a half go either way: a prompt of 3000 loses by it (94 / 98, 627 / 628, 93 / 98), three prompts of 1000 would gain
+// (53 / 53, 290 / 287, 56 / 55), the 16 ragged ones are such a batch too.
 // In three rounds workgroups are out of step by themselves (prompt of 16384 nothing, of 8192 with a window of 2048 288 / 297).
 template <typename KT, bool SINKS>
 __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged_batch &bt, const Tile &t, int kvh, bool urgent, Rows128Lds<KT> &lds) {
@@ -971,8 +976,8 @@ __device__ __forceinline__ void rows128_piece(const AttnArgs &a, const lvr_paged
     int pages = pages_of(t.begin + TK);
     if constexpr (FP4)
         if (t.begin < t.end) unfold(t.begin, none, lds.k[0], lds.v[0], lds.odd[0]);
-    // A tile is worked on while the next one is on its way.  The buffers are told apart for the compiler, which else waits for what comes into one before it
-    // reads the other.
+    // A tile is worked on while the next one is on its way.  The buffers are told apart for the compiler, which else waits for what comes into one
+    // before it reads the other.
     auto step = [&](int place, int buf, const char *__restrict k, char *__restrict v, char *__restrict next_k, char *__restrict next_v) __attribute__((always_inline)) {
         const int k0 = key_at<SINKS>(t, place);
         uint32_t next_none = 0;

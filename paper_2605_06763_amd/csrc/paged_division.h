@@ -7,23 +7,28 @@ namespace {
 
 // Pieces of work a launch aims at, over all KV heads: of tiles of 16 rows alone, and where there are tiles of 128 rows.  A piece costs a
 // workgroup's start and, where its tile is cut, a partial result to be written and read; too few leave compute units idle at the end.
-// us with 256 / 512 / 1024 pieces (8 KV heads) tiles of 16 rows: one sequence of 32768 keys 28 / 32 / 34, four ragged ones (32 tiles)
-// 32 / 35 / 38, eight 44 / 43 / 42, 48 of them 314 / 296 / 295; tiles of 128: 32 tokens over 131072 keys 165 / 137 / 179, 512 of 8192
-// 120 / 86 / 100, 1000 of 12000 327 / 218 / 225, 1000 of 12000 beside 31 single tokens 419 / 291 / 310, fp32 prompt of 2048 399 / 356 / 341.
+// us with 256 / 512 / 1024 pieces (8 KV heads), tiles of 16 rows: one sequence of 32768 keys 30 / 34 / 38, four ragged ones (32 tiles)
+// 37 / 34 / 32, eight 76 / 63 / 62, 48 of them 428 / 375 / 381, in 4 bits 132 / 115 / 116; tiles of 128: 32 tokens over 131072 keys
+// 126 / 139 / 176, 512 of 8192 99 / 85 / 98, 1000 of 12000 250 / 202 / 215, 1000 of 12000 beside 31 single tokens 290 / 286 / 274, fp32 prompt
+// of 2048 394 / 317 / 344.
 constexpr int ROWS16_PIECES = 512, ROWS16_PIECES_FEW = 256, MIXED_PIECES = 512;
 constexpr int FEW_TILES = 32;   // sequences times KV heads up to which a batch of single tokens makes few pieces
-// Keys of the shortest run.  us with 64 / 128 / 256 / 512: one token over 1024 keys 9.3 / 9.9 / 10.9 / 12.2, over 2048 10.0 / 10.3 / 11.3 /
-// 13.3, over 8192 13.2 / 13.2 / 13.2 / 15.0; four prompts of 1024 73.3 / 73.5 / 72.2.
+// Keys of the shortest run.  us with 64 / 128 / 256 / 512: one token over 1024 keys 8.5 / 9.2 / 10.2 / 12.1, over 2048 8.7 / 9.4 / 10.3 / 12.3,
+// in 4 bits 8.7 / 8.6 / 9.1 / 10.3, over 8192 13.0 / 13.1 / 13.0 / 14.0; four prompts of 1024 64.5 / 65.6 / 65.7 / 64.3.
 constexpr int MIN_RUN = 64;
 // Rows of a sequence up to which it is taken in tiles of 16.  A wave of a 128-row tile works on 32 of them however many there are, and on
-// fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 57 in a tile of 128 / 46 in four of 16,
-// eight such sequences of 4096 keys 41 / 58; fp32 171 / 98).  The rule goes by the rows alone, and for bf16 takes the side on which many sequences gain.
+// fp32 takes so long that reading the keys again costs less (us, 64 rows over 32768 keys: bf16 55 in a tile of 128 / 51 in four of 16,
+// eight such sequences 200 / 341 and of 4096 keys 42 / 57; fp32 174 / 107, 1025 / 771 and 160 / 117).  The rule goes by the rows alone, and for
+// bf16 takes the side on which many sequences gain.
 constexpr int NARROW_BF16 = 32, NARROW_F32 = 64;
-constexpr int NARROW_FP4_ALONE = 64;   // of all sequences together, on pages in 4 bits (16 tokens, 32 heads on 8, over 32768 keys: 49 us in a tile of 128, 28 in four of 16)
+// Of all sequences together, on pages in 4 bits (16 tokens, 32 heads on 8, over 32768 keys: 49 us in a tile of 128, 28 in four of 16; 9 tokens over
+// 3000 21 and 12).
+constexpr int NARROW_FP4_ALONE = 64;
 // Keys up to which a tile of 16 rows is not cut, on pages in 4 bits and on bf16 ones with first keys: a workgroup takes 0.6 us for 128 of them in
-// 4 bits, merging takes three.  us uncut / in runs of 64: one token over 256 keys in 4 bits 6.1 / 8.8, 512 7.3 / 8.8, 16 of them over 512 7.8 / 11.0;
-// bf16, a window of 64 with four first keys 8.6 / 9.8, of 192 9.3 / 9.4; fp32 12.4 / 11.8 and 15.2 / 11.4.  bf16 without first keys is cut from 64
-// keys on, as it was before there was this rule; it would gain as much by it (one token over 100 keys 5.7 / 8.4, 200 7.0 / 8.4, 256 6.6 / 8.2).
+// 4 bits, merging takes three.  us uncut / in runs of 64: one token over 256 keys in 4 bits 5.7 / 8.2, 512 6.9 / 8.3, 16 of them over 512 7.4 / 10.4;
+// bf16, a window of 64 with four first keys 7.5 / 9.2.  fp32 goes either way (11.4 / 11.5, over 200 keys 11.5 / 10.8, 16 sequences 12.8 / 16.5) and is
+// cut.  So is bf16 without first keys beyond 64 keys, as it was before there was this rule; it would gain as much by it (one token over 100 keys
+// 5.7 / 8.4, 200 7.0 / 8.4, 256 6.6 / 8.2).
 constexpr int UNCUT_FP4 = 512, UNCUT_BF16 = 256;
 constexpr int WIDE_ROOM = 2 * MIXED_PIECES, NARROW_ROOM = 3 * (ROWS16_PIECES > MIXED_PIECES ? ROWS16_PIECES : MIXED_PIECES);   // partial results
 
@@ -84,9 +89,9 @@ __host__ __device__ __forceinline__ int token_of(const AttnArgs &a, int row) { r
 // launch has as many workgroups beside one for each tile: should there be more, L grows until there are not (prompts of a few hundred tokens
 // get there with the shortest runs).
 //
-// A batch of up to 64 sequences stays in registers.  Of a larger one every wave reads the lengths anew, to divide it and to find its piece: single tokens over
-// 64 keys, 8 KV heads: 64 sequences 7.1 us, 256 25, 1024 180, 4096 1848 (the read of their keys: 2.8, 11, 45, 180); over 2048 keys 256 sequences 359 us and
-// 1024 1445, the read's rate.
+// A batch of up to 64 sequences stays in registers.  Of a larger one every wave reads the lengths anew, to divide it and to find its piece: single
+// tokens over 64 keys, 8 KV heads: 64 sequences 7.3 us, 256 25, 1024 173, 4096 1806 (the read of their keys: 2.8, 11, 45, 180); over 2048 keys 256
+// sequences 360 us and 1024 1441, the read's rate.
 //
 // SINKS: a.sinks may be more than 0; UNCUT: a.uncut may be (without them the code has nothing of that).
 template <bool MIXED, typename WAVE, bool SINKS = true, bool UNCUT = true>
@@ -134,9 +139,9 @@ struct Division {
         }
         run = (about<WAVE>(span, runs) + 64) & ~63;   // the last run takes what is left, whatever was rounded
     }
-    // Sequences of one tile each that all go into as many runs: where rounding up made more pieces than wanted, as many as are wanted at most.  Pieces of one
-    // length that pass a whole round by a few end late (us rounded up / so, 8 KV heads: 12 sequences of 8192 keys bf16 88 / 77, 4 bits 32.5 / 27.1, fp32 166 / 145; 20 of
-    // 4096 74 / 66; 5 of 8192 43.5 / 38.3; 3 of them 27.7 / 23.1).
+    // Sequences of one tile each that all go into as many runs: where rounding up made more pieces than wanted, as many as are wanted at most.  Pieces
+    // of one length that pass a whole round by a few end late (us rounded up / so, 8 KV heads: 12 sequences of 8192 keys bf16 88 / 78, 4 bits 31 / 25.5,
+    // fp32 165 / 145; 20 of 4096 73 / 66; 5 of 8192 43 / 37.5; 3 of them 26.8 / 22.3).
     __host__ __device__ __forceinline__ void level(int target) {
         const uint64_t with = WAVE::ballot(tiles == 1);
         if (with == 0) return;
