@@ -714,7 +714,7 @@ __device__ __forceinline__ void rows16_piece(const AttnArgs &a, const lvr_paged_
 //
 // 32 rows to a wave and two workgroups to a compute unit: 128 KiB of LDS and up to 256 registers a lane, so that one workgroup's matrix
 // instructions meet the other's exponentials.  A prompt of 16384 tokens (32 heads on 8, 2.2 TFLOP): 2.08 to 2.15 ms on different cards, 1020 to
-// 1060 TFLOP/s; matrix units busy 49 % and vector units 43 % of the clocks, where the library's product of 8192 x 8192 matrices reaches
+// 1060 TFLOP/s; matrix units busy 48 % and vector units 43 % of the clocks, where the library's product of 8192 x 8192 matrices reaches
 // 1148 to 1409 TFLOP/s.  fp32, 8192 tokens: 135 TFLOP/s of the 154 the library reaches.  One workgroup to a compute unit takes 1.43 times as long as
 // two, whose instructions meet for the most part.  Tried without gain: the scores of the next tile made between the exponentials of this one (-2 %),
 // V's operands read a step ahead (bf16 0 to 1 %, 4 bits -1 %), priority for exponentials (-2 to -6 %), tiles through registers (653 TFLOP/s: the
