@@ -288,7 +288,8 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *k, *v, *q = nullptr, *q_out = nullptr, *pos = nullptr, *qw = nullptr, *kw = nullptr;
     int64_t tokens = -1, strides[3] = {0, 0, 0};
     LVR_PLAIN(
-        LVR_NOT_PLAIN(n == (NORM ? 17 : 14) && (NORM ? lib.paged_norm_append != nullptr : lib.paged_append != nullptr) && p.begin(a[0], a[1], a[2], a[13]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
+        LVR_NOT_PLAIN(n == (NORM ? 17 : 14) && (NORM ? lib.paged_norm_append != nullptr : lib.paged_append != nullptr) &&
+                      p.begin(a[0], a[1], a[2], a[13]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
                       p.tokens(a[5], p.c->n_kv_heads, tokens, k, strides[0]) && p.tokens(a[6], p.c->n_kv_heads, tokens, v, strides[1]) &&
                       p.batch(a[7], a[8], a[9]) && (a[10] == Py_None) == (a[11] == Py_None));
         if (a[10] != Py_None)
@@ -327,9 +328,11 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int64_t tokens = -1, stride;
     int32_t window = 0, sinks = 0;
     LVR_PLAIN(
-        LVR_NOT_PLAIN(n == (SINKS ? 13 : 12) && (SINKS ? lib.paged_sink_attention != nullptr : lib.paged_attention != nullptr) && p.begin(a[0], a[1], a[2], a[11]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
+        LVR_NOT_PLAIN(n == (SINKS ? 13 : 12) && (SINKS ? lib.paged_sink_attention != nullptr : lib.paged_attention != nullptr) &&
+                      p.begin(a[0], a[1], a[2], a[11]) && p.pool(a[3], p.k_pages) && p.pool(a[4], p.v_pages) &&
                       p.tokens(a[5], p.c->n_q_heads, tokens, q, stride) && p.batch(a[6], a[7], a[8]) &&
-                      p.whole(a[9], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, out) && keys(a[10], window) && (!SINKS || keys(a[12], sinks)));)
+                      p.whole(a[9], p.type, {tokens, (int64_t)p.c->n_q_heads, (int64_t)p.c->head_dim}, out) && keys(a[10], window) &&
+                      (!SINKS || keys(a[12], sinks)));)
     return result_of([&] {
         if (SINKS)
             return lib.paged_sink_attention(p.h, p.k_pages, p.v_pages, q, stride, (const int32_t *)p.start, (const int32_t *)p.len, (const int32_t *)p.table,
